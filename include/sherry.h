@@ -491,6 +491,207 @@ int sherry_gemv3_batched(const sherry_gemv_desc* descs_dev, int count,
                          int64_t total_blocks, void* stream);
 
 /* ---------------------------------------------------------------------- */
+/* The same products with an epilogue: bias, activation, gate, residual.   */
+/* ---------------------------------------------------------------------- */
+
+/* Activations of an epilogue, in fp32. */
+#define SHERRY_ACT_NONE 0
+#define SHERRY_ACT_RELU 1      /* max(z, 0)                                  */
+#define SHERRY_ACT_RELU2 2     /* max(z, 0)^2                                */
+#define SHERRY_ACT_SILU 3      /* z / (1 + exp(-z))                          */
+#define SHERRY_ACT_GELU 4      /* z (1 + erf(z / sqrt 2)) / 2                */
+#define SHERRY_ACT_GELU_TANH 5 /* z (1 + tanh(sqrt(2/pi)(z + 0.044715 z^3)))/2 */
+
+/* y[i][j] = act(p[i][j] + bias[j]) * gate[i][j] + residual[i][j], p the
+ * product's fp32 result as sherry_gemm, _channel or _group give it; each step
+ * is rounded to fp32.  All NULL and SHERRY_ACT_NONE: the product itself. */
+typedef struct sherry_epilogue {
+  const float* bias;       /* device, fp32 [n], 4-byte aligned, or NULL       */
+  const float* gate;       /* device, fp32 [m][gate_stride], or NULL          */
+  const float* residual;   /* device, fp32 [m][residual_stride], or NULL      */
+  int64_t gate_stride;     /* elements from row to row, >= n; 0: n            */
+  int64_t residual_stride; /* the same for residual                           */
+  int32_t act;             /* SHERRY_ACT_*                                    */
+  int32_t reserved;        /* set to 0                                        */
+} sherry_epilogue;
+
+/* Product of any m with an epilogue.  At most one of w_scales (per channel)
+ * and w_group_scales (per group) is not NULL (SHERRY_E_INVALID); with both
+ * NULL the weight scale is w_scale.  Other arguments as sherry_gemm (gate and
+ * residual may be y itself with stride n, and may not overlap it otherwise).
+ * Runs the VALU GEMV for m <= 4, the register-decoded kernel for more. */
+int sherry_gemm_epilogue(const uint8_t* w, const int8_t* x, const float* x_scale,
+                         float w_scale, const float* w_scales,
+                         const float* w_group_scales, const sherry_epilogue* epi,
+                         float* y, int64_t m, int64_t n, int64_t k, void* stream);
+
+/* One token of fp32 activations, quantized in the same launch (as
+ * sherry_gemv_f32: k <= SHERRY_FUSED_MAX_K, x 16-byte aligned, x_scale an
+ * output or NULL). */
+int sherry_gemv_f32_epilogue(const uint8_t* w, const float* x, float* x_scale,
+                             float w_scale, const float* w_scales,
+                             const float* w_group_scales, const sherry_epilogue* epi,
+                             float* y, int64_t n, int64_t k, void* stream);
+
+/* ---------------------------------------------------------------------- */
+/* Paged key-value cache: what stands between a layer's q/k/v and o.       */
+/*                                                                        */
+/* Row r of sequence b and key-value head h is slot r % page_size of page  */
+/* table[b][r / page_size].  A page holds kv_heads x page_size rows of     */
+/* head_dim values, so the rows of one head in one page are contiguous.    */
+/* Types: values of these codes.                                          */
+/* ---------------------------------------------------------------------- */
+
+#define SHERRY_F32 0
+#define SHERRY_F16 1
+#define SHERRY_BF16 2
+#define SHERRY_I8 3 /* caches only: int8 rows with one fp32 scale per row     */
+
+#define SHERRY_MAX_HEAD_DIM 256
+#define SHERRY_MAX_CACHE_ROWS (1LL << 30) /* table_width * page_size          */
+
+typedef struct sherry_cache_desc {
+  void* k;               /* device, [pages][kv_heads][page_size][head_dim],   */
+  void* v;               /* of type, 16-byte aligned                          */
+  float* k_scale;        /* device, fp32 [pages][kv_heads][page_size], 16-    */
+  float* v_scale;        /* byte aligned, with SHERRY_I8; else NULL           */
+  const int32_t* table;  /* device, int32 [batch][table_width]: page of each  */
+                         /* page_size rows.  An entry outside [0, pages) that */
+                         /* a sequence's length reaches makes its rows absent */
+  int64_t page_stride;   /* elements from page to page in k and v, a multiple */
+                         /* of 8 (SHERRY_I8: 16) and at least kv_heads *      */
+                         /* page_size * head_dim; 0: exactly that             */
+  int32_t type;          /* SHERRY_F16, SHERRY_BF16 or SHERRY_I8              */
+  int32_t pages;         /* >= 1                                              */
+  int32_t kv_heads;      /* 1 .. 4096                                         */
+  int32_t page_size;     /* >= 1                                              */
+  int32_t head_dim;      /* a multiple of 8 (SHERRY_I8: 16), 8 .. 256         */
+  int32_t batch;         /* sequences, 1 .. 65535                             */
+  int32_t table_width;   /* >= 1; table_width * page_size <=                  */
+                         /* SHERRY_MAX_CACHE_ROWS                             */
+  int32_t reserved;      /* set to 0                                          */
+} sherry_cache_desc;
+
+/* Pairs of a rotary embedding: (i, i + rot_dim / 2) or (2 i, 2 i + 1). */
+#define SHERRY_ROPE_HALVES 0
+#define SHERRY_ROPE_PAIRS 1
+
+/* New tokens of any number of sequences, with rotary positions. */
+typedef struct sherry_append_desc {
+  const void* q;         /* device, [tokens][heads][head_dim] of type, or     */
+                         /* NULL (heads is then ignored)                      */
+  const void* k;         /* device, [tokens][kv_heads][head_dim] of type      */
+  const void* v;         /* device, as k                                      */
+  void* q_out;           /* device, as q: q rotated; may be q                 */
+  const int32_t* seq;    /* device, int32 [tokens]: the token's sequence      */
+  const int32_t* slot;   /* device, int32 [tokens]: its row there             */
+  const int32_t* pos;    /* device, int32 [tokens]: its rotary position       */
+  const float* cos;      /* device, fp32 [rope_rows][rot_dim / 2], or both    */
+  const float* sin;      /* NULL: no rotation                                 */
+  float* weight;         /* device, fp32 [batch][kv_heads][row_stride] or     */
+                         /* NULL: set to 0 at the new rows                    */
+  int32_t* position;     /* the same in int32, or NULL: set to pos            */
+  int64_t row_stride;    /* >= table_width * page_size when weight or         */
+                         /* position is not NULL                              */
+  int64_t q_stride, k_stride, v_stride, q_out_stride; /* elements from token  */
+                         /* to token; 0: contiguous                           */
+  int32_t tokens;        /* >= 1                                              */
+  int32_t heads;
+  int32_t type;          /* of q, k, v and q_out: SHERRY_F32, _F16 or _BF16   */
+  int32_t rope_rows;     /* positions in cos and sin                          */
+  int32_t rot_dim;       /* even, 2 .. head_dim; later values are not rotated */
+  int32_t pairing;       /* SHERRY_ROPE_HALVES or SHERRY_ROPE_PAIRS           */
+} sherry_append_desc;
+
+/* Rotates q and k (a c - b s, b c + a s in fp32, each operation rounded),
+ * writes q_out, and stores k and v into the cache: rounded to nearest even,
+ * or with SHERRY_I8 quantized per row as sherry_quantize_act does (s = absmax
+ * / 127, clamp(rint(x / s), -127, 127); a zero row gives 0 and 0).  A token
+ * whose seq, slot, page or (with cos) pos is out of range is left out
+ * entirely.  No two tokens may have the same seq and slot.  Input rows are
+ * aligned to their element.  cache->table and the rows that exist are not
+ * changed; lengths are the caller's. */
+int sherry_cache_append(const sherry_cache_desc* cache, const sherry_append_desc* args,
+                        void* stream);
+
+/* Attention of one new token per sequence over its cached rows. */
+typedef struct sherry_attend_desc {
+  const void* q;         /* device, [batch][heads][head_dim] of type, 16-byte */
+                         /* aligned; query head i reads key-value head i /    */
+                         /* (heads / kv_heads)                                */
+  void* out;             /* device, as q                                      */
+  const int32_t* length; /* device, int32 [batch]: rows of each sequence      */
+                         /* (below 0: none; past the table: all of it)        */
+  const uint8_t* mask;   /* device, [batch][mask_stride], or NULL: rows with  */
+                         /* 0 are left out for every head                     */
+  const int32_t* position; /* device, int32 [batch][kv_heads][row_stride], or */
+                         /* NULL: what window goes by                         */
+  const int32_t* q_pos;  /* device, int32 [batch]: the token's own position   */
+                         /* (needed with position and window)                 */
+  float* weight;         /* device, fp32 [batch][kv_heads][row_stride], or    */
+                         /* NULL: each row's probabilities, summed over the   */
+                         /* query heads that share it, are added to it        */
+  void* workspace;       /* device, 16-byte aligned, workspace_bytes >=       */
+  size_t workspace_bytes;/* sherry_cache_attend_workspace; its contents do    */
+                         /* not matter                                        */
+  int64_t q_stride, out_stride; /* elements from token to token, a multiple   */
+                         /* of 8; 0: contiguous                               */
+  int64_t mask_stride, row_stride; /* >= table_width * page_size where used   */
+  int32_t heads;         /* a multiple of kv_heads                            */
+  int32_t type;          /* of q and out: SHERRY_F32, _F16 or _BF16           */
+  int32_t window;        /* 0: all rows; else the last window rows, or with   */
+                         /* position the rows with position > q_pos - window  */
+  float scale;           /* of the scores, e.g. head_dim ^ -1/2               */
+} sherry_attend_desc;
+
+/* Bytes of workspace that sherry_cache_attend needs with these descriptors
+ * (host only; pointers in them are only compared with NULL); 0 if they are
+ * invalid. */
+size_t sherry_cache_attend_workspace(const sherry_cache_desc* cache,
+                                     const sherry_attend_desc* args);
+
+/* out = sum_r p_r v_r, p = softmax over the rows left in of scale * q . k_r; a
+ * token with no row left in (or only scores of -infinity) gives 0.  Rows left
+ * out never reach the result, whatever they hold; a NaN or an infinity in the
+ * others makes the results that it enters NaN or infinite.  Scores, statistics and
+ * sums are in fp32; with fp32 q the products keep q and the probabilities to
+ * 22 bits and more, else the probabilities to 16. */
+int sherry_cache_attend(const sherry_cache_desc* cache, const sherry_attend_desc* args,
+                        void* stream);
+
+/* Cuts every sequence and key-value head down to `keep` rows. */
+typedef struct sherry_evict_desc {
+  const int32_t* length;   /* device, int32 [batch], as sherry_attend_desc    */
+  const float* weight;     /* device, fp32 [batch][kv_heads][row_stride]      */
+  const int32_t* position; /* device, int32, the same shape, or NULL: a row's */
+                           /* position is its slot                            */
+  const int32_t* recent_from; /* device, int32 [batch] or NULL: rows with     */
+                           /* position >= recent_from[b] come before all      */
+                           /* others, whatever their weight (if they are more */
+                           /* than keep: those in the lowest slots)           */
+  int32_t* length_out;     /* device, int32 [batch]: min(length, keep); may   */
+                           /* not be length                                   */
+  int32_t* kept;           /* device, int32 [batch][kv_heads][out_stride]:    */
+                           /* former slot of each row, -1 past the end        */
+  float* weight_out;       /* device, fp32, the same shape, or NULL, and      */
+  int32_t* position_out;   /* int32, or NULL: the kept rows' weight and       */
+                           /* position, 0 past the end                        */
+  int64_t row_stride, out_stride; /* >= table_width * page_size, >= keep      */
+  int32_t keep;            /* 1 .. SHERRY_MAX_CACHE_ROWS                      */
+  int32_t reserved;        /* set to 0                                        */
+} sherry_evict_desc;
+
+/* Keeps the rows with the largest accumulated weight (ties: lowest slot; NaN
+ * counts as -infinity).  Kept rows in slots below the new length stay where
+ * they are; those past it move, in ascending order, into the slots below it
+ * that were given up, so the cache is compacted in place with the fewest
+ * moves, and pages past ceil(length_out / page_size) are free.  k, v and the
+ * scales are moved in the pages (a move from or to an absent page is left
+ * out); weight and position are only read, and no output may overlap them. */
+int sherry_cache_evict(const sherry_cache_desc* cache, const sherry_evict_desc* args,
+                       void* stream);
+
+/* ---------------------------------------------------------------------- */
 /* Diagnostics.                                                            */
 /* ---------------------------------------------------------------------- */
 

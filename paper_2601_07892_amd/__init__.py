@@ -34,6 +34,12 @@ SHERRY_ALUT_MAX_K = 8192
 SHERRY_MAX_K = 174720
 SHERRY_MAX_M = 1 << 24
 SHERRY_FUSED_MAX_K = 32768
+SHERRY_ACT_NONE, SHERRY_ACT_RELU, SHERRY_ACT_RELU2 = 0, 1, 2
+SHERRY_ACT_SILU, SHERRY_ACT_GELU, SHERRY_ACT_GELU_TANH = 3, 4, 5
+SHERRY_F32, SHERRY_F16, SHERRY_BF16, SHERRY_I8 = 0, 1, 2, 3
+SHERRY_ROPE_HALVES, SHERRY_ROPE_PAIRS = 0, 1
+SHERRY_MAX_HEAD_DIM = 256
+SHERRY_MAX_CACHE_ROWS = 1 << 30
 
 EXPORTS = [
     "sherry_status_str", "sherry_version", "sherry_last_error", "sherry_packed_bytes", "sherry_pack",
@@ -49,6 +55,8 @@ EXPORTS = [
     "sherry_quantize_act_batched", "sherry_pack_il", "sherry_unpack_il",
     "sherry_gemv_f32_il_batched_prepare", "sherry_gemv_f32_il_batched",
     "sherry_gemm_il_batched_prepare", "sherry_gemm_il_batched", "sherry_interleave",
+    "sherry_gemm_epilogue", "sherry_gemv_f32_epilogue", "sherry_cache_append",
+    "sherry_cache_attend_workspace", "sherry_cache_attend", "sherry_cache_evict",
 ]
 
 
@@ -95,6 +103,60 @@ class sherry_quant_desc(ctypes.Structure):
         ("x", ctypes.c_void_p), ("q", ctypes.c_void_p), ("x_scale", ctypes.c_void_p),
         ("m", ctypes.c_int32), ("k", ctypes.c_int32), ("row_begin", ctypes.c_int32),
         ("reserved", ctypes.c_int32),
+    ]
+
+
+class sherry_epilogue(ctypes.Structure):
+    _fields_ = [
+        ("bias", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("residual", ctypes.c_void_p),
+        ("gate_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64),
+        ("act", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class sherry_cache_desc(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+        ("type", ctypes.c_int32), ("pages", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+        ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("batch", ctypes.c_int32),
+        ("table_width", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class sherry_append_desc(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("q_out", ctypes.c_void_p), ("seq", ctypes.c_void_p), ("slot", ctypes.c_void_p),
+        ("pos", ctypes.c_void_p), ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p),
+        ("weight", ctypes.c_void_p), ("position", ctypes.c_void_p),
+        ("row_stride", ctypes.c_int64), ("q_stride", ctypes.c_int64),
+        ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+        ("q_out_stride", ctypes.c_int64), ("tokens", ctypes.c_int32), ("heads", ctypes.c_int32),
+        ("type", ctypes.c_int32), ("rope_rows", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+        ("pairing", ctypes.c_int32),
+    ]
+
+
+class sherry_attend_desc(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("length", ctypes.c_void_p),
+        ("mask", ctypes.c_void_p), ("position", ctypes.c_void_p), ("q_pos", ctypes.c_void_p),
+        ("weight", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t), ("q_stride", ctypes.c_int64),
+        ("out_stride", ctypes.c_int64), ("mask_stride", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64), ("heads", ctypes.c_int32), ("type", ctypes.c_int32),
+        ("window", ctypes.c_int32), ("scale", ctypes.c_float),
+    ]
+
+
+class sherry_evict_desc(ctypes.Structure):
+    _fields_ = [
+        ("length", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("position", ctypes.c_void_p),
+        ("recent_from", ctypes.c_void_p), ("length_out", ctypes.c_void_p),
+        ("kept", ctypes.c_void_p), ("weight_out", ctypes.c_void_p),
+        ("position_out", ctypes.c_void_p), ("row_stride", ctypes.c_int64),
+        ("out_stride", ctypes.c_int64), ("keep", ctypes.c_int32), ("reserved", ctypes.c_int32),
     ]
 
 
@@ -169,6 +231,18 @@ def _load():
                                                 ctypes.c_int),
         "sherry_quantize_act_batched": ([vp, ctypes.c_int, i64, ctypes.c_int32, vp],
                                         ctypes.c_int),
+        "sherry_gemm_epilogue": ([vp, vp, vp, f32, vp, vp, ctypes.POINTER(sherry_epilogue), vp, i64,
+                                  i64, i64, vp], ctypes.c_int),
+        "sherry_gemv_f32_epilogue": ([vp, vp, vp, f32, vp, vp, ctypes.POINTER(sherry_epilogue), vp,
+                                      i64, i64, vp], ctypes.c_int),
+        "sherry_cache_append": ([ctypes.POINTER(sherry_cache_desc),
+                                 ctypes.POINTER(sherry_append_desc), vp], ctypes.c_int),
+        "sherry_cache_attend_workspace": ([ctypes.POINTER(sherry_cache_desc),
+                                           ctypes.POINTER(sherry_attend_desc)], ctypes.c_size_t),
+        "sherry_cache_attend": ([ctypes.POINTER(sherry_cache_desc),
+                                 ctypes.POINTER(sherry_attend_desc), vp], ctypes.c_int),
+        "sherry_cache_evict": ([ctypes.POINTER(sherry_cache_desc),
+                                ctypes.POINTER(sherry_evict_desc), vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -493,6 +567,46 @@ def sherry_gemm_il_batched_prepare(descs) -> tuple[int, int]:
 def sherry_gemm_il_batched(descs_dev, count: int, total_blocks: int, max_m: int, stream=None):
     _check(lib.sherry_gemm_il_batched(_ptr(descs_dev), count, total_blocks, max_m,
                                       _stream(stream)), "sherry_gemm_il_batched")
+
+
+# ---- products with an epilogue; the paged cache -----------------------------------
+# epi, cache and args: descriptors (the classes above) that the caller fills with
+# device pointers and keeps as long as the buffers.
+
+def sherry_gemm_epilogue(w, x, x_scale, w_scale: float, w_scales, w_group_scales, epi, y, m: int,
+                         n: int, k: int, stream=None):
+    """y = act(product + bias) * gate + residual of m tokens (int8 x [m][k])."""
+    _check(lib.sherry_gemm_epilogue(_ptr(w), _ptr(x), _ptr(x_scale), float(w_scale),
+                                    _ptr(w_scales), _ptr(w_group_scales), epi, _ptr(y), m, n, k,
+                                    _stream(stream)), "sherry_gemm_epilogue")
+
+
+def sherry_gemv_f32_epilogue(w, x, x_scale, w_scale: float, w_scales, w_group_scales, epi, y,
+                             n: int, k: int, stream=None):
+    """sherry_gemm_epilogue of one fp32 token, quantized in the same launch."""
+    _check(lib.sherry_gemv_f32_epilogue(_ptr(w), _ptr(x), _ptr(x_scale), float(w_scale),
+                                        _ptr(w_scales), _ptr(w_group_scales), epi, _ptr(y), n, k,
+                                        _stream(stream)), "sherry_gemv_f32_epilogue")
+
+
+def sherry_cache_append(cache, args, stream=None):
+    """Rotates the tokens of args (sherry_append_desc) and stores them in cache."""
+    _check(lib.sherry_cache_append(cache, args, _stream(stream)), "sherry_cache_append")
+
+
+def sherry_cache_attend_workspace(cache, args) -> int:
+    """Bytes of args.workspace (0: the descriptors are invalid)."""
+    return int(lib.sherry_cache_attend_workspace(cache, args))
+
+
+def sherry_cache_attend(cache, args, stream=None):
+    """Attention of one new token per sequence of cache (sherry_attend_desc)."""
+    _check(lib.sherry_cache_attend(cache, args, _stream(stream)), "sherry_cache_attend")
+
+
+def sherry_cache_evict(cache, args, stream=None):
+    """Cuts the sequences of cache down by weight (sherry_evict_desc)."""
+    _check(lib.sherry_cache_evict(cache, args, _stream(stream)), "sherry_cache_evict")
 
 
 def sherry_gemv2(w2, x, x_scale, w_scale: float, y, acc, n: int, k: int, stream=None):

@@ -229,6 +229,60 @@ extern "C" int sherry_gemm_channel(const uint8_t* w, const int8_t* x, const floa
   return gemm_dispatch(w, x, x_scale, WScale{w_scales, 0.0f}, y, acc, m, n, k, kernel, stream);
 }
 
+static_assert(sizeof(sherry_epilogue) == 48, "sherry_epilogue layout");
+
+namespace {
+// Checks an epilogue of rows of n and gives it as the kernels take it, with
+// the weight scales of the call.
+int check_epilogue(const sherry_epilogue* e, const float* w_scales, const float* w_group_scales,
+                   int64_t n, Epi* out) {
+  if (!e || (w_scales && w_group_scales)) return SHERRY_E_INVALID;
+  if (e->act < SHERRY_ACT_NONE || e->act > SHERRY_ACT_GELU_TANH) return SHERRY_E_INVALID;
+  if ((e->gate_stride != 0 && e->gate_stride < n) || (e->residual_stride != 0 && e->residual_stride < n))
+    return SHERRY_E_SHAPE;
+  if (!aligned(e->bias, 4) || !aligned(e->gate, 4) || !aligned(e->residual, 4) ||
+      !aligned(w_scales, 4) || !aligned(w_group_scales, 4))
+    return SHERRY_E_ALIGN;
+  *out = Epi{e->bias, e->gate, e->residual, e->gate_stride ? e->gate_stride : n,
+             e->residual_stride ? e->residual_stride : n, e->act};
+  return SHERRY_OK;
+}
+}  // namespace
+
+extern "C" int sherry_gemm_epilogue(const uint8_t* w, const int8_t* x, const float* x_scale,
+                                    float w_scale, const float* w_scales,
+                                    const float* w_group_scales, const sherry_epilogue* epi,
+                                    float* y, int64_t m, int64_t n, int64_t k, void* stream) {
+  const bool few = m <= kGemvMaxM;
+  int st = check_product(w, x, x_scale, y, m, n, k, few ? 4 : 16);
+  if (st != SHERRY_OK) return st;
+  Epi e;
+  st = check_epilogue(epi, w_scales, w_group_scales, n, &e);
+  if (st != SHERRY_OK) return st;
+  const WScale ws{w_scales, w_scale};
+  hipStream_t s = as_stream(stream);
+  if (w_group_scales)
+    return few ? launch_gemv_group(w, x, x_scale, w_group_scales, y, nullptr, m, n, k, s, &e)
+               : launch_wide_group(w, x, x_scale, w_group_scales, y, nullptr, m, n, k, s, &e);
+  return few ? launch_gemv_valu(w, x, x_scale, ws, y, nullptr, m, n, k, s, &e)
+             : launch_wide(w, x, x_scale, ws, y, nullptr, m, n, k, s, &e);
+}
+
+extern "C" int sherry_gemv_f32_epilogue(const uint8_t* w, const float* x, float* x_scale,
+                                        float w_scale, const float* w_scales,
+                                        const float* w_group_scales, const sherry_epilogue* epi,
+                                        float* y, int64_t n, int64_t k, void* stream) {
+  int st = check_fused(w, x, x_scale, y, nullptr, n, k);
+  if (st != SHERRY_OK) return st;
+  Epi e;
+  st = check_epilogue(epi, w_scales, w_group_scales, n, &e);
+  if (st != SHERRY_OK) return st;
+  hipStream_t s = as_stream(stream);
+  if (w_group_scales)
+    return launch_gemv_f32_group(w, x, x_scale, w_group_scales, y, nullptr, n, k, s, &e);
+  return launch_gemv_f32(w, x, x_scale, WScale{w_scales, w_scale}, y, nullptr, n, k, s, &e);
+}
+
 extern "C" int sherry_gemm(const uint8_t* w, const int8_t* x, const float* x_scale,
                            float w_scale, float* y, int32_t* acc, int64_t m, int64_t n,
                            int64_t k, void* stream) {

@@ -502,12 +502,12 @@ __device__ __forceinline__ void ring_run_groups_mfma(const UnitRun& run,
 // y = sx * sum over containers of float(acc_c) * gs[row][c], summed in fp32
 // in container order per wave and then over the S waves in order; redf is
 // LDS for the fp32 partial sums.
-template <int M, bool kGrp = false, bool kTotals = true, class X, class Prelude>
+template <int M, bool kGrp = false, bool kTotals = true, class X, class Prelude, class E = NoEpi>
 __device__ __forceinline__ void gemv_block(const uint8_t* w_, const X& xsrc, Prelude prelude,
                                            WScale ws, float* y, int32_t* acc_out, int64_t n,
                                            int k, int g, int S, const uint32_t* lut,
                                            int32_t* red, const float* gs = nullptr,
-                                           float* redf = nullptr) {
+                                           float* redf = nullptr, const E& epi = E{}) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int C = (k + kTileK - 1) / kTileK;
@@ -543,6 +543,17 @@ __device__ __forceinline__ void gemv_block(const uint8_t* w_, const X& xsrc, Pre
     const int64_t row0 = int64_t(r0) * kTileRows + (t & 63);
     swo[j] = (ws.rows && t < tpb * M * 64 && r0 < R && row0 < n) ? as_global(ws.rows)[row0]
                                                                   : ws.tensor;
+  }
+  // and so is what an epilogue reads
+  EpiValues ev[E::kUse ? kOut : 1];
+  if constexpr (E::kUse) {
+#pragma unroll
+    for (int j = 0; j < kOut; ++j) {
+      const int t = static_cast<int>(threadIdx.x) + j * kGemvThreads;
+      const int r0 = g * tpb + (t >> 6) / M;
+      const int64_t row0 = int64_t(r0) * kTileRows + (t & 63);
+      ev[j] = epi_load(epi, (t >> 6) % M, row0, t < tpb * M * 64 && r0 < R && row0 < n);
+    }
   }
   __builtin_amdgcn_sched_barrier(0);
   float accf[M];
@@ -635,6 +646,11 @@ __device__ __forceinline__ void gemv_block(const uint8_t* w_, const X& xsrc, Pre
   // inside the loop would also wait for the stores issued before it)
 #pragma unroll
   for (int j = 0; j < kOut; ++j) asm volatile("" ::"v"(swo[j]));
+  if constexpr (E::kUse) {
+#pragma unroll
+    for (int j = 0; j < kOut; ++j)
+      asm volatile("" ::"v"(ev[j].bias), "v"(ev[j].gate), "v"(ev[j].residual));
+  }
   // thread t -> (tile lt2, token m, row i); the S waves of a tile are adjacent
 #pragma unroll
   for (int j = 0; j < kOut; ++j) {
@@ -651,10 +667,14 @@ __device__ __forceinline__ void gemv_block(const uint8_t* w_, const X& xsrc, Pre
     if constexpr (kGrp) {
       float f = 0.0f;
       for (int p = 0; p < S; ++p) f += redf[((lt2 * S + p) * M + m) * 64 + i];
-      as_global_mut(y)[m * n + row] = f * sx[m];
+      f *= sx[m];
+      if constexpr (E::kUse) f = epi_apply(epi, f, ev[j]);
+      as_global_mut(y)[m * n + row] = f;
     } else {
       const float s = sx[m] * swo[j];
-      as_global_mut(y)[m * n + row] = static_cast<float>(a) * s;
+      float f = static_cast<float>(a) * s;
+      if constexpr (E::kUse) f = epi_apply(epi, f, ev[j]);
+      as_global_mut(y)[m * n + row] = f;
     }
     if (acc_out) as_global_mut(acc_out)[m * n + row] = a;
   }
@@ -865,24 +885,24 @@ __global__ __launch_bounds__(kGemvThreads) void gemv_tok_batched_kernel(
   }
 }
 
-template <int M>
+template <int M, class E = NoEpi>
 __global__ __launch_bounds__(kGemvThreads) void gemv_kernel(
     const uint8_t* __restrict__ w, const int8_t* __restrict__ x,
-    const float* __restrict__ x_scale, WScale ws, float* __restrict__ y,
-    int32_t* __restrict__ acc, int64_t n, int64_t k, int split) {
+    const float* __restrict__ x_scale, WScale ws, typename E::Out y,
+    int32_t* __restrict__ acc, int64_t n, int64_t k, int split, E epi) {
   __shared__ uint32_t lut[32];
   __shared__ int32_t red[kGemvWaves * M * 64];
   fill_lut(lut);
   gemv_block<M>(w, XFromSgpr<M>{as_const(reinterpret_cast<const int32_t*>(x)), static_cast<int>(k)},
                 ReadScales<M>{x_scale}, ws, y, acc, n, static_cast<int>(k), blockIdx.x, split,
-                lut, red);
+                lut, red, nullptr, nullptr, epi);
 }
 
-template <int M>
+template <int M, class E = NoEpi>
 __global__ __launch_bounds__(kGemvThreads) void gemv_group_kernel(
     const uint8_t* __restrict__ w, const int8_t* __restrict__ x,
-    const float* __restrict__ x_scale, const float* __restrict__ gs, float* __restrict__ y,
-    int32_t* __restrict__ acc, int64_t n, int64_t k, int split) {
+    const float* __restrict__ x_scale, const float* __restrict__ gs, typename E::Out y,
+    int32_t* __restrict__ acc, int64_t n, int64_t k, int split, E epi) {
   __shared__ uint32_t lut[32];
   __shared__ int32_t red[kGemvWaves * M * 64];
   __shared__ float redf[kGemvWaves * M * 64];
@@ -891,7 +911,7 @@ __global__ __launch_bounds__(kGemvThreads) void gemv_group_kernel(
                       XFromSgpr<M>{as_const(reinterpret_cast<const int32_t*>(x)),
                                    static_cast<int>(k)},
                       ReadScales<M>{x_scale}, WScale{nullptr, 0.0f}, y, acc, n,
-                      static_cast<int>(k), blockIdx.x, split, lut, red, gs, redf);
+                      static_cast<int>(k), blockIdx.x, split, lut, red, gs, redf, epi);
 }
 
 __global__ __launch_bounds__(kGemvThreads) void gemv_batched_kernel(
@@ -1013,13 +1033,13 @@ struct QuantizeRow {
 
 // Fused product of one block: the row length picks the quantizer (rows up
 // to 2048, 8192 and 16384 values from registers, longer ones in two passes).
-template <bool kGrp = false, bool kIL = false>
+template <bool kGrp = false, bool kIL = false, class E = NoEpi>
 __device__ __forceinline__ void fused_block(const uint8_t* w, const float* x, float* x_scale,
                                             bool write_scale, WScale ws, float* y,
                                             int32_t* acc, int64_t n, int k, int g, int S,
                                             const uint32_t* lut, int32_t* red, float* part,
                                             int8_t* xq, const float* gs = nullptr,
-                                            float* redf = nullptr) {
+                                            float* redf = nullptr, const E& epi = E{}) {
   const int kp = ((k + kTileK - 1) / kTileK) * kTileK;
   // per-tensor and per-channel scales sum a tile row's containers in int32 on
   // the matrix cores; per-group scales need each container's sum per lane;
@@ -1033,39 +1053,41 @@ __device__ __forceinline__ void fused_block(const uint8_t* w, const float* x, fl
   if (kp <= 4 * kGemvThreads) {
     gemv_block<1, kGrp>(w, xsrc,
                         QuantizeRow<1>{x, k, kp, xq, part, x_scale, write_scale}, ws, y, acc,
-                        n, k, g, S, lut, red, gs, redf);
+                        n, k, g, S, lut, red, gs, redf, epi);
   } else if (kp <= 16 * kGemvThreads) {
     gemv_block<1, kGrp>(w, xsrc,
                         QuantizeRow<4>{x, k, kp, xq, part, x_scale, write_scale}, ws, y, acc,
-                        n, k, g, S, lut, red, gs, redf);
+                        n, k, g, S, lut, red, gs, redf, epi);
   } else if (kp <= 32 * kGemvThreads) {
     gemv_block<1, kGrp>(w, xsrc,
                         QuantizeRow<8>{x, k, kp, xq, part, x_scale, write_scale}, ws, y, acc,
-                        n, k, g, S, lut, red, gs, redf);
+                        n, k, g, S, lut, red, gs, redf, epi);
   } else {
     gemv_block<1, kGrp>(w, xsrc,
                         QuantizeRow<0>{x, k, kp, xq, part, x_scale, write_scale}, ws, y, acc,
-                        n, k, g, S, lut, red, gs, redf);
+                        n, k, g, S, lut, red, gs, redf, epi);
   }
 }
 
+template <class E>
 __global__ __launch_bounds__(kGemvThreads) void gemv_f32_kernel(
     const uint8_t* __restrict__ w, const float* __restrict__ x, float* __restrict__ x_scale,
-    WScale ws, float* __restrict__ y, int32_t* __restrict__ acc, int64_t n, int64_t k,
-    int split) {
+    WScale ws, typename E::Out y, int32_t* __restrict__ acc, int64_t n, int64_t k,
+    int split, E epi) {
   __shared__ uint32_t lut[32];
   __shared__ int32_t red[kGemvWaves * 64];
   __shared__ float part[kGemvWaves];
   __shared__ __attribute__((aligned(16))) int8_t xq[kFusedMaxK];
   fill_lut(lut);
   fused_block(w, x, x_scale, blockIdx.x == 0, ws, y, acc, n, static_cast<int>(k), blockIdx.x,
-              split, lut, red, part, xq);
+              split, lut, red, part, xq, nullptr, nullptr, epi);
 }
 
+template <class E>
 __global__ __launch_bounds__(kGemvThreads) void gemv_f32_group_kernel(
     const uint8_t* __restrict__ w, const float* __restrict__ x, float* __restrict__ x_scale,
-    const float* __restrict__ gs, float* __restrict__ y, int32_t* __restrict__ acc, int64_t n,
-    int64_t k, int split) {
+    const float* __restrict__ gs, typename E::Out y, int32_t* __restrict__ acc, int64_t n,
+    int64_t k, int split, E epi) {
   __shared__ uint32_t lut[32];
   __shared__ int32_t red[kGemvWaves * 64];
   __shared__ float redf[kGemvWaves * 64];
@@ -1073,7 +1095,7 @@ __global__ __launch_bounds__(kGemvThreads) void gemv_f32_group_kernel(
   __shared__ __attribute__((aligned(16))) int8_t xq[kFusedMaxK];
   fill_lut(lut);
   fused_block<true>(w, x, x_scale, blockIdx.x == 0, WScale{nullptr, 0.0f}, y, acc, n,
-                    static_cast<int>(k), blockIdx.x, split, lut, red, part, xq, gs, redf);
+                    static_cast<int>(k), blockIdx.x, split, lut, red, part, xq, gs, redf, epi);
 }
 
 template <bool kIL>
@@ -1118,22 +1140,46 @@ __global__ __launch_bounds__(kGemvThreads) void gemv_f32_batched_kernel(
 
 }  // namespace
 
+namespace {
+template <class E>
+int launch_gemv_m(dim3 grid, hipStream_t s, const uint8_t* w, const int8_t* x,
+                  const float* x_scale, WScale ws, float* y, int32_t* acc, int64_t m, int64_t n,
+                  int64_t k, int S, const E& e) {
+  const dim3 block(kGemvThreads);
+  switch (m) {
+    case 1: return launch(gemv_kernel<1, E>, grid, block, 0, s, w, x, x_scale, ws, y, acc, n, k, S, e);
+    case 2: return launch(gemv_kernel<2, E>, grid, block, 0, s, w, x, x_scale, ws, y, acc, n, k, S, e);
+    case 3: return launch(gemv_kernel<3, E>, grid, block, 0, s, w, x, x_scale, ws, y, acc, n, k, S, e);
+    case 4: return launch(gemv_kernel<4, E>, grid, block, 0, s, w, x, x_scale, ws, y, acc, n, k, S, e);
+    default: return SHERRY_E_SHAPE;
+  }
+}
+template <class E>
+int launch_gemv_group_m(dim3 grid, hipStream_t s, const uint8_t* w, const int8_t* x,
+                        const float* x_scale, const float* gs, float* y, int32_t* acc, int64_t m,
+                        int64_t n, int64_t k, int S, const E& e) {
+  const dim3 block(kGemvThreads);
+  switch (m) {
+    case 1: return launch(gemv_group_kernel<1, E>, grid, block, 0, s, w, x, x_scale, gs, y, acc, n, k, S, e);
+    case 2: return launch(gemv_group_kernel<2, E>, grid, block, 0, s, w, x, x_scale, gs, y, acc, n, k, S, e);
+    case 3: return launch(gemv_group_kernel<3, E>, grid, block, 0, s, w, x, x_scale, gs, y, acc, n, k, S, e);
+    case 4: return launch(gemv_group_kernel<4, E>, grid, block, 0, s, w, x, x_scale, gs, y, acc, n, k, S, e);
+    default: return SHERRY_E_SHAPE;
+  }
+}
+}  // namespace
+
 int launch_gemv_valu(const uint8_t* w, const int8_t* x, const float* x_scale, WScale ws,
-                     float* y, int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s) {
+                     float* y, int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s,
+                     const Epi* epi) {
   const int64_t R = ceil_div(n, kTileRows);
   const int C = static_cast<int>(ceil_div(k, kTileK));
   // a lone launch has only this product to fill the GPU: split every tile
   // over all waves of a workgroup unless there are plenty of tiles
   const int S = (R * gemv_split(C) >= 4096) ? gemv_split(C) : kGemvWaves;
   const dim3 grid(static_cast<unsigned>(ceil_div(R * S, kGemvWaves)));
-  const dim3 block(kGemvThreads);
-  switch (m) {
-    case 1: return launch(gemv_kernel<1>, grid, block, 0, s, w, x, x_scale, ws, y, acc, n, k, S);
-    case 2: return launch(gemv_kernel<2>, grid, block, 0, s, w, x, x_scale, ws, y, acc, n, k, S);
-    case 3: return launch(gemv_kernel<3>, grid, block, 0, s, w, x, x_scale, ws, y, acc, n, k, S);
-    case 4: return launch(gemv_kernel<4>, grid, block, 0, s, w, x, x_scale, ws, y, acc, n, k, S);
-    default: return SHERRY_E_SHAPE;
-  }
+  return epi ? launch_gemv_m(grid, s, w, x, x_scale, ws, y, acc, m, n, k, S, *epi)
+             : launch_gemv_m(grid, s, w, x, x_scale, ws, y, acc, m, n, k, S, NoEpi{});
 }
 
 bool gemv_tok_fits(int64_t m, int64_t k) {
@@ -1203,28 +1249,25 @@ int launch_gemv_tok_batched(const sherry_gemm_desc* descs, int count, int64_t to
 }
 
 int launch_gemv_group(const uint8_t* w, const int8_t* x, const float* x_scale, const float* gs,
-                      float* y, int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s) {
+                      float* y, int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s,
+                      const Epi* epi) {
   const int64_t R = ceil_div(n, kTileRows);
   const int C = static_cast<int>(ceil_div(k, kTileK));
   const int S = (R * gemv_split(C) >= 4096) ? gemv_split(C) : kGemvWaves;
   const dim3 grid(static_cast<unsigned>(ceil_div(R * S, kGemvWaves)));
-  const dim3 block(kGemvThreads);
-  switch (m) {
-    case 1: return launch(gemv_group_kernel<1>, grid, block, 0, s, w, x, x_scale, gs, y, acc, n, k, S);
-    case 2: return launch(gemv_group_kernel<2>, grid, block, 0, s, w, x, x_scale, gs, y, acc, n, k, S);
-    case 3: return launch(gemv_group_kernel<3>, grid, block, 0, s, w, x, x_scale, gs, y, acc, n, k, S);
-    case 4: return launch(gemv_group_kernel<4>, grid, block, 0, s, w, x, x_scale, gs, y, acc, n, k, S);
-    default: return SHERRY_E_SHAPE;
-  }
+  return epi ? launch_gemv_group_m(grid, s, w, x, x_scale, gs, y, acc, m, n, k, S, *epi)
+             : launch_gemv_group_m(grid, s, w, x, x_scale, gs, y, acc, m, n, k, S, NoEpi{});
 }
 
 int launch_gemv_f32_group(const uint8_t* w, const float* x, float* x_scale, const float* gs,
-                          float* y, int32_t* acc, int64_t n, int64_t k, hipStream_t s) {
+                          float* y, int32_t* acc, int64_t n, int64_t k, hipStream_t s,
+                          const Epi* epi) {
   const int64_t R = ceil_div(n, kTileRows);
   const int C = static_cast<int>(ceil_div(k, kTileK));
   const int S = (R * gemv_split(C, kFusedTarget) >= 4096) ? gemv_split(C, kFusedTarget) : kGemvWaves;
-  return launch(gemv_f32_group_kernel, dim3(static_cast<unsigned>(ceil_div(R * S, kGemvWaves))),
-                dim3(kGemvThreads), 0, s, w, x, x_scale, gs, y, acc, n, k, S);
+  const dim3 grid(static_cast<unsigned>(ceil_div(R * S, kGemvWaves))), block(kGemvThreads);
+  return epi ? launch(gemv_f32_group_kernel<Epi>, grid, block, 0, s, w, x, x_scale, gs, y, acc, n, k, S, *epi)
+             : launch(gemv_f32_group_kernel<NoEpi>, grid, block, 0, s, w, x, x_scale, gs, y, acc, n, k, S, NoEpi{});
 }
 
 int launch_gemv_batched(const sherry_gemv_desc* descs, int count, int64_t total_blocks,
@@ -1235,12 +1278,13 @@ int launch_gemv_batched(const sherry_gemv_desc* descs, int count, int64_t total_
 }
 
 int launch_gemv_f32(const uint8_t* w, const float* x, float* x_scale, WScale ws, float* y,
-                    int32_t* acc, int64_t n, int64_t k, hipStream_t s) {
+                    int32_t* acc, int64_t n, int64_t k, hipStream_t s, const Epi* epi) {
   const int64_t R = ceil_div(n, kTileRows);
   const int C = static_cast<int>(ceil_div(k, kTileK));
   const int S = (R * gemv_split(C, kFusedTarget) >= 4096) ? gemv_split(C, kFusedTarget) : kGemvWaves;
-  return launch(gemv_f32_kernel, dim3(static_cast<unsigned>(ceil_div(R * S, kGemvWaves))),
-                dim3(kGemvThreads), 0, s, w, x, x_scale, ws, y, acc, n, k, S);
+  const dim3 grid(static_cast<unsigned>(ceil_div(R * S, kGemvWaves))), block(kGemvThreads);
+  return epi ? launch(gemv_f32_kernel<Epi>, grid, block, 0, s, w, x, x_scale, ws, y, acc, n, k, S, *epi)
+             : launch(gemv_f32_kernel<NoEpi>, grid, block, 0, s, w, x, x_scale, ws, y, acc, n, k, S, NoEpi{});
 }
 
 int launch_gemv_f32_batched(const sherry_gemv_f32_desc* descs, int count, int64_t total_blocks,

@@ -243,6 +243,63 @@ struct WScale {
   }
 };
 
+// Epilogue of a product: y = act(p + bias[n]) * gate[m][n] + residual[m][n], each
+// operation rounded (sherry_epilogue).  NoEpi: y = p.
+struct NoEpi {
+  static constexpr bool kUse = false;
+  using Out = float* __restrict__;  // the kernels' y
+  __host__ __device__ __forceinline__ NoEpi from(int64_t) const { return *this; }
+};
+struct Epi {
+  static constexpr bool kUse = true;
+  using Out = float*;  // (gate or residual may be y)
+  const float* bias;
+  const float* gate;
+  const float* residual;
+  int64_t gate_ld, residual_ld;
+  int act;
+  // Epilogue of the tokens from t on.
+  __host__ __device__ __forceinline__ Epi from(int64_t t) const {
+    Epi e = *this;
+    if (gate) e.gate += t * gate_ld;
+    if (residual) e.residual += t * residual_ld;
+    return e;
+  }
+};
+
+__device__ __forceinline__ float activate(float z, int act) {
+  switch (act) {
+    case SHERRY_ACT_RELU: return fmaxf(z, 0.0f);
+    case SHERRY_ACT_RELU2: return fmaxf(z, 0.0f) * fmaxf(z, 0.0f);
+    case SHERRY_ACT_SILU: return z / (1.0f + expf(-z));
+    case SHERRY_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    case SHERRY_ACT_GELU_TANH:
+      return 0.5f * z * (1.0f + tanhf(0.79788456080286536f * (z + 0.044715f * z * z * z)));
+    default: return z;
+  }
+}
+
+// What the epilogue of one output reads: loaded before the product's stream, so
+// that no load stands between the stores.
+struct EpiValues {
+  float bias = 0.0f, gate = 1.0f, residual = 0.0f;
+};
+__device__ __forceinline__ EpiValues epi_load(const Epi& e, int64_t m, int64_t n, bool in) {
+  EpiValues v;
+  if (e.bias && in) v.bias = as_global(e.bias)[n];
+  if (e.gate && in) v.gate = as_global(e.gate)[m * e.gate_ld + n];
+  if (e.residual && in) v.residual = as_global(e.residual)[m * e.residual_ld + n];
+  return v;
+}
+// (no operation that the epilogue does not ask for: p + 0 is not p for p = -0)
+__device__ __forceinline__ float epi_apply(const Epi& e, float p, const EpiValues& v) {
+  if (e.bias) p += v.bias;
+  p = activate(p, e.act);
+  if (e.gate) p *= v.gate;
+  if (e.residual) p += v.residual;
+  return p;
+}
+
 // ---- host-side launchers (each returns a sherry_status) -------------------
 
 int launch_quantize(const float* x, int64_t m, int64_t k, int8_t* q,
@@ -252,9 +309,10 @@ int launch_quantize(const float* x, int64_t m, int64_t k, int8_t* q,
 int launch_quantize_batched(const sherry_quant_desc* descs, int count, int64_t total_rows,
                             int64_t max_k, hipStream_t s);
 
+// epi: an epilogue, or NULL (here and below).
 int launch_gemv_valu(const uint8_t* w, const int8_t* x, const float* x_scale,
                      WScale ws, float* y, int32_t* acc, int64_t m,
-                     int64_t n, int64_t k, hipStream_t s);
+                     int64_t n, int64_t k, hipStream_t s, const Epi* epi = nullptr);
 
 // Activation-table product for one token (k <= SHERRY_ALUT_MAX_K).
 int launch_gemv_alut(const uint8_t* w, const int8_t* x, const float* x_scale, WScale ws,
@@ -288,24 +346,28 @@ int launch_smallm_batched(const sherry_gemm_desc* descs, int count, int64_t tota
 // per-group scales: lone, and grouped in wide_blocks(n) tile groups x blocks of
 // wide_batched_tokens(max_m) tokens.
 int launch_wide(const uint8_t* w, const int8_t* x, const float* x_scale, WScale ws, float* y,
-                int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s);
+                int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s,
+                const Epi* epi = nullptr);
 int launch_wide_group(const uint8_t* w, const int8_t* x, const float* x_scale, const float* gs,
-                      float* y, int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s);
+                      float* y, int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s,
+                      const Epi* epi = nullptr);
 int launch_wide_batched(const sherry_gemm_desc* descs, int count, int64_t total_blocks,
                         int max_m, bool groups, hipStream_t s);
 int launch_gemv_batched(const sherry_gemv_desc* descs, int count,
                         int64_t total_blocks, hipStream_t s);
 int launch_gemv_f32(const uint8_t* w, const float* x, float* x_scale, WScale ws, float* y,
-                    int32_t* acc, int64_t n, int64_t k, hipStream_t s);
+                    int32_t* acc, int64_t n, int64_t k, hipStream_t s, const Epi* epi = nullptr);
 // il: lane-interleaved units (sherry_pack_il; no per-group scales).
 int launch_gemv_f32_batched(const sherry_gemv_f32_desc* descs, int count, int64_t total_blocks,
                             bool il, hipStream_t s);
 // Per-group weight scales gs: fp32 [n][ceil(k/128)] (one per 128 weights of
 // a row).
 int launch_gemv_group(const uint8_t* w, const int8_t* x, const float* x_scale, const float* gs,
-                      float* y, int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s);
+                      float* y, int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s,
+                      const Epi* epi = nullptr);
 int launch_gemv_f32_group(const uint8_t* w, const float* x, float* x_scale, const float* gs,
-                          float* y, int32_t* acc, int64_t n, int64_t k, hipStream_t s);
+                          float* y, int32_t* acc, int64_t n, int64_t k, hipStream_t s,
+                          const Epi* epi = nullptr);
 
 // MFMA tile configuration chosen for an m x n product: 0 skinny (32 x 256),
 // 1 small (128 x 128), 2 mid (128 x 256), 3 large (256 x 256).

@@ -197,6 +197,50 @@ __device__ __forceinline__ void wd_slice(uint32_t (&wv)[32], const uint32_t (&d)
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// Whether an epilogue's rows can be read in 16-byte pieces where y's can be
+// written in them.
+__device__ __forceinline__ bool epi_pieces(const NoEpi&) { return true; }
+__device__ __forceinline__ bool epi_pieces(const Epi& e) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(e.bias) | reinterpret_cast<uintptr_t>(e.gate) |
+                      reinterpret_cast<uintptr_t>(e.residual);
+  return p % 16 == 0 && (!e.gate || e.gate_ld % 4 == 0) && (!e.residual || e.residual_ld % 4 == 0);
+}
+
+// What the epilogue of PN pieces (four rows of token t + 8 i each) reads.
+template <class E, int PN>
+struct WdExtra;
+template <int PN>
+struct WdExtra<NoEpi, PN> {};
+template <int PN>
+struct WdExtra<Epi, PN> {
+  float4 bias, gate[PN], residual[PN];
+  static __device__ __forceinline__ float4 four(const float* p, int left, bool whole) {
+    if (whole) return *reinterpret_cast<const SHERRY_GLOBAL float4*>(as_global(p));
+    float v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = u < left ? as_global(p)[u] : 0.0f;
+    return make_float4(v[0], v[1], v[2], v[3]);
+  }
+  __device__ __forceinline__ void load(const Epi& e, int t, int row, int m, int n, bool whole) {
+    const int left = whole ? 4 : n - row;  // rows of the piece that exist
+    if (e.bias) bias = four(e.bias + row, left, whole);
+#pragma unroll
+    for (int i = 0; i < PN; ++i) {
+      const int tok = t + 8 * i;
+      const int in = tok < m ? left : 0;
+      if (e.gate) gate[i] = four(e.gate + int64_t(tok) * e.gate_ld + row, in, whole);
+      if (e.residual)
+        residual[i] = four(e.residual + int64_t(tok) * e.residual_ld + row, in, whole);
+    }
+  }
+  __device__ __forceinline__ float4 apply(const Epi& e, float4 v, int i) const {
+    const EpiValues a{bias.x, gate[i].x, residual[i].x}, b{bias.y, gate[i].y, residual[i].y},
+        c{bias.z, gate[i].z, residual[i].z}, d{bias.w, gate[i].w, residual[i].w};
+    return make_float4(epi_apply(e, v.x, a), epi_apply(e, v.y, b), epi_apply(e, v.z, c),
+                       epi_apply(e, v.w, d));
+  }
+};
+
 // Workgroup g of problem p: tiles TILES * g .. TILES * g + TILES - 1, wave w:
 // tile w / S, part w % S of its units ([sp U, min((sp + 1) U, C)), U =
 // ceil(C/S); units past a part's end read zeros and multiply zeros).
@@ -206,8 +250,8 @@ __device__ __forceinline__ void wd_slice(uint32_t (&wv)[32], const uint32_t (&d)
 // next unit's stage readable and the previous one's free).  So the number
 // issued after any stage's last DMA is a constant, and the wait before each
 // barrier an exact vmcnt.
-template <class G>
-__device__ __forceinline__ void wd_block(const WdProblem& p, int g, int8_t* lds) {
+template <class G, class E = NoEpi>
+__device__ __forceinline__ void wd_block(const WdProblem& p, int g, int8_t* lds, const E& epi = E{}) {
   constexpr int MT = G::MT, S = G::S, W = G::W;
   constexpr int D = G::NST - 1;
   // opaque, so that a caller's loop over blocks keeps no address of this
@@ -508,13 +552,24 @@ __device__ __forceinline__ void wd_block(const WdProblem& p, int g, int8_t* lds)
   };
   const bool whole = p.m >= G::TOK && (r + 1) * kTileRows <= p.n && (p.n % 4 == 0) &&
                      (reinterpret_cast<uintptr_t>(p.y) % 16 == 0) &&
-                     (!acc_out || reinterpret_cast<uintptr_t>(acc_out) % 16 == 0);
+                     (!acc_out || reinterpret_cast<uintptr_t>(acc_out) % 16 == 0) && epi_pieces(epi);
   const bool vec = (p.n % 4 == 0) && (reinterpret_cast<uintptr_t>(p.y) % 16 == 0) &&
                    (!acc_out || reinterpret_cast<uintptr_t>(acc_out) % 16 == 0);
+  // what an epilogue reads of a block, a block ahead of its stores (a wait for a
+  // load between the stores would wait for those before it)
+  WdExtra<E, PN> extra[2];
+  auto fetch = [&](int b) {
+    if constexpr (E::kUse) {
+      const int row = r * kTileRows + 32 * (hs + b % HN) + 4 * c4;
+      extra[b & 1].load(epi, 32 * (b / HN) + tokb + (lane >> 3), row, p.m, p.n, whole);
+    }
+  };
+  fetch(0);
   put(0);
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     const int h = b % HN, tb = b / HN;
+    if (b + 1 < NB) fetch(b + 1);
     __asm__ volatile("" ::: "memory");
     const int32_t* st = strip + (b & 1) * 32 * kWdSW;
     v4i v[PN];
@@ -539,6 +594,7 @@ __device__ __forceinline__ void wd_block(const WdProblem& p, int g, int8_t* lds)
         o4.y = out(v[i].y, sx[i], swl[h][1]);
         o4.z = out(v[i].z, sx[i], swl[h][2]);
         o4.w = out(v[i].w, sx[i], swl[h][3]);
+        if constexpr (E::kUse) o4 = extra[b & 1].apply(epi, o4, i);
         *reinterpret_cast<float4*>(yp + int64_t(8 * i) * p.n) = o4;
         if (acc_out) *reinterpret_cast<v4i*>(ap + int64_t(8 * i) * p.n) = v[i];
       }
@@ -551,6 +607,10 @@ __device__ __forceinline__ void wd_block(const WdProblem& p, int g, int8_t* lds)
         float o4[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) o4[u] = out(vv[u], sx[i], swl[h][u]);
+        if constexpr (E::kUse) {
+          const float4 t = extra[b & 1].apply(epi, make_float4(o4[0], o4[1], o4[2], o4[3]), i);
+          o4[0] = t.x, o4[1] = t.y, o4[2] = t.z, o4[3] = t.w;
+        }
         float* yrow = as_global_mut(p.y) + int64_t(tok) * p.n + row;
         if (vec) {
           *reinterpret_cast<float4*>(yrow) = make_float4(o4[0], o4[1], o4[2], o4[3]);
@@ -579,9 +639,9 @@ __device__ __forceinline__ void wd_tokens(WdProblem& p, int64_t t0) {
 }
 
 // grid: x = groups of TILES tiles, y = token blocks (wide_xcd_order: in eighths)
-template <class G>
+template <class G, class E>
 __global__ __launch_bounds__(G::THREADS) __attribute__((amdgpu_waves_per_eu(G::EU))) void wide_kernel(
-    WdProblem p) {
+    WdProblem p, E epi) {
   __shared__ __attribute__((aligned(16))) int8_t lds[G::LDS];
   const int groups = static_cast<int>(gridDim.x);
   int g = blockIdx.x, tb = blockIdx.y;
@@ -591,7 +651,7 @@ __global__ __launch_bounds__(G::THREADS) __attribute__((amdgpu_waves_per_eu(G::E
     g = b - tb * groups;
   }
   wd_tokens<G>(p, int64_t(tb) * G::TOK);
-  wd_block<G>(p, g, lds);
+  wd_block<G>(p, g, lds, epi.from(int64_t(tb) * G::TOK));
 }
 
 // Grouped launch of 8 x 64 blocks, PER workgroups each (wide_run64).
@@ -687,8 +747,8 @@ __global__ __launch_bounds__(B::THREADS) __attribute__((amdgpu_waves_per_eu(B::E
 
 constexpr int64_t kWdMaxGridY = 32768;  // further token blocks go to further launches
 
-template <class G>
-int launch_wide_cfg(const WdProblem& p, hipStream_t s) {
+template <class G, class E>
+int launch_wide_cfg(const WdProblem& p, hipStream_t s, const E& epi) {
   const int64_t R = ceil_div(p.n, kTileRows), TB = ceil_div(p.m, G::TOK);
   for (int64_t b0 = 0; b0 < TB; b0 += kWdMaxGridY) {
     const int64_t nb = TB - b0 < kWdMaxGridY ? TB - b0 : kWdMaxGridY, t0 = b0 * G::TOK;
@@ -698,9 +758,9 @@ int launch_wide_cfg(const WdProblem& p, hipStream_t s) {
     q.y += t0 * p.n;
     if (q.acc) q.acc += t0 * p.n;
     q.m = static_cast<int>(p.m - t0);
-    const int rc = launch(wide_kernel<G>,
+    const int rc = launch(wide_kernel<G, E>,
                           dim3(static_cast<unsigned>(ceil_div(R, G::TILES)), static_cast<unsigned>(nb)),
-                          dim3(G::THREADS), 0, s, q);
+                          dim3(G::THREADS), 0, s, q, epi.from(t0));
     if (rc != SHERRY_OK) return rc;
   }
   return SHERRY_OK;
@@ -749,14 +809,26 @@ static_assert(wd_is<WdGrpMid<1>>(kWideGroupCost[kWideMid]) &&
                   wd_is<WdGrpTiny<1>>(kWideGroupCost[kWideTiny]),
               "the shapes that the cost model prices");
 
-template <int GR>
-int launch_wide_group_gr(const WdProblem& p, hipStream_t s) {
+template <int GR, class E>
+int launch_wide_group_gr(const WdProblem& p, hipStream_t s, const E& epi) {
   switch (wide_pick_group(p.m, p.n, p.k, GR == 4)) {
-    case kWideMid: return launch_wide_cfg<WdGrpMid<GR>>(p, s);
-    case kWideHalf: return launch_wide_cfg<WdGrpHalf<GR>>(p, s);
-    case kWidePair: return launch_wide_cfg<WdGrpPair<GR>>(p, s);
-    case kWideShort: return launch_wide_cfg<WdGrpShort<GR>>(p, s);
-    default: return launch_wide_cfg<WdGrpTiny<GR>>(p, s);
+    case kWideMid: return launch_wide_cfg<WdGrpMid<GR>>(p, s, epi);
+    case kWideHalf: return launch_wide_cfg<WdGrpHalf<GR>>(p, s, epi);
+    case kWidePair: return launch_wide_cfg<WdGrpPair<GR>>(p, s, epi);
+    case kWideShort: return launch_wide_cfg<WdGrpShort<GR>>(p, s, epi);
+    default: return launch_wide_cfg<WdGrpTiny<GR>>(p, s, epi);
+  }
+}
+
+template <class E>
+int launch_wide_shape(const WdProblem& p, hipStream_t s, const E& epi) {
+  switch (wide_pick(p.m, p.n, p.k)) {
+    case kWideLong: return launch_wide_cfg<WdLong>(p, s, epi);
+    case kWideMid: return launch_wide_cfg<WdMid>(p, s, epi);
+    case kWideHalf: return launch_wide_cfg<WdHalf>(p, s, epi);
+    case kWideQuarter: return launch_wide_cfg<WdQuarter>(p, s, epi);
+    case kWideShort: return launch_wide_cfg<WdShort>(p, s, epi);
+    default: return launch_wide_cfg<WdTiny>(p, s, epi);
   }
 }
 
@@ -777,21 +849,15 @@ int launch_wide_batched32_cfg(const sherry_gemm_desc* descs, int count, int64_t 
 }  // namespace
 
 int launch_wide(const uint8_t* w, const int8_t* x, const float* x_scale, WScale ws, float* y,
-                int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s) {
+                int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s, const Epi* epi) {
   const WdProblem p{w, x, x_scale, y, acc, static_cast<int>(n), static_cast<int>(k),
                     static_cast<int>(m), ws, nullptr};
-  switch (wide_pick(m, n, k)) {
-    case kWideLong: return launch_wide_cfg<WdLong>(p, s);
-    case kWideMid: return launch_wide_cfg<WdMid>(p, s);
-    case kWideHalf: return launch_wide_cfg<WdHalf>(p, s);
-    case kWideQuarter: return launch_wide_cfg<WdQuarter>(p, s);
-    case kWideShort: return launch_wide_cfg<WdShort>(p, s);
-    default: return launch_wide_cfg<WdTiny>(p, s);
-  }
+  return epi ? launch_wide_shape(p, s, *epi) : launch_wide_shape(p, s, NoEpi{});
 }
 
 int launch_wide_group(const uint8_t* w, const int8_t* x, const float* x_scale, const float* gs,
-                      float* y, int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s) {
+                      float* y, int32_t* acc, int64_t m, int64_t n, int64_t k, hipStream_t s,
+                      const Epi* epi) {
   if (acc) {
     // int32 totals from an unscaled launch (its y is overwritten below)
     const int rc = launch_wide(w, x, x_scale, WScale{nullptr, 1.0f}, y, acc, m, n, k, s);
@@ -800,7 +866,8 @@ int launch_wide_group(const uint8_t* w, const int8_t* x, const float* x_scale, c
   const WdProblem p{w, x, x_scale, y, nullptr, static_cast<int>(n), static_cast<int>(k),
                     static_cast<int>(m), WScale{nullptr, 0.0f}, gs};
   const bool pieces = ceil_div(k, kTileK) % 4 == 0 && (reinterpret_cast<uintptr_t>(gs) & 15) == 0;
-  return pieces ? launch_wide_group_gr<4>(p, s) : launch_wide_group_gr<1>(p, s);
+  if (epi) return pieces ? launch_wide_group_gr<4>(p, s, *epi) : launch_wide_group_gr<1>(p, s, *epi);
+  return pieces ? launch_wide_group_gr<4>(p, s, NoEpi{}) : launch_wide_group_gr<1>(p, s, NoEpi{});
 }
 
 int launch_wide_batched(const sherry_gemm_desc* descs, int count, int64_t total_blocks,
