@@ -10,8 +10,13 @@
 // head_dim operations per query head, far below what the matrix cores do in
 // that time, so the cache's bytes are the floor.
 //
-// Work mapping.  A workgroup of four waves takes one key-value head, up to 16
-// of its query heads and a run of 32-row tiles; wave w takes tiles w, w + 4, ...
+// Work mapping.  The 32-row tiles of all sequences, one after the other, are
+// cut into as many equal runs as workgroups fit the GPU; a workgroup of four
+// waves takes a run for one key-value head and up to 16 of its query heads.
+// The lengths are known to the device alone, so every workgroup finds its
+// place from them.  A run that passes the end of a sequence goes on with the
+// next one; what a workgroup finds for a sequence, unless it has all of it, is
+// joined by a second launch.  Wave w takes tiles w, w + 4, ... of its run.
 // Both products run on 16x16x32 MFMAs without moving anything between lanes:
 //  * S^T = K Q^T: lane l holds 8 values of row l % 16 of a 16-row half tile,
 //    dims of block l / 16, so a row is read with 16-byte loads as it lies; the
@@ -24,11 +29,15 @@
 //    eight rows into the V^T operands.  The sums have query head l % 16 in lane
 //    l again, so the running maximum rescales them lane by lane.
 //
-// Precision.  Cached values are exact in the operands.  q and p are split
-// into terms of bf16 (or, for f16 caches, f16) whose products are summed in
-// fp32: three bf16 terms hold all 24 bits, two 16; two f16 terms 22 (q is
-// scaled by a power of two per head, p by 2^14, so that their low terms stay
-// normal).  fp32 inputs take three and two, 16-bit inputs two.
+// Precision.  Cached values are exact in the operands (int8 rows as f16
+// integers, their scales applied to the scores and the probabilities).  q and
+// p are split into terms of bf16 (or, for f16 and int8 caches, f16) whose
+// products are summed in fp32: three bf16 terms hold all 24 bits, two 16; two
+// f16 terms 22 (q is scaled by a power of two per head, p by 2^14 over the
+// largest scale of V so far, so that their low terms stay normal).  fp32 inputs
+// take three and two, 16-bit inputs two.
+#include <type_traits>
+
 #include "cache_internal.h"
 
 namespace sherry {
@@ -40,9 +49,9 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;
-constexpr int kTile = 32;            // rows per wave and step
-constexpr int kMinTiles = 4;         // tiles of the shortest split: one per wave
-constexpr int kTargetGroups = 1024;  // workgroups that a launch is split into
+constexpr int kMinTiles = kWaves;  // tiles of the shortest run: one per wave
+constexpr int kCus = 256;
+constexpr int kTile = 32;          // rows per wave and step
 constexpr int kMaxGroup = 256;       // query heads per key-value head
 constexpr int kOutside = 0x7FFFFFF0;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -57,11 +66,13 @@ struct Attend {
   const int32_t* position;
   const int32_t* q_pos;
   float* weight;
-  float* sums;   // partial sums [split][y][gmax][DP]
-  float2* stat;  // their maximum (of the scores in units of ln 2) and sum
+  // what workgroup column w found for sequence b is part w + b
+  int2* parts;   // [batch]: a sequence's first part and how many it has
+  float2* stat;  // [part][y][gmax]: maximum (of scores in units of ln 2) and sum
+  float* sums;   // [part][y][gmax][DP]
   float* score;  // [batch][heads][score_stride], in units of ln 2 (weight only)
   int64_t q_stride, out_stride, mask_stride, row_stride, score_stride;
-  int heads, group, gtiles, gmax, type, window, target, splits;
+  int heads, group, gtiles, gmax, type, window, columns;
   float scale;
 };
 
@@ -70,7 +81,6 @@ struct Attend {
 // Rows [begin, end) of a sequence that can be attended to, and their tiles.
 struct Span {
   int begin, end;
-  __device__ __forceinline__ int first_tile() const { return begin / kTile; }
   __device__ __forceinline__ int tiles() const {
     return end > begin ? (end + kTile - 1) / kTile - begin / kTile : 0;
   }
@@ -87,58 +97,56 @@ __device__ __forceinline__ int wave_sum(int v) {
   return v;
 }
 
-// Tiles per split: the launch's tiles over its target of splits, so that the
-// lengths, which only the device knows, decide how many a sequence gets.
-__device__ __forceinline__ int split_tiles(const Attend& a) {
-  const int lane = threadIdx.x & 63;
-  int total = 0;
-  for (int b0 = 0; b0 < a.c.batch; b0 += 64)
-    total += b0 + lane < a.c.batch ? span_of(a, b0 + lane).tiles() : 0;
-  total = wave_sum(total);
-  const int t = (total + a.target - 1) / a.target;
-  return t <= kMinTiles ? kMinTiles : (t + kWaves - 1) / kWaves * kWaves;
-}
+// What a sequence costs a workgroup besides its tiles (finding it, its q, the
+// first loads, the sums' way out), in tiles.  Without it a workgroup that
+// gets many short sequences ends the launch.
+constexpr int kSequence = 6;
+__device__ __forceinline__ int cost_of(int tiles) { return tiles ? tiles + kSequence : 0; }
 
-// Sequence and part of split w; b = -1: there is no such split.
-struct Part {
-  int b, part;
+// Each workgroup column takes `run` of the sequences' costs, one after the
+// other; a sequence's first kSequence units are no tiles.
+struct Place {
+  int b, at;  // sequence, and the unit of its cost, where a column starts; b = -1: nowhere
+  int run;
 };
-__device__ __forceinline__ Part find_split(const Attend& a, int t, int w) {
+__device__ __forceinline__ Place find_place(const Attend& a, int w) {
   const int lane = threadIdx.x & 63;
+  const int n0 = lane < a.c.batch ? cost_of(span_of(a, lane).tiles()) : 0;
+  int total = n0;
+  for (int b = 64 + lane; b < a.c.batch; b += 64) total += cost_of(span_of(a, b).tiles());
+  total = wave_sum(total);
+  int run = (total + a.columns - 1) / a.columns;
+  run = run < kMinTiles ? kMinTiles : run;
+  const int64_t start = int64_t(w) * run;
+  if (start >= total) return Place{-1, 0, run};
   int before = 0;
   for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
-    const int n = b0 + lane < a.c.batch ? (span_of(a, b0 + lane).tiles() + t - 1) / t : 0;
+    const int n = b0 == 0 ? n0 : b0 + lane < a.c.batch ? cost_of(span_of(a, b0 + lane).tiles()) : 0;
     int upto = n;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int v = __shfl_up(upto, o, 64);
       if (lane >= o) upto += v;
     }
-    const uint64_t past = __ballot(before + upto > w);
+    const uint64_t past = __ballot(before + upto > start);
     if (past) {
       const int at = __builtin_ctzll(past);
       const int first = before + __shfl(upto - n, at, 64);
-      return Part{__builtin_amdgcn_readfirstlane(b0 + at),
-                  __builtin_amdgcn_readfirstlane(w - first)};
+      return Place{__builtin_amdgcn_readfirstlane(b0 + at),
+                   __builtin_amdgcn_readfirstlane(static_cast<int>(start) - first), run};
     }
     before += __shfl(upto, 63, 64);
   }
-  return Part{-1, 0};
+  return Place{-1, 0, run};
 }
-// First split of sequence b, and how many it has.
-struct Run {
-  int first, count;
-};
-__device__ __forceinline__ Run splits_of(const Attend& a, int t, int b) {
+// The next sequence from b on that has tiles (batch: none).
+__device__ __forceinline__ int next_sequence(const Attend& a, int b) {
   const int lane = threadIdx.x & 63;
-  int before = 0, own = 0;
-  for (int b0 = 0; b0 <= b; b0 += 64) {
-    const int i = b0 + lane;
-    const int n = i <= b && i < a.c.batch ? (span_of(a, i).tiles() + t - 1) / t : 0;
-    if (i < b) before += n;
-    if (i == b) own = n;
+  for (; b < a.c.batch; b += 64) {
+    const uint64_t some = __ballot(b + lane < a.c.batch && span_of(a, b + lane).tiles() > 0);
+    if (some) return __builtin_amdgcn_readfirstlane(b + static_cast<int>(__builtin_ctzll(some)));
   }
-  return Run{wave_sum(before), wave_sum(own)};
+  return a.c.batch;
 }
 
 // ---- operands -----------------------------------------------------------------
@@ -193,37 +201,57 @@ __device__ __forceinline__ void split(const float (&x)[8], u32x4 (&t)[NT]) {
     }
 }
 
-// Two words of int8 as eight bf16 values (exact).
-__device__ __forceinline__ float byte_f32(uint32_t w, int i) {
-  return static_cast<float>(static_cast<int8_t>(w >> (8 * i)));
-}
-__device__ __forceinline__ u32x4 bytes_bf16(uint32_t w0, uint32_t w1) {
+// Pairs of int8 as f16 (exact).  With its sign bit flipped a byte is u = x +
+// 128.  K: below a byte 0x64 it is the low byte of the f16 value 1024 + u.
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u32x4 bytes_f16(uint32_t w0, uint32_t w1) {
   u32x4 r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t w = i < 2 ? w0 : w1;
-    r[i] = upper(__float_as_uint(byte_f32(w, 2 * (i & 1) + 1)),
-                 __float_as_uint(byte_f32(w, 2 * (i & 1))));
+    const uint32_t w = (i < 2 ? w0 : w1) ^ 0x80808080u;
+    const uint32_t pair = __builtin_amdgcn_perm(0x64646464u, w, i & 1 ? 0x04030402u : 0x04010400u);
+    r[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, pair) - v2h{1152, 1152});
   }
   return r;
 }
+// V: byte i of lo and of hi (sign bits flipped) as the f16 values x 2^-9: u alone
+// is the subnormal u 2^-24, and u 2^-24 * 2^15 - 128 * 2^-9 is one operation.
+constexpr int kByteDown = 9;
+template <int i>
+__device__ __forceinline__ uint32_t byte_pair_f16(uint32_t hi, uint32_t lo) {
+  const uint32_t pair = __builtin_amdgcn_perm(hi, lo, 0x0C000C00u | (4 + i) << 16 | i);
+  const v2h v = __builtin_elementwise_fma(__builtin_bit_cast(v2h, pair), v2h{32768, 32768},
+                                          v2h{(_Float16)-0.25f, (_Float16)-0.25f});
+  return __builtin_bit_cast(uint32_t, v);
+}
 
+// The largest of a value in the lanes n, n + 16, n + 32, n + 48.
 __device__ __forceinline__ float max_over_blocks(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float sum_over_blocks(float v) {
   v += __shfl_xor(v, 16, 64);
   return v + __shfl_xor(v, 32, 64);
 }
 
+// Waves per SIMD, and workgroups per CU, that the registers allow without
+// spilling (more of them, spilling, were slower throughout: 16 sequences of 4000
+// to 8000 rows of 64 values 32 us with three, 39 with four; tiles of 64 rows
+// 34 .. 43).
+__host__ __device__ constexpr int waves_for(int dp) { return dp == 64 ? 3 : dp == 128 ? 2 : 1; }
+
 // CT: cache type; NT: terms of q and p; DP: head_dim rounded up to 64, 128 or
 // 256; ANY: pages of any size (else page_size % 16 == 0, so that a half tile
 // lies in one page and its rows are read through one buffer resource).
-template <int CT_, int NT_, int DP_, bool ANY_>
+// MORE: mask, position or weight are given.
+template <int CT_, int NT_, int DP_, bool ANY_, bool MORE_>
 struct Cfg {
   static constexpr int CT = CT_, NT = NT_, DP = DP_;
-  static constexpr bool ANY = ANY_, F16 = CT == SHERRY_F16, I8 = CT == SHERRY_I8;
+  static constexpr int EU = waves_for(DP);
+  static constexpr bool ANY = ANY_, MORE = MORE_, F16 = CT != SHERRY_BF16, I8 = CT == SHERRY_I8;
   static constexpr int E = I8 ? 1 : 2;         // bytes per value
   static constexpr int KS = DP / 32;           // MFMA steps of a score
   static constexpr int KL = DP * E / 64;       // 16-byte loads per lane and half tile of K
@@ -279,79 +307,115 @@ __device__ __forceinline__ void global_words(uint32_t* to, const char* p, bool i
 template <class G>
 struct Rows {
   const Attend& a;
-  int b, h, begin, end, qmin;  // rows with position <= qmin are left out
-  // the tile that was looked up last
-  uint32_t valid = 0;      // bit r: row r of the tile is attended to
-  int page[2] = {0, 0};    // !ANY: page of each half
-  int64_t row = 0;         // ANY: element offset of row lane % 32
-  int64_t srow = 0;        // ANY: the same of its scale
+  int b, h, begin, end;
+  const uint8_t* mask = nullptr;      // of b; NULL: not given
+  const int32_t* position = nullptr;  // of b and h; NULL: no window by them
+  int qmin = 0;                       // rows with position <= qmin are left out
+  // the tile whose look-up finished last
+  uint32_t valid = 0;       // bit r: row r of the tile is attended to
+  int rows[2] = {0, 0};     // !ANY: rows of each half that are read
+  int64_t at[2] = {0, 0};   // !ANY: element offset of each half
+  int64_t srow[2] = {0, 0}; // !ANY, int8: offset of the half's scales
+  int64_t row = 0;          // ANY: element offset of row lane % 32
+  int64_t sat = 0;          // ANY, int8: offset of its scale
+  // what a look-up has read of the tile after it
+  int next_page[2] = {-1, -1}, next_pos = 0;
+  uint32_t next_mask = 1;
+  bool next_on = true;
 
-  __device__ __forceinline__ void look_up(int tile) {
-    const int l = threadIdx.x & 31;
-    const int p0 = tile * kTile, p = p0 + l;
-    bool ok = p >= begin && p < end;
+  __device__ __forceinline__ Rows(const Attend& args, int b_, int h_, int begin_, int end_)
+      : a(args), b(b_), h(h_), begin(begin_), end(end_) {
+    if constexpr (G::MORE) {
+      if (a.mask) mask = a.mask + int64_t(b) * a.mask_stride;
+      if (a.position && a.window) {
+        position = a.position + (int64_t(b) * a.c.kv + h) * a.row_stride;
+        qmin = as_const(a.q_pos)[b] - a.window;
+      }
+    }
+  }
+
+  __device__ __forceinline__ int page_of(int tile, int t) const {
+    const int ph = tile * kTile + 16 * t;
+    return ph < end ? as_const(a.c.table)[int64_t(b) * a.c.width + a.c.by_page.quotient(ph)] : -1;
+  }
+  // Reads what decides a tile's rows; finish() uses it a tile later, when it
+  // has arrived.
+  __device__ __forceinline__ void start(int tile) {
+    const int l = threadIdx.x & 31, p0 = tile * kTile;
     if constexpr (G::ANY) {
-      const int i = a.c.by_page.div(p);
-      const int pid = ok ? as_global(a.c.table)[int64_t(b) * a.c.width + i] : -1;
-      ok = ok && pid >= 0 && pid < a.c.pages;
-      const int off = p - i * a.c.page_size;
-      row = ok ? a.c.at(pid, h) + int64_t(off) * a.c.dim : 0;
-      srow = ok ? a.c.scale_at(pid, h) + off : 0;
+      const int p = p0 + l;
+      const bool in = p >= begin && p < end;
+      next_page[0] = in ? as_global(a.c.table)[int64_t(b) * a.c.width + a.c.by_page.div(p)] : -1;
+      next_on = in;
     } else {
+      next_page[0] = page_of(tile, 0);
+      next_page[1] = page_of(tile, 1);
+    }
+    if constexpr (G::MORE) {
+      // (rows past the end read zeros, and are left out by it)
+      const int n = end - p0 < kTile ? end - p0 : kTile;
+      if (mask)
+        next_mask = __builtin_amdgcn_raw_buffer_load_b8(
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(mask) + p0, 0, n, kBufferWord3), l, 0, 0);
+      if (position)
+        next_pos = __builtin_amdgcn_raw_buffer_load_b32(
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(position) + p0, 0, 4 * n, kBufferWord3),
+            4 * l, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void finish(int tile) {
+    const int p0 = tile * kTile;
+    bool ok = next_on;
+    if constexpr (G::MORE) {
+      ok = ok && next_mask != 0 && (!position || next_pos > qmin);
+    }
+    if constexpr (G::ANY) {
+      const int p = p0 + (threadIdx.x & 31);
+      const int pid = next_page[0], off = p - a.c.by_page.div(p) * a.c.page_size;
+      ok = ok && pid >= 0 && pid < a.c.pages;
+      row = ok ? a.c.at(pid, h) + int64_t(off) * a.c.dim : 0;
+      if constexpr (G::I8) sat = ok ? a.c.scale_at(pid, h) + off : 0;
+      valid = static_cast<uint32_t>(__ballot(ok));
+    } else {
+      // (scalar: the rows from begin to end, and of pages that exist)
+      const uint32_t from = begin > p0 ? ~0u << (begin - p0) : ~0u;
+      const uint32_t to = end - p0 < kTile ? (1u << (end - p0)) - 1 : ~0u;
+      valid = from & to;
+      if constexpr (G::MORE) valid &= static_cast<uint32_t>(__ballot(ok));
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int ph = p0 + 16 * t;
-        const int i = a.c.by_page.div(ph);
-        const int pid = ph < end ? as_const(a.c.table)[int64_t(b) * a.c.width + i] : -1;
-        const bool in = pid >= 0 && pid < a.c.pages;
-        page[t] = in ? pid : 0;
-        if ((l >> 4) == t) ok = ok && in;
+        const bool in = static_cast<uint32_t>(next_page[t]) < static_cast<uint32_t>(a.c.pages);
+        if (!in) valid &= t ? 0xFFFFu : 0xFFFF0000u;
+        const int pid = in ? next_page[t] : 0;
+        const int off = ph - a.c.by_page.quotient(ph) * a.c.page_size;
+        rows[t] = valid >> (16 * t) & 0xFFFFu ? (end - ph < 16 ? end - ph : 16) : 0;
+        at[t] = a.c.at(pid, h) + int64_t(off) * a.c.dim;
+        if constexpr (G::I8) srow[t] = a.c.scale_at(pid, h) + off;
       }
     }
-    if (a.mask && ok) ok = as_global(a.mask)[int64_t(b) * a.mask_stride + p] != 0;
-    if (a.position && a.window && ok)
-      ok = as_global(a.position)[(int64_t(b) * a.c.kv + h) * a.row_stride + p] > qmin;
-    valid = static_cast<uint32_t>(__ballot(ok));
   }
 
-  __device__ __forceinline__ int half_bits(int t) const { return (valid >> (16 * t)) & 0xFFFF; }
-  // Rows of a half up to its last valid one.
-  __device__ __forceinline__ int half_rows(int t) const {
-    const int bits = half_bits(t);
-    return bits ? 32 - __builtin_clz(bits) : 0;
-  }
-  __device__ __forceinline__ __amdgpu_buffer_rsrc_t half(const char* pool, int tile, int t) const {
-    const int ph = tile * kTile + 16 * t;
-    const int off = ph - a.c.by_page.div(ph) * a.c.page_size;
-    const char* base = pool + (a.c.at(page[t], h) + int64_t(off) * a.c.dim) * G::E;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0,
-                                             half_rows(t) * a.c.dim * G::E, kBufferWord3);
-  }
-  __device__ __forceinline__ __amdgpu_buffer_rsrc_t half_scales(const float* pool, int tile,
-                                                                int t) const {
-    const int ph = tile * kTile + 16 * t;
-    const int off = ph - a.c.by_page.div(ph) * a.c.page_size;
-    const float* base = pool + a.c.scale_at(page[t], h) + off;
-    // (whole 16-byte pieces: those of rows past the last valid one lie in the page too)
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0,
-                                             ((half_rows(t) + 3) & ~3) * 4, kBufferWord3);
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t half(const char* pool, int t) const {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pool) + at[t] * G::E, 0,
+                                             rows[t] * a.c.dim * G::E, kBufferWord3);
   }
 
   // K: row lane % 16 of each half, dims of block lane / 16.
-  __device__ __forceinline__ void load_k(int tile, uint32_t (&k)[2][G::KL * 4]) const {
+  __device__ __forceinline__ void load_k(uint32_t (&k)[2][G::KL * 4]) const {
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       if constexpr (G::ANY) {
-        const int64_t at = __shfl(row, 16 * t + n, 64);
+        const int64_t from = __shfl(row, 16 * t + n, 64);
         const bool ok = (valid >> (16 * t + n)) & 1;
 #pragma unroll
         for (int s = 0; s < G::KL; ++s) {
           const int d = (G::I8 ? 64 : 32) * s + (G::I8 ? 16 : 8) * g;
-          global_words<4>(&k[t][4 * s], a.c.k + (at + d) * G::E, ok && d < a.c.dim);
+          global_words<4>(&k[t][4 * s], a.c.k + (from + d) * G::E, ok && d < a.c.dim);
         }
       } else {
-        const __amdgpu_buffer_rsrc_t r = half(a.c.k, tile, t);
+        const __amdgpu_buffer_rsrc_t r = half(a.c.k, t);
 #pragma unroll
         for (int s = 0; s < G::KL; ++s) {
           const int d = (G::I8 ? 64 : 32) * s + (G::I8 ? 16 : 8) * g;
@@ -360,14 +424,14 @@ struct Rows {
       }
     }
   }
-  // V: rows 16 (j / 4) + 4 (lane / 16) + j % 4, values of column lane % 16.
-  __device__ __forceinline__ void load_v(int tile, uint32_t (&v)[8][G::VW]) const {
+  // V: rows 4 (lane / 16) + 0..3 of each half, values of column lane % 16.
+  __device__ __forceinline__ void load_v(uint32_t (&v)[8][G::VW]) const {
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     constexpr int PW = G::VW / G::VP;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       __amdgpu_buffer_rsrc_t r;
-      if constexpr (!G::ANY) r = half(a.c.v, tile, t);
+      if constexpr (!G::ANY) r = half(a.c.v, t);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -375,319 +439,394 @@ struct Rows {
           const int d = v_dim<G>(n, 8 * c), hr = 4 * g + j;
           uint32_t* to = &v[4 * t + j][PW * c];
           if constexpr (G::ANY) {
-            const int64_t at = __shfl(row, 16 * t + hr, 64);
+            const int64_t from = __shfl(row, 16 * t + hr, 64);
             const bool ok = (valid >> (16 * t + hr)) & 1;
-            global_words<PW>(to, a.c.v + (at + d) * G::E, ok && d < a.c.dim);
+            global_words<PW>(to, a.c.v + (from + d) * G::E, ok && d < a.c.dim);
           } else {
             buffer_words<PW>(to, r, d < a.c.dim ? (hr * a.c.dim + d) * G::E : kOutside);
           }
         }
     }
   }
-  // Scales of rows 16 t + 4 (lane / 16) + 0..3.
-  __device__ __forceinline__ void load_scales(const float* pool, int tile, float (&s)[8]) const {
+  // Scales of rows 4 (lane / 16) + 0..3 of each half.
+  __device__ __forceinline__ void load_scales(const float* pool, float (&s)[8]) const {
     const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       if constexpr (G::ANY) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int hr = 16 * t + 4 * g + j;
-          const int64_t at = __shfl(srow, hr, 64);
-          s[4 * t + j] = (valid >> hr) & 1 ? as_global(pool)[at] : 0.0f;
+          const int r = 16 * t + 4 * g + j;
+          const int64_t from = __shfl(sat, r, 64);
+          s[4 * t + j] = (valid >> r) & 1 ? as_global(pool)[from] : 0.0f;
         }
       } else {
-        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(half_scales(pool, tile, t), 16 * g, 0, 0);
+        // (whole 16-byte pieces: those of rows past the last one lie in the page too)
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<float*>(pool) + srow[t], 0, ((rows[t] + 3) & ~3) * 4, kBufferWord3);
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, 16 * g, 0, 0);
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[4 * t + j] = __uint_as_float(v[j]);
       }
     }
   }
-  // Rows left out inside a half hold anything: their V values become zeros
-  // (those after its last valid row were not read, and are zeros already).
-  __device__ __forceinline__ bool holes(uint32_t bits) const {
-    const uint32_t lo = bits & 0xFFFF, hi = bits >> 16;
-    return (lo & (lo + 1)) != 0 || (hi & (hi + 1)) != 0;
+  // Whether rows that were read are left out: they hold anything, and their V
+  // values become zeros (rows that were not read are zeros already).
+  __device__ __forceinline__ bool holes() const {
+    return valid != ((1u << rows[0]) - 1 | ((1u << rows[1]) - 1) << 16);
   }
 };
 
-// grid: x = key-value heads x tiles of 16 query heads, y = splits
+template <class F, int... is>
+__device__ __forceinline__ void for_each(F&& f, std::integer_sequence<int, is...>) {
+  (f(std::integral_constant<int, is>{}), ...);
+}
+
+// q of one sequence in terms, and the factor of its scores in units of ln 2.
 template <class G>
-__global__ __launch_bounds__(64 * kWaves) void attend_kernel(Attend a) {
+__device__ __forceinline__ float load_q(const Attend& a, int b, int head0, int heads,
+                                        u32x4 (&qf)[G::NT][G::KS]) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  float factor = a.scale * kLog2e;
+  float q[G::KS][8];
+  const bool mine = n < heads;
+  const int64_t at = int64_t(b) * a.q_stride + int64_t(head0 + (mine ? n : 0)) * a.c.dim;
+  float top = 0.0f;
+#pragma unroll
+  for (int s = 0; s < G::KS; ++s) {
+    const int d = k_dim<G>(s, g);
+    const bool in = mine && d < a.c.dim;
+    if (a.type == SHERRY_F32) {
+      const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + d);
+      const float4 lo = in ? p[0] : make_float4(0, 0, 0, 0), hi = in ? p[1] : make_float4(0, 0, 0, 0);
+      q[s][0] = lo.x, q[s][1] = lo.y, q[s][2] = lo.z, q[s][3] = lo.w;
+      q[s][4] = hi.x, q[s][5] = hi.y, q[s][6] = hi.z, q[s][7] = hi.w;
+    } else {
+      const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) + at + d);
+      const u32x4 v = in ? *p : u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint16_t x = static_cast<uint16_t>(v[i >> 1] >> (16 * (i & 1)));
+        q[s][i] = a.type == SHERRY_BF16 ? from_bf16(x) : from_f16(x);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(q[s][i]));
+  }
+  if constexpr (G::F16) {
+    // q / 2^e in [-2, 2): exact, and far from f16's limits
+    top = max_over_blocks(top);
+    const int e = (__float_as_uint(top) >> 23) & 255;
+    const bool use = e > 0 && e < 254;
+    const float down = use ? __uint_as_float(static_cast<uint32_t>(254 - e) << 23) : 1.0f;
+    factor *= use ? __uint_as_float(static_cast<uint32_t>(e) << 23) : 1.0f;
+#pragma unroll
+    for (int s = 0; s < G::KS; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[s][i] *= down;
+  }
+#pragma unroll
+  for (int s = 0; s < G::KS; ++s) {
+    u32x4 t[G::NT];
+    split<G::F16, G::NT>(q[s], t);
+#pragma unroll
+    for (int i = 0; i < G::NT; ++i) qf[i][s] = t[i];
+  }
+  return factor;
+}
+
+// grid: x = key-value heads x tiles of 16 query heads, y = columns
+template <class G>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::EU))) void attend_kernel(
+    Attend a) {
   constexpr int DP = G::DP, NT = G::NT;
   __shared__ float red[kWaves * 16 * (DP + 4)];
   __shared__ float2 stat[kWaves][16];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int T = __builtin_amdgcn_readfirstlane(split_tiles(a));
-  const Part w = find_split(a, T, blockIdx.y);
-  if (w.b < 0) return;
-  const int b = w.b;
+  // (uniform values, which the compiler does not see through the wave's sums)
+  const Place place = find_place(a, blockIdx.y);
+  const int b_first = __builtin_amdgcn_readfirstlane(place.b);
+  if (b_first < 0) return;
   const int h = blockIdx.x / a.gtiles, gt = blockIdx.x - h * a.gtiles;
   const int heads = a.group - 16 * gt < 16 ? a.group - 16 * gt : 16;  // of this workgroup
   const int head0 = h * a.group + 16 * gt;
-  const Span sp = span_of(a, b);
-  const int begin = __builtin_amdgcn_readfirstlane(sp.begin);
-  const int end = __builtin_amdgcn_readfirstlane(sp.end);
-  const int t0 = begin / kTile + w.part * T;
-  const int all = (end + kTile - 1) / kTile;
-  const int t1 = t0 + T < all ? t0 + T : all;
+  const int run = __builtin_amdgcn_readfirstlane(place.run);
+  // of the run, and of b's cost before it
+  int left = run, at_cost = __builtin_amdgcn_readfirstlane(place.at);
+  for (int b = b_first; left > 0 && b < a.c.batch;
+       b = __builtin_amdgcn_readfirstlane(next_sequence(a, b + 1)), at_cost = 0) {
+    const Span sp = span_of(a, b);
+    const int begin = __builtin_amdgcn_readfirstlane(sp.begin);
+    const int end = __builtin_amdgcn_readfirstlane(sp.end);
+    const int tiles = __builtin_amdgcn_readfirstlane(sp.tiles());
+    // units [at_cost, upto) of the sequence's cost: the tiles among them
+    const int upto = tiles + kSequence < at_cost + left ? tiles + kSequence : at_cost + left;
+    left -= upto - at_cost;
+    const int n0 = at_cost > kSequence ? at_cost - kSequence : 0, n1 = upto - kSequence;
+    if (n1 <= n0) continue;  // (the next column takes the first tiles)
+    const int t0 = begin / kTile + n0, t1 = begin / kTile + n1;
 
-  // q in terms, and the factor of its scores in units of ln 2
-  u32x4 qf[NT][G::KS];
-  float factor = a.scale * kLog2e;
-  {
-    float q[G::KS][8];
-    const bool mine = n < heads;
-    const int64_t at = int64_t(b) * a.q_stride + int64_t(head0 + (mine ? n : 0)) * a.c.dim;
-    float top = 0.0f;
+    u32x4 qf[NT][G::KS];
+    const float factor = load_q<G>(a, b, head0, heads, qf);
+    Rows<G> rows(a, b, h, begin, end);
+    float* score = nullptr;  // of this lane's head, and its rows of a tile
+    if (G::MORE && a.weight)
+      score = a.score + (int64_t(b) * a.heads + head0 + (n < heads ? n : 0)) * a.score_stride + 4 * g;
+    constexpr float kUp = G::F16 ? 14.0f : 0.0f;  // p is held times 2^14 in f16
+    v4f o[G::CH];
 #pragma unroll
-    for (int s = 0; s < G::KS; ++s) {
-      const int d = k_dim<G>(s, g);
-      const bool in = mine && d < a.c.dim;
-      if (a.type == SHERRY_F32) {
-        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + d);
-        const float4 lo = in ? p[0] : make_float4(0, 0, 0, 0), hi = in ? p[1] : make_float4(0, 0, 0, 0);
-        q[s][0] = lo.x, q[s][1] = lo.y, q[s][2] = lo.z, q[s][3] = lo.w;
-        q[s][4] = hi.x, q[s][5] = hi.y, q[s][6] = hi.z, q[s][7] = hi.w;
-      } else {
-        const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) + at + d);
-        const u32x4 v = in ? *p : u32x4{0, 0, 0, 0};
+    for (int e = 0; e < G::CH; ++e) o[e] = v4f{0, 0, 0, 0};
+    float m = kMinusInf, l = 0.0f;
+    // int8: V's scales are held over 2^ve, the largest of them so far
+    int ve = -126;
+
+    uint32_t kr[2][G::KL * 4], vr[8][G::VW];
+    float ksc[8], vsc[8];
+    int tile = t0 + wave;
+    if (tile < t1) {
+      rows.start(tile);
+      rows.finish(tile);
+      rows.load_k(kr);
+      if constexpr (G::I8) rows.load_scales(a.c.ks, ksc);
+      rows.load_v(vr);
+      if constexpr (G::I8) rows.load_scales(a.c.vs, vsc);
+      if (tile + kWaves < t1) rows.start(tile + kWaves);
+    }
+    for (; tile < t1; tile += kWaves) {
+      const uint32_t valid = rows.valid;
+      const bool holes = !G::I8 && !G::ANY && rows.holes();
+      const int next = tile + kWaves;
+      v4f s[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) s[t] = v4f{0, 0, 0, 0};
+#pragma unroll
+      for (int st = 0; st < G::KS; ++st)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          u32x4 kf;
+          if constexpr (G::I8) {
+            kf = bytes_f16(kr[t][2 * st], kr[t][2 * st + 1]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) kf[i] = kr[t][4 * st + i];
+          }
+#pragma unroll
+          for (int i = NT - 1; i >= 0; --i) s[t] = mfma<G::F16>(kf, qf[i][st], s[t]);
+        }
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        x[i] = s[i >> 2][i & 3] * (G::I8 ? factor * ksc[i] : factor);
+      if (next < t1) {
+        rows.finish(next);
+        rows.load_k(kr);
+        if constexpr (G::I8) rows.load_scales(a.c.ks, ksc);
+        if (next + kWaves < t1) rows.start(next + kWaves);
+      }
+      uint32_t mine = 0xFF;  // bit i: row of x[i] is attended to
+      if (valid != 0xFFFFFFFFu) {
+        mine = ((valid >> (4 * g)) & 0xF) | (((valid >> (16 + 4 * g)) & 0xF) << 4);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const uint16_t x = static_cast<uint16_t>(v[i >> 1] >> (16 * (i & 1)));
-          q[s][i] = a.type == SHERRY_BF16 ? from_bf16(x) : from_f16(x);
+          x[i] = (mine >> i) & 1 ? x[i] : kMinusInf;
+          if constexpr (G::I8) vsc[i] = (mine >> i) & 1 ? vsc[i] : 0.0f;
         }
       }
+      if (G::MORE && a.weight && n < heads) {
+        float* to = score + tile * kTile;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(q[s][i]));
-    }
-    if constexpr (G::F16) {
-      // q / 2^e in [-2, 2): exact, and far from f16's limits
-      top = max_over_blocks(top);
-      const int e = (__float_as_uint(top) >> 23) & 255;
-      const bool use = e > 0 && e < 254;
-      const float down = use ? __uint_as_float(static_cast<uint32_t>(254 - e) << 23) : 1.0f;
-      factor *= use ? __uint_as_float(static_cast<uint32_t>(e) << 23) : 1.0f;
+        for (int t = 0; t < 2; ++t)
+          *reinterpret_cast<SHERRY_GLOBAL v4f*>(as_global_mut(to) + 16 * t) =
+              v4f{x[4 * t], x[4 * t + 1], x[4 * t + 2], x[4 * t + 3]};
+      }
+      float top = x[0];
 #pragma unroll
-      for (int s = 0; s < G::KS; ++s)
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
+      top = fmaxf(m, max_over_blocks(top));
+      const float base = top == kMinusInf ? 0.0f : top;
+      int vt = ve;
+      if constexpr (G::I8) {
+        float big = 0.0f;  // of the tile's V scales
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[s][i] *= down;
-    }
+        for (int i = 0; i < 8; ++i) big = fmaxf(big, vsc[i]);
+        big = max_over_blocks(big);
+        const int e = static_cast<int>(__float_as_uint(big) >> 23) - 127;
+        vt = e > ve ? (e < 127 ? e : 127) : ve;
+      }
+      if (__any(top > m || vt > ve)) {
+        float down = __builtin_amdgcn_exp2f(m - base);
+        l *= down;
+        if constexpr (G::I8) down = ldexpf(down, ve - vt);
 #pragma unroll
-    for (int s = 0; s < G::KS; ++s) {
-      u32x4 t[NT];
-      split<G::F16, NT>(q[s], t);
+        for (int e = 0; e < G::CH; ++e)
 #pragma unroll
-      for (int i = 0; i < NT; ++i) qf[i][s] = t[i];
-    }
-  }
-
-  Rows<G> rows{a, b, h, begin, end,
-               a.position && a.window ? as_global(a.q_pos)[b] - a.window : 0};
-  constexpr float kUp = G::F16 ? 14.0f : 0.0f;  // p is held times 2^14 in f16
-  v4f o[G::CH];
+          for (int r = 0; r < 4; ++r) o[e][r] *= down;
+        m = top;
+        ve = vt;
+      }
+      if (holes) {
 #pragma unroll
-  for (int e = 0; e < G::CH; ++e) o[e] = v4f{0, 0, 0, 0};
-  float m = kMinusInf, l = 0.0f;
-
-  uint32_t kr[2][G::KL * 4], vr[8][G::VW];
-  float ksc[8], vsc[8];
-  int tile = t0 + wave;
-  if (tile < t1) {
-    rows.look_up(tile);
-    rows.load_k(tile, kr);
-    if constexpr (G::I8) rows.load_scales(a.c.ks, tile, ksc);
-    rows.load_v(tile, vr);
-    if constexpr (G::I8) rows.load_scales(a.c.vs, tile, vsc);
-  }
-  for (; tile < t1; tile += kWaves) {
-    const uint32_t valid = rows.valid;
-    const int next = tile + kWaves;
-    v4f s[2];
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
-    for (int t = 0; t < 2; ++t) s[t] = v4f{0, 0, 0, 0};
+          for (int i = 0; i < G::VW; ++i) vr[j][i] = (mine >> j) & 1 ? vr[j][i] : 0;
+      }
+      const float low = base - kUp, vdown = G::I8 ? ldexpf(1.0f, -ve) : 1.0f;
+      float p[8];
 #pragma unroll
-    for (int st = 0; st < G::KS; ++st)
+      for (int i = 0; i < 8; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(x[i] - low);
+        l += p[i];
+        if constexpr (G::I8) p[i] *= vsc[i] * vdown;
+      }
+      u32x4 pf[NT];
+      split<G::F16, NT>(p, pf);
+      if constexpr (G::I8) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        u32x4 kf;
-        if constexpr (G::I8) {
-          kf = bytes_bf16(kr[t][2 * st], kr[t][2 * st + 1]);
-        } else {
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) kf[i] = kr[t][4 * st + i];
+          for (int i = 0; i < G::VW; ++i) vr[j][i] ^= 0x80808080u;
+      }
+      auto value = [&](auto ec) {
+        constexpr int e = decltype(ec)::value;
+        u32x4 vf;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (G::I8)
+            vf[i] = byte_pair_f16<e & 3>(vr[2 * i + 1][e >> 2], vr[2 * i][e >> 2]);
+          else
+            vf[i] = e & 1 ? upper(vr[2 * i + 1][e >> 1], vr[2 * i][e >> 1])
+                          : lower(vr[2 * i + 1][e >> 1], vr[2 * i][e >> 1]);
         }
 #pragma unroll
-        for (int i = NT - 1; i >= 0; --i) s[t] = mfma<G::F16>(kf, qf[i][st], s[t]);
+        for (int i = NT - 1; i >= 0; --i) o[e] = mfma<G::F16>(vf, pf[i], o[e]);
+      };
+      for_each(value, std::make_integer_sequence<int, G::CH>{});
+      if (next < t1) {
+        rows.load_v(vr);
+        if constexpr (G::I8) rows.load_scales(a.c.vs, vsc);
       }
-    float x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      x[i] = s[i >> 2][i & 3] * factor;
-      if constexpr (G::I8) x[i] *= ksc[i];
     }
-    if (next < t1) {
-      rows.look_up(next);
-      rows.load_k(next, kr);
-      if constexpr (G::I8) rows.load_scales(a.c.ks, next, ksc);
-    }
-    uint32_t mine = 0xFF;  // bit i: row of x[i] is attended to
-    if (valid != 0xFFFFFFFFu) {
-      mine = ((valid >> (4 * g)) & 0xF) | (((valid >> (16 + 4 * g)) & 0xF) << 4);
+
+    // the four waves' sums at their common maximum
+    l = sum_over_blocks(l);
+    if (g == 0) stat[wave][n] = make_float2(m, l);
+    __syncthreads();
+    float top = kMinusInf;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = (mine >> i) & 1 ? x[i] : kMinusInf;
-    }
-    if (a.weight && n < heads) {
-      float* to = a.score + (int64_t(b) * a.heads + head0 + n) * a.score_stride + tile * kTile + 4 * g;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        *reinterpret_cast<float4*>(to + 16 * t) = make_float4(x[4 * t], x[4 * t + 1], x[4 * t + 2], x[4 * t + 3]);
-    }
-    float top = x[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
-    top = fmaxf(m, max_over_blocks(top));
-    const float base = top == kMinusInf ? 0.0f : top;
-    if (__any(top > m)) {
-      const float down = __builtin_amdgcn_exp2f(m - base);
-      l *= down;
+    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, stat[i][n].x);
+    float down = m == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+    if constexpr (G::I8) down = ldexpf(down, ve + kByteDown);
+    if (n < heads) {
 #pragma unroll
       for (int e = 0; e < G::CH; ++e)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[e][r] *= down;
-      m = top;
+        for (int r = 0; r < 4; ++r)
+          red[(wave * 16 + n) * (DP + 4) + v_dim<G>(4 * g + r, e)] = m == kMinusInf ? 0.0f : o[e][r] * down;
     }
-    float p[8];
+    __syncthreads();
+    const bool whole = t1 - t0 == tiles;  // nothing to join
+    const int64_t at = ((int64_t(blockIdx.y) + b) * gridDim.x + blockIdx.x) * a.gmax;
+    auto sum_of = [&](int hd) {
+      float mx = kMinusInf, sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(x[i] - base + kUp);
-      l += p[i];
-      if constexpr (G::I8) p[i] = (mine >> i) & 1 ? p[i] * vsc[i] : 0.0f;
-    }
-    u32x4 pf[NT];
-    split<G::F16, NT>(p, pf);
-    if (!G::I8 && !G::ANY && rows.holes(valid)) {
+      for (int i = 0; i < kWaves; ++i) mx = fmaxf(mx, stat[i][hd].x);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int i = 0; i < kWaves; ++i)
+        if (stat[i][hd].x != kMinusInf) sum += stat[i][hd].y * __builtin_amdgcn_exp2f(stat[i][hd].x - mx);
+      return make_float2(mx, sum);
+    };
+    for (int i = threadIdx.x; i < heads * DP; i += 64 * kWaves) {
+      const int hd = i / DP, d = i % DP;
+      float v = 0.0f;
 #pragma unroll
-        for (int i = 0; i < G::VW; ++i) vr[j][i] = (mine >> j) & 1 ? vr[j][i] : 0;
-    }
-#pragma unroll
-    for (int e = 0; e < G::CH; ++e) {
-      u32x4 vf;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (G::I8)
-          vf[i] = upper(__float_as_uint(byte_f32(vr[2 * i + 1][e >> 2], e & 3)),
-                        __float_as_uint(byte_f32(vr[2 * i][e >> 2], e & 3)));
-        else
-          vf[i] = e & 1 ? upper(vr[2 * i + 1][e >> 1], vr[2 * i][e >> 1])
-                        : lower(vr[2 * i + 1][e >> 1], vr[2 * i][e >> 1]);
+      for (int j = 0; j < kWaves; ++j) v += red[(j * 16 + hd) * (DP + 4) + d];
+      if (whole) {
+        const float sum = sum_of(hd).y;
+        if (d < a.c.dim)
+          store_from_f32(a.out, int64_t(b) * a.out_stride + int64_t(head0 + hd) * a.c.dim + d, a.type,
+                         sum == 0.0f ? 0.0f : v / sum);
+      } else {
+        as_global_mut(a.sums)[(at + hd) * DP + d] = v;
       }
-#pragma unroll
-      for (int i = NT - 1; i >= 0; --i) o[e] = mfma<G::F16>(vf, pf[i], o[e]);
     }
-    if (next < t1) {
-      rows.load_v(next, vr);
-      if constexpr (G::I8) rows.load_scales(a.c.vs, next, vsc);
+    if (threadIdx.x < heads) as_global_mut(a.stat)[at + threadIdx.x] = sum_of(threadIdx.x);
+    if (n0 == 0 && blockIdx.x == 0 && threadIdx.x == 0) {
+      // the rest of the sequence is in whole runs and a last one
+      const int more = tiles - n1;
+      as_global_mut(a.parts)[b] = make_int2(static_cast<int>(blockIdx.y) + b, 1 + (more + run - 1) / run);
     }
-  }
-
-  // the four waves' sums at their common maximum
-  l = sum_over_blocks(l);
-  if (g == 0) stat[wave][n] = make_float2(m, l);
-  __syncthreads();
-  float top = kMinusInf;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) top = fmaxf(top, stat[i][n].x);
-  const float down = m == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
-  if (n < heads) {
-#pragma unroll
-    for (int e = 0; e < G::CH; ++e)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        red[(wave * 16 + n) * (DP + 4) + v_dim<G>(4 * g + r, e)] = m == kMinusInf ? 0.0f : o[e][r] * down;
-  }
-  __syncthreads();
-  const int64_t at = (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * a.gmax;
-  for (int i = threadIdx.x; i < heads * DP; i += 64 * kWaves) {
-    const int hd = i / DP, d = i % DP;
-    float v = 0.0f;
-#pragma unroll
-    for (int j = 0; j < kWaves; ++j) v += red[(j * 16 + hd) * (DP + 4) + d];
-    a.sums[(at + hd) * DP + d] = v;
-  }
-  if (threadIdx.x < heads) {
-    const int hd = threadIdx.x;
-    float mx = kMinusInf, sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) mx = fmaxf(mx, stat[i][hd].x);
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i)
-      if (stat[i][hd].x != kMinusInf) sum += stat[i][hd].y * __builtin_amdgcn_exp2f(stat[i][hd].x - mx);
-    a.stat[at + hd] = make_float2(mx, sum);
+    __syncthreads();  // (the next sequence writes stat and red again)
   }
 }
 
-// Maximum and sum of a query head over the splits of its sequence (every lane).
-__device__ __forceinline__ float2 join_stat(const Attend& a, const Run& run, int y, int hd) {
-  const int lane = threadIdx.x & 63;
-  const int64_t step = int64_t(a.c.kv) * a.gtiles * a.gmax;
-  const float2* st = a.stat + (int64_t(run.first) * a.c.kv * a.gtiles + y) * a.gmax + hd;
-  float m = kMinusInf, l = 0.0f;
-  for (int i = lane; i < run.count; i += 64) {
-    const float2 s = st[i * step];
-    const float top = fmaxf(m, s.x);
-    if (top != kMinusInf) {
-      l = l * (m == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(m - top)) +
-          (s.x == kMinusInf ? 0.0f : s.y * __builtin_amdgcn_exp2f(s.x - top));
-      m = top;
-    }
-  }
-  const float top = wave_max_f32(m);
-  l = m == kMinusInf ? 0.0f : l * __builtin_amdgcn_exp2f(m - top);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
-  return make_float2(top, l);
+// Two maxima with their sums, as one (a maximum of -infinity: nothing yet).
+__device__ __forceinline__ float factor_at(float m, float top) {
+  return m == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
 }
 
 constexpr int kWeightRows = 1024;  // rows of weight per workgroup
 
-// Blocks [0, batch * heads): the query heads' outputs, their splits joined;
-// then, for weight, [batch][kv][rows / kWeightRows].
+// Blocks [0, batch * heads): the query heads' outputs, the parts of their
+// sequence joined; then, for weight, [batch][kv][rows / kWeightRows].
 template <int DP, bool F16>
 __global__ __launch_bounds__(256) void attend_join_kernel(Attend a) {
+  constexpr int PER = DP / 64;
   __shared__ float red[4][DP];
+  __shared__ float2 st[4];
   __shared__ float2 lse[kMaxGroup];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int T = split_tiles(a);
   int blk = blockIdx.x;
+  const int64_t step = int64_t(a.c.kv) * a.gtiles * a.gmax;  // from part to part, in heads
   if (blk < a.c.batch * a.heads) {
     const int b = blk / a.heads, head = blk - b * a.heads;
     const int h = head / a.group, i = head - h * a.group;
-    const int y = h * a.gtiles + i / 16, hd = i % 16;
-    const Run run = splits_of(a, T, b);
-    const float2 st = join_stat(a, run, y, hd);
-    constexpr int PER = DP / 64;
-    float sum[PER];
+    const int hd = (h * a.gtiles + i / 16) * a.gmax + i % 16;
+    const int2 parts = as_global(a.parts)[b];  // (not set for an empty sequence)
+    const bool none = span_of(a, b).tiles() == 0;
+    if (!none && parts.y == 1) return;  // written already
+    float m = kMinusInf, l = 0.0f, sum[PER];
 #pragma unroll
     for (int j = 0; j < PER; ++j) sum[j] = 0.0f;
-    for (int w = wave; w < run.count; w += 4) {
-      const int64_t at = (int64_t(run.first + w) * a.c.kv * a.gtiles + y) * a.gmax + hd;
-      const float m = a.stat[at].x;
-      if (m == kMinusInf) continue;
-      const float f = __builtin_amdgcn_exp2f(m - st.x);
+    if (!none) {
+      constexpr int AT = 4;  // parts in flight per wave
+      for (int p0 = wave; p0 < parts.y; p0 += 4 * AT) {
+        float2 s[AT];
+        float v[AT][PER];
 #pragma unroll
-      for (int j = 0; j < PER; ++j) sum[j] += f * a.sums[at * DP + 64 * j + lane];
+        for (int u = 0; u < AT; ++u) {
+          const int p = p0 + 4 * u < parts.y ? p0 + 4 * u : p0;
+          const int64_t at = (parts.x + p) * step + hd;
+          s[u] = as_global(a.stat)[at];
+          if (p0 + 4 * u >= parts.y) s[u].x = kMinusInf;
+#pragma unroll
+          for (int j = 0; j < PER; ++j) v[u][j] = as_global(a.sums)[at * DP + 64 * j + lane];
+        }
+#pragma unroll
+        for (int u = 0; u < AT; ++u) {
+          if (s[u].x == kMinusInf) continue;
+          const float top = fmaxf(m, s[u].x), f0 = factor_at(m, top), f1 = factor_at(s[u].x, top);
+          l = l * f0 + s[u].y * f1;
+#pragma unroll
+          for (int j = 0; j < PER; ++j) sum[j] = sum[j] * f0 + v[u][j] * f1;
+          m = top;
+        }
+      }
     }
+    if (lane == 0) st[wave] = make_float2(m, l);
+    __syncthreads();
+    const float top = fmaxf(fmaxf(st[0].x, st[1].x), fmaxf(st[2].x, st[3].x));
+    const float f = factor_at(m, top);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) red[wave][64 * j + lane] = sum[j];
+    for (int j = 0; j < PER; ++j) red[wave][64 * j + lane] = m == kMinusInf ? 0.0f : sum[j] * f;
+    float total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) total += st[i].x == kMinusInf ? 0.0f : st[i].y * factor_at(st[i].x, top);
     __syncthreads();
     for (int d = threadIdx.x; d < a.c.dim; d += 256) {
       const float v = red[0][d] + red[1][d] + red[2][d] + red[3][d];
       store_from_f32(a.out, int64_t(b) * a.out_stride + int64_t(head) * a.c.dim + d, a.type,
-                     st.y == 0.0f ? 0.0f : v / st.y);
+                     total == 0.0f ? 0.0f : v / total);
     }
     return;
   }
@@ -699,37 +838,50 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a) {
   const int r0 = ch * kWeightRows > sp.begin ? ch * kWeightRows : sp.begin;
   const int r1 = (ch + 1) * kWeightRows < sp.end ? (ch + 1) * kWeightRows : sp.end;
   if (r0 >= r1) return;
-  const Run run = splits_of(a, T, b);
+  const int2 parts = as_global(a.parts)[b];
   constexpr float kUp = F16 ? 16384.0f : 1.0f;  // (f16: the sums are held times 2^14)
   for (int i = wave; i < a.group; i += 4) {
-    const float2 st = join_stat(a, run, h * a.gtiles + i / 16, i % 16);
+    const int hd = (h * a.gtiles + i / 16) * a.gmax + i % 16;
+    float m = kMinusInf, l = 0.0f;
+    for (int p = lane; p < parts.y; p += 64) {
+      const float2 s = as_global(a.stat)[(parts.x + p) * step + hd];
+      if (s.x == kMinusInf) continue;
+      const float top = fmaxf(m, s.x);
+      l = l * factor_at(m, top) + s.y * factor_at(s.x, top);
+      m = top;
+    }
+    const float top = wave_max_f32(m);
+    l = m == kMinusInf ? 0.0f : l * factor_at(m, top);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
     // a row's probability is 2^(x - max) / sum; nothing attended to: 0
-    if (lane == 0) lse[i] = st.y == 0.0f ? make_float2(0.0f, 0.0f) : make_float2(st.x, kUp / st.y);
+    if (lane == 0) lse[i] = l == 0.0f ? make_float2(0.0f, 0.0f) : make_float2(top, kUp / l);
   }
   __syncthreads();
   for (int r = r0 + threadIdx.x; r < r1; r += 256) {
     float p = 0.0f;
     for (int i = 0; i < a.group; ++i)
-      p += __builtin_amdgcn_exp2f(a.score[(int64_t(b) * a.heads + h * a.group + i) * a.score_stride + r] - lse[i].x) *
-           lse[i].y;
-    a.weight[(int64_t(b) * a.c.kv + h) * a.row_stride + r] += p;
+      p += __builtin_amdgcn_exp2f(as_global(a.score)[(int64_t(b) * a.heads + h * a.group + i) * a.score_stride + r] -
+                                  lse[i].x) * lse[i].y;
+    as_global_mut(a.weight)[(int64_t(b) * a.c.kv + h) * a.row_stride + r] += p;
   }
 }
 
-template <int CT, int NT, int DP, bool ANY>
+template <class G>
 int launch_cfg(const Attend& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(a.c.kv * a.gtiles), static_cast<unsigned>(a.splits));
-  const int rc = launch(attend_kernel<Cfg<CT, NT, DP, ANY>>, grid, dim3(64 * kWaves), 0, s, a);
+  const dim3 grid(static_cast<unsigned>(a.c.kv * a.gtiles), static_cast<unsigned>(a.columns));
+  const int rc = launch(attend_kernel<G>, grid, dim3(64 * kWaves), 0, s, a);
   if (rc != SHERRY_OK) return rc;
   int64_t blocks = int64_t(a.c.batch) * a.heads;
   if (a.weight) blocks += int64_t(a.c.batch) * a.c.kv * ceil_div(a.c.rows, kWeightRows);
-  return launch(attend_join_kernel<DP, CT == SHERRY_F16>, dim3(static_cast<unsigned>(blocks)),
-                dim3(256), 0, s, a);
+  return launch(attend_join_kernel<G::DP, G::F16>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
 }
 template <int CT, int NT, int DP>
 int launch_pages(const Attend& a, hipStream_t s) {
-  return a.c.page_size % 16 == 0 ? launch_cfg<CT, NT, DP, false>(a, s)
-                                 : launch_cfg<CT, NT, DP, true>(a, s);
+  const bool more = a.mask || a.position || a.weight;
+  if (a.c.page_size % 16 == 0)
+    return more ? launch_cfg<Cfg<CT, NT, DP, false, true>>(a, s) : launch_cfg<Cfg<CT, NT, DP, false, false>>(a, s);
+  return more ? launch_cfg<Cfg<CT, NT, DP, true, true>>(a, s) : launch_cfg<Cfg<CT, NT, DP, true, false>>(a, s);
 }
 template <int CT, int NT>
 int launch_dim(const Attend& a, hipStream_t s) {
@@ -740,26 +892,31 @@ int launch_dim(const Attend& a, hipStream_t s) {
 
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-// The split of a launch and the parts of its workspace.
+// The columns of a launch and the parts of its workspace.
 struct Shape {
-  int group, gtiles, gmax, target, splits;
+  int group, gtiles, gmax, columns;
   int64_t score_stride;
-  size_t stat_bytes, sum_bytes, score_bytes;
+  size_t parts_bytes, stat_bytes, sum_bytes, score_bytes;
+  size_t bytes() const { return parts_bytes + stat_bytes + sum_bytes + score_bytes; }
 };
 Shape shape_of(const sherry_cache_desc& c, const sherry_attend_desc& d) {
   Shape s{};
   s.group = d.heads / c.kv_heads;
   s.gtiles = static_cast<int>(ceil_div(s.group, 16));
   s.gmax = s.group < 16 ? s.group : 16;
+  const int dp = padded_dim(c.head_dim);
   const int64_t y = int64_t(c.kv_heads) * s.gtiles;
-  s.target = static_cast<int>(y >= kTargetGroups ? 1 : kTargetGroups / y);
-  const int64_t rows = int64_t(c.table_width) * c.page_size;
-  const int64_t most = int64_t(c.batch) * ceil_div(ceil_div(rows, kTile) + 1, kMinTiles);
-  s.splits = static_cast<int>(most < s.target + c.batch ? most : s.target + c.batch);
+  const int64_t rows = int64_t(c.table_width) * c.page_size, tiles = ceil_div(rows, kTile);
+  // as many workgroups as run at once, but no more than full sequences make
+  const int64_t groups = kCus * waves_for(dp), fit = y >= groups ? 1 : groups / y;
+  const int64_t most = ceil_div(c.batch * (tiles + kSequence), kMinTiles);
+  s.columns = static_cast<int>(most < fit ? most : fit);
   auto up = [](int64_t n) { return static_cast<size_t>((n + 255) / 256 * 256); };
-  s.stat_bytes = up(s.splits * y * s.gmax * 8);
-  s.sum_bytes = up(s.splits * y * s.gmax * padded_dim(c.head_dim) * 4);
-  s.score_stride = ceil_div(rows, kTile) * kTile;
+  const int64_t parts = int64_t(s.columns) + c.batch;
+  s.parts_bytes = up(int64_t(c.batch) * 8);
+  s.stat_bytes = up(parts * y * s.gmax * 8);
+  s.sum_bytes = up(parts * y * s.gmax * dp * 4);
+  s.score_stride = tiles * kTile;
   s.score_bytes = d.weight ? up(int64_t(c.batch) * d.heads * s.score_stride * 4) : 0;
   return s;
 }
@@ -767,25 +924,26 @@ Shape shape_of(const sherry_cache_desc& c, const sherry_attend_desc& d) {
 }  // namespace
 
 size_t attend_workspace(const sherry_cache_desc& c, const sherry_attend_desc& d) {
-  const Shape s = shape_of(c, d);
-  return s.stat_bytes + s.sum_bytes + s.score_bytes;
+  return shape_of(c, d).bytes();
 }
 
 int launch_attend(const sherry_cache_desc& c, const sherry_attend_desc& d, hipStream_t s) {
   const Shape sh = shape_of(c, d);
   char* ws = static_cast<char*>(d.workspace);
+  char* stat = ws + sh.parts_bytes;
+  char* sums = stat + sh.stat_bytes;
   const int64_t row = int64_t(d.heads) * c.head_dim;
   const Attend a{cache_of(c), d.q, d.out, d.length, d.mask, d.position, d.q_pos, d.weight,
-                 reinterpret_cast<float*>(ws + sh.stat_bytes), reinterpret_cast<float2*>(ws),
-                 reinterpret_cast<float*>(ws + sh.stat_bytes + sh.sum_bytes),
+                 reinterpret_cast<int2*>(ws), reinterpret_cast<float2*>(stat),
+                 reinterpret_cast<float*>(sums), reinterpret_cast<float*>(sums + sh.sum_bytes),
                  d.q_stride ? d.q_stride : row, d.out_stride ? d.out_stride : row, d.mask_stride,
                  d.row_stride, sh.score_stride, d.heads, sh.group, sh.gtiles, sh.gmax, d.type,
-                 d.window, sh.target, sh.splits, d.scale};
+                 d.window, sh.columns, d.scale};
   const bool f32 = d.type == SHERRY_F32;
   switch (c.type) {
     case SHERRY_F16: return launch_dim<SHERRY_F16, 2>(a, s);
     case SHERRY_BF16: return f32 ? launch_dim<SHERRY_BF16, 3>(a, s) : launch_dim<SHERRY_BF16, 2>(a, s);
-    default: return f32 ? launch_dim<SHERRY_I8, 3>(a, s) : launch_dim<SHERRY_I8, 2>(a, s);
+    default: return launch_dim<SHERRY_I8, 2>(a, s);
   }
 }
 

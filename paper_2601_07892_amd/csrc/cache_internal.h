@@ -18,8 +18,10 @@ struct FastDiv {
     return f;
   }
   __device__ __forceinline__ uint32_t div(uint32_t n) const {
-    return d <= 1 ? n : __umulhi(n, mul) >> shift;
+    return d <= 1 ? n : quotient(n);
   }
+  // d >= 2
+  __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return __umulhi(n, mul) >> shift; }
 };
 
 // A sherry_cache_desc as the kernels take it.
