@@ -50,6 +50,9 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;
 constexpr int kMinTiles = kWaves;  // tiles of the shortest run: one per wave
+// Up to this many tiles of capacity a workgroup takes a sequence whole, and
+// nothing is left to join: WHOLEUS
+constexpr int kWholeTiles = 16;
 constexpr int kCus = 256;
 constexpr int kTile = 32;          // rows per wave and step
 constexpr int kMaxGroup = 256;       // query heads per key-value head
@@ -73,6 +76,7 @@ struct Attend {
   float* score;  // [batch][heads][score_stride], in units of ln 2 (weight only)
   int64_t q_stride, out_stride, mask_stride, row_stride, score_stride;
   int heads, group, gtiles, gmax, type, window, columns;
+  bool whole;    // column w is sequence w
   float scale;
 };
 
@@ -91,9 +95,14 @@ __device__ __forceinline__ Span span_of(const Attend& a, int b) {
   return Span{last && n > a.window ? n - a.window : 0, n};
 }
 
-__device__ __forceinline__ int wave_sum(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+// Inclusive sums over the lanes (steps inside 16 lanes, then across them).
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);  // from 1, 2, 4, 8 lanes below
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, true);  // lane 15 of the row below
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, true);  // lane 31
   return v;
 }
 
@@ -111,31 +120,26 @@ struct Place {
 };
 __device__ __forceinline__ Place find_place(const Attend& a, int w) {
   const int lane = threadIdx.x & 63;
-  const int n0 = lane < a.c.batch ? cost_of(span_of(a, lane).tiles()) : 0;
-  int total = n0;
-  for (int b = 64 + lane; b < a.c.batch; b += 64) total += cost_of(span_of(a, b).tiles());
-  total = wave_sum(total);
+  auto cost = [&](int b) { return b < a.c.batch ? cost_of(span_of(a, b).tiles()) : 0; };
+  const int n0 = cost(lane), upto0 = wave_scan(n0);
+  int total = __builtin_amdgcn_readlane(upto0, 63);
+  for (int b = 64; b < a.c.batch; b += 64)
+    total += __builtin_amdgcn_readlane(wave_scan(cost(b + lane)), 63);
   int run = (total + a.columns - 1) / a.columns;
   run = run < kMinTiles ? kMinTiles : run;
   const int64_t start = int64_t(w) * run;
   if (start >= total) return Place{-1, 0, run};
   int before = 0;
   for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
-    const int n = b0 == 0 ? n0 : b0 + lane < a.c.batch ? cost_of(span_of(a, b0 + lane).tiles()) : 0;
-    int upto = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += v;
-    }
+    const int n = b0 == 0 ? n0 : cost(b0 + lane);
+    const int upto = b0 == 0 ? upto0 : wave_scan(n);
     const uint64_t past = __ballot(before + upto > start);
     if (past) {
       const int at = __builtin_ctzll(past);
-      const int first = before + __shfl(upto - n, at, 64);
-      return Place{__builtin_amdgcn_readfirstlane(b0 + at),
-                   __builtin_amdgcn_readfirstlane(static_cast<int>(start) - first), run};
+      const int first = before + __builtin_amdgcn_readlane(upto - n, at);
+      return Place{b0 + at, static_cast<int>(start) - first, run};
     }
-    before += __shfl(upto, 63, 64);
+    before += __builtin_amdgcn_readlane(upto, 63);
   }
   return Place{-1, 0, run};
 }
@@ -482,37 +486,50 @@ __device__ __forceinline__ void for_each(F&& f, std::integer_sequence<int, is...
   (f(std::integral_constant<int, is>{}), ...);
 }
 
-// q of one sequence in terms, and the factor of its scores in units of ln 2.
+// This lane's values of a sequence's q as they lie (fp32, or pairs of 16 bits).
 template <class G>
-__device__ __forceinline__ float load_q(const Attend& a, int b, int head0, int heads,
-                                        u32x4 (&qf)[G::NT][G::KS]) {
+__device__ __forceinline__ void load_q(const Attend& a, int b, int head0, int heads,
+                                       u32x4 (&q)[G::KS][2]) {
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  float factor = a.scale * kLog2e;
-  float q[G::KS][8];
   const bool mine = n < heads;
   const int64_t at = int64_t(b) * a.q_stride + int64_t(head0 + (mine ? n : 0)) * a.c.dim;
-  float top = 0.0f;
 #pragma unroll
   for (int s = 0; s < G::KS; ++s) {
     const int d = k_dim<G>(s, g);
     const bool in = mine && d < a.c.dim;
+    const u32x4 zero = {0, 0, 0, 0};
     if (a.type == SHERRY_F32) {
-      const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + d);
-      const float4 lo = in ? p[0] : make_float4(0, 0, 0, 0), hi = in ? p[1] : make_float4(0, 0, 0, 0);
-      q[s][0] = lo.x, q[s][1] = lo.y, q[s][2] = lo.z, q[s][3] = lo.w;
-      q[s][4] = hi.x, q[s][5] = hi.y, q[s][6] = hi.z, q[s][7] = hi.w;
+      const SHERRY_GLOBAL u32x4* p =
+          reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(static_cast<const float*>(a.q)) + at + d);
+      q[s][0] = in ? p[0] : zero;
+      q[s][1] = in ? p[1] : zero;
     } else {
-      const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) + at + d);
-      const u32x4 v = in ? *p : u32x4{0, 0, 0, 0};
+      const SHERRY_GLOBAL u32x4* p =
+          reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(static_cast<const uint16_t*>(a.q)) + at + d);
+      q[s][0] = in ? *p : zero;
+      q[s][1] = zero;
+    }
+  }
+}
+// The same in terms, and the factor of its scores in units of ln 2.
+template <class G>
+__device__ __forceinline__ float split_q(const Attend& a, const u32x4 (&raw)[G::KS][2],
+                                         u32x4 (&qf)[G::NT][G::KS]) {
+  float factor = a.scale * kLog2e;
+  float q[G::KS][8];
+  float top = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint16_t x = static_cast<uint16_t>(v[i >> 1] >> (16 * (i & 1)));
+  for (int s = 0; s < G::KS; ++s)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (a.type == SHERRY_F32) {
+        q[s][i] = __uint_as_float(raw[s][i >> 2][i & 3]);
+      } else {
+        const uint16_t x = static_cast<uint16_t>(raw[s][0][i >> 1] >> (16 * (i & 1)));
         q[s][i] = a.type == SHERRY_BF16 ? from_bf16(x) : from_f16(x);
       }
+      top = fmaxf(top, fabsf(q[s][i]));
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(q[s][i]));
-  }
   if constexpr (G::F16) {
     // q / 2^e in [-2, 2): exact, and far from f16's limits
     top = max_over_blocks(top);
@@ -545,7 +562,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // (uniform values, which the compiler does not see through the wave's sums)
-  const Place place = find_place(a, blockIdx.y);
+  const Place place = a.whole ? Place{static_cast<int>(blockIdx.y), 0, 1 << 30} : find_place(a, blockIdx.y);
   const int b_first = __builtin_amdgcn_readfirstlane(place.b);
   if (b_first < 0) return;
   const int h = blockIdx.x / a.gtiles, gt = blockIdx.x - h * a.gtiles;
@@ -554,21 +571,26 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
   const int run = __builtin_amdgcn_readfirstlane(place.run);
   // of the run, and of b's cost before it
   int left = run, at_cost = __builtin_amdgcn_readfirstlane(place.at);
-  for (int b = b_first; left > 0 && b < a.c.batch;
-       b = __builtin_amdgcn_readfirstlane(next_sequence(a, b + 1)), at_cost = 0) {
+  for (int b = b_first; b < a.c.batch;) {
     const Span sp = span_of(a, b);
     const int begin = __builtin_amdgcn_readfirstlane(sp.begin);
     const int end = __builtin_amdgcn_readfirstlane(sp.end);
     const int tiles = __builtin_amdgcn_readfirstlane(sp.tiles());
     // units [at_cost, upto) of the sequence's cost: the tiles among them
     const int upto = tiles + kSequence < at_cost + left ? tiles + kSequence : at_cost + left;
-    left -= upto - at_cost;
+    left = a.whole ? 0 : left - (upto - at_cost);
     const int n0 = at_cost > kSequence ? at_cost - kSequence : 0, n1 = upto - kSequence;
-    if (n1 <= n0) continue;  // (the next column takes the first tiles)
+    if (n1 <= n0) {  // the run ends before the first tile; or there are none
+      if (a.whole)
+        for (int i = threadIdx.x; i < heads * a.c.dim; i += 64 * kWaves)
+          store_from_f32(a.out, int64_t(b) * a.out_stride + int64_t(head0) * a.c.dim + i, a.type, 0.0f);
+      return;
+    }
     const int t0 = begin / kTile + n0, t1 = begin / kTile + n1;
 
-    u32x4 qf[NT][G::KS];
-    const float factor = load_q<G>(a, b, head0, heads, qf);
+    // q first, then the first tile's rows, so that their latencies overlap
+    u32x4 qraw[G::KS][2], qf[NT][G::KS];
+    load_q<G>(a, b, head0, heads, qraw);
     Rows<G> rows(a, b, h, begin, end);
     float* score = nullptr;  // of this lane's head, and its rows of a tile
     if (G::MORE && a.weight)
@@ -593,6 +615,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
       if constexpr (G::I8) rows.load_scales(a.c.vs, vsc);
       if (tile + kWaves < t1) rows.start(tile + kWaves);
     }
+    const float factor = split_q<G>(a, qraw, qf);
     for (; tile < t1; tile += kWaves) {
       const uint32_t valid = rows.valid;
       const bool holes = !G::I8 && !G::ANY && rows.holes();
@@ -750,12 +773,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
         as_global_mut(a.sums)[(at + hd) * DP + d] = v;
       }
     }
+    if (a.whole) return;
     if (threadIdx.x < heads) as_global_mut(a.stat)[at + threadIdx.x] = sum_of(threadIdx.x);
     if (n0 == 0 && blockIdx.x == 0 && threadIdx.x == 0) {
       // the rest of the sequence is in whole runs and a last one
       const int more = tiles - n1;
       as_global_mut(a.parts)[b] = make_int2(static_cast<int>(blockIdx.y) + b, 1 + (more + run - 1) / run);
     }
+    if (left <= 0) return;
+    b = __builtin_amdgcn_readfirstlane(next_sequence(a, b + 1));
+    at_cost = 0;
     __syncthreads();  // (the next sequence writes stat and red again)
   }
 }
@@ -857,21 +884,37 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a) {
     // a row's probability is 2^(x - max) / sum; nothing attended to: 0
     if (lane == 0) lse[i] = l == 0.0f ? make_float2(0.0f, 0.0f) : make_float2(top, kUp / l);
   }
-  __syncthreads();
-  for (int r = r0 + threadIdx.x; r < r1; r += 256) {
-    float p = 0.0f;
-    for (int i = 0; i < a.group; ++i)
-      p += __builtin_amdgcn_exp2f(as_global(a.score)[(int64_t(b) * a.heads + h * a.group + i) * a.score_stride + r] -
-                                  lse[i].x) * lse[i].y;
-    as_global_mut(a.weight)[(int64_t(b) * a.c.kv + h) * a.row_stride + r] += p;
+  // four rows per thread at once
+  constexpr int AT = kWeightRows / 256;
+  float* to = a.weight + (int64_t(b) * a.c.kv + h) * a.row_stride;
+  const float* from = a.score + (int64_t(b) * a.heads + h * a.group) * a.score_stride;
+  float p[AT], w[AT];
+  int r[AT];
+#pragma unroll
+  for (int j = 0; j < AT; ++j) {
+    r[j] = ch * kWeightRows + 256 * j + threadIdx.x;
+    const bool in = r[j] >= r0 && r[j] < r1;
+    if (!in) r[j] = r0;
+    w[j] = as_global(to)[r[j]];
+    p[j] = 0.0f;
+    if (!in) r[j] = -1;
   }
+  __syncthreads();  // lse
+#pragma unroll 4
+  for (int i = 0; i < a.group; ++i)
+#pragma unroll
+    for (int j = 0; j < AT; ++j)
+      p[j] += __builtin_amdgcn_exp2f(as_global(from)[i * a.score_stride + (r[j] < 0 ? r0 : r[j])] - lse[i].x) * lse[i].y;
+#pragma unroll
+  for (int j = 0; j < AT; ++j)
+    if (r[j] >= 0) as_global_mut(to)[r[j]] = w[j] + p[j];
 }
 
 template <class G>
 int launch_cfg(const Attend& a, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(a.c.kv * a.gtiles), static_cast<unsigned>(a.columns));
   const int rc = launch(attend_kernel<G>, grid, dim3(64 * kWaves), 0, s, a);
-  if (rc != SHERRY_OK) return rc;
+  if (rc != SHERRY_OK || a.whole) return rc;
   int64_t blocks = int64_t(a.c.batch) * a.heads;
   if (a.weight) blocks += int64_t(a.c.batch) * a.c.kv * ceil_div(a.c.rows, kWeightRows);
   return launch(attend_join_kernel<G::DP, G::F16>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
@@ -895,6 +938,7 @@ int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // The columns of a launch and the parts of its workspace.
 struct Shape {
   int group, gtiles, gmax, columns;
+  bool whole;
   int64_t score_stride;
   size_t parts_bytes, stat_bytes, sum_bytes, score_bytes;
   size_t bytes() const { return parts_bytes + stat_bytes + sum_bytes + score_bytes; }
@@ -910,7 +954,8 @@ Shape shape_of(const sherry_cache_desc& c, const sherry_attend_desc& d) {
   // as many workgroups as run at once, but no more than full sequences make
   const int64_t groups = kCus * waves_for(dp), fit = y >= groups ? 1 : groups / y;
   const int64_t most = ceil_div(c.batch * (tiles + kSequence), kMinTiles);
-  s.columns = static_cast<int>(most < fit ? most : fit);
+  s.whole = !d.weight && tiles <= kWholeTiles;
+  s.columns = s.whole ? c.batch : static_cast<int>(most < fit ? most : fit);
   auto up = [](int64_t n) { return static_cast<size_t>((n + 255) / 256 * 256); };
   const int64_t parts = int64_t(s.columns) + c.batch;
   s.parts_bytes = up(int64_t(c.batch) * 8);
@@ -938,7 +983,7 @@ int launch_attend(const sherry_cache_desc& c, const sherry_attend_desc& d, hipSt
                  reinterpret_cast<float*>(sums), reinterpret_cast<float*>(sums + sh.sum_bytes),
                  d.q_stride ? d.q_stride : row, d.out_stride ? d.out_stride : row, d.mask_stride,
                  d.row_stride, sh.score_stride, d.heads, sh.group, sh.gtiles, sh.gmax, d.type,
-                 d.window, sh.columns, d.scale};
+                 d.window, sh.columns, sh.whole, d.scale};
   const bool f32 = d.type == SHERRY_F32;
   switch (c.type) {
     case SHERRY_F16: return launch_dim<SHERRY_F16, 2>(a, s);
