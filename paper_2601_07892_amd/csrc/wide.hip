@@ -233,11 +233,25 @@ struct WdExtra<Epi, PN> {
         residual[i] = four(e.residual + int64_t(tok) * e.residual_ld + row, in, whole);
     }
   }
-  __device__ __forceinline__ float4 apply(const Epi& e, float4 v, int i) const {
-    const EpiValues a{bias.x, gate[i].x, residual[i].x}, b{bias.y, gate[i].y, residual[i].y},
-        c{bias.z, gate[i].z, residual[i].z}, d{bias.w, gate[i].w, residual[i].w};
-    return make_float4(epi_apply(e, v.x, a), epi_apply(e, v.y, b), epi_apply(e, v.z, c),
-                       epi_apply(e, v.w, d));
+  // (one step after the other over all pieces: each activation's code stands once)
+  __device__ __forceinline__ void apply(const Epi& e, float (&v)[4 * PN]) const {
+    if (e.bias) {
+#pragma unroll
+      for (int i = 0; i < PN; ++i)
+        v[4 * i] += bias.x, v[4 * i + 1] += bias.y, v[4 * i + 2] += bias.z, v[4 * i + 3] += bias.w;
+    }
+    activate_all(v, e.act);
+    if (e.gate) {
+#pragma unroll
+      for (int i = 0; i < PN; ++i)
+        v[4 * i] *= gate[i].x, v[4 * i + 1] *= gate[i].y, v[4 * i + 2] *= gate[i].z, v[4 * i + 3] *= gate[i].w;
+    }
+    if (e.residual) {
+#pragma unroll
+      for (int i = 0; i < PN; ++i)
+        v[4 * i] += residual[i].x, v[4 * i + 1] += residual[i].y, v[4 * i + 2] += residual[i].z,
+            v[4 * i + 3] += residual[i].w;
+    }
   }
 };
 
@@ -583,6 +597,27 @@ __device__ __forceinline__ void wd_block(const WdProblem& p, int g, int8_t* lds,
     __asm__ volatile("" ::: "memory");
     if (b + 1 < NB) put(b + 1);
     const int row = r * kTileRows + 32 * (hs + h) + 4 * c4;
+    if constexpr (E::kUse) {
+      float o[4 * PN];
+#pragma unroll
+      for (int i = 0; i < PN; ++i)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) o[4 * i + u] = out(v[i][u], sx[i], swl[h][u]);
+      extra[b & 1].apply(epi, o);
+      float* yp = as_global_mut(p.y) + int64_t(32 * tb + tokb + (lane >> 3)) * p.n + row;
+#pragma unroll
+      for (int i = 0; i < PN; ++i, yp += int64_t(8) * p.n) {
+        if (whole) {
+          *reinterpret_cast<float4*>(yp) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+          continue;
+        }
+        const int tok = 32 * tb + tokb + (lane >> 3) + 8 * i;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (tok < p.m && row + u < p.n) yp[u] = o[4 * i + u];
+      }
+      continue;
+    }
     if (whole) {
       const int64_t at = int64_t(32 * tb + tokb + (lane >> 3)) * p.n + row;
       float* yp = as_global_mut(p.y) + at;
@@ -594,7 +629,6 @@ __device__ __forceinline__ void wd_block(const WdProblem& p, int g, int8_t* lds,
         o4.y = out(v[i].y, sx[i], swl[h][1]);
         o4.z = out(v[i].z, sx[i], swl[h][2]);
         o4.w = out(v[i].w, sx[i], swl[h][3]);
-        if constexpr (E::kUse) o4 = extra[b & 1].apply(epi, o4, i);
         *reinterpret_cast<float4*>(yp + int64_t(8 * i) * p.n) = o4;
         if (acc_out) *reinterpret_cast<v4i*>(ap + int64_t(8 * i) * p.n) = v[i];
       }
@@ -607,10 +641,6 @@ __device__ __forceinline__ void wd_block(const WdProblem& p, int g, int8_t* lds,
         float o4[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) o4[u] = out(vv[u], sx[i], swl[h][u]);
-        if constexpr (E::kUse) {
-          const float4 t = extra[b & 1].apply(epi, make_float4(o4[0], o4[1], o4[2], o4[3]), i);
-          o4[0] = t.x, o4[1] = t.y, o4[2] = t.z, o4[3] = t.w;
-        }
         float* yrow = as_global_mut(p.y) + int64_t(tok) * p.n + row;
         if (vec) {
           *reinterpret_cast<float4*>(yrow) = make_float4(o4[0], o4[1], o4[2], o4[3]);
