@@ -680,6 +680,12 @@ __global__ __launch_bounds__(G::THREADS) __attribute__((amdgpu_waves_per_eu(G::E
     tb = b / groups;
     g = b - tb * groups;
   }
+  if constexpr (E::kUse) {
+    // (their many vector uses would otherwise keep them in vector registers, and
+    // every load of the stream in a loop over its lanes)
+    g = __builtin_amdgcn_readfirstlane(g);
+    tb = __builtin_amdgcn_readfirstlane(tb);
+  }
   wd_tokens<G>(p, int64_t(tb) * G::TOK);
   wd_block<G>(p, g, lds, epi.from(int64_t(tb) * G::TOK));
 }
