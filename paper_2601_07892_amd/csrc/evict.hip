@@ -66,10 +66,70 @@ __device__ __forceinline__ int waves_before(int v, int* part, int& total) {
   return before;
 }
 
+// Each wave takes a run of slots, 64 at a time, and keeps their keys: J per
+// lane, for sequences of up to 1024 J rows; J = 0 reads them again in every pass.
+template <int J>
+struct Run {
+  const Keys& keys;
+  int first, end;  // of this wave
+  uint32_t key[J > 0 ? J : 1];
+
+  __device__ __forceinline__ Run(const Keys& k, int n) : keys(k) {
+    const int seg = J > 0 ? 64 * J : ((n + kWaves - 1) / kWaves + 63) / 64 * 64;
+    // (short sequences are spread over the waves too)
+    const int even = ((n + kWaves - 1) / kWaves + 63) / 64 * 64;
+    const int use = even < seg ? even : seg;
+    first = static_cast<int>(threadIdx.x >> 6) * use;
+    end = first + use < n ? first + use : n;
+    if constexpr (J > 0) {
+      // (every load goes out, so that none waits for another's branch)
+      float w[J];
+      int32_t p[J];
+      const int last = n - 1;
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int i = first + 64 * j + static_cast<int>(threadIdx.x & 63);
+        w[j] = as_global(keys.w)[i < last ? i : last];
+      }
+      if (keys.recent && keys.pos) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const int i = first + 64 * j + static_cast<int>(threadIdx.x & 63);
+          p[j] = as_global(keys.pos)[i < last ? i : last];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int i = first + 64 * j + static_cast<int>(threadIdx.x & 63);
+        const bool recent = keys.recent && (keys.pos ? p[j] : i) >= keys.from;
+        key[j] = recent ? 0xFFFFFFFFu : weight_key(w[j]);
+      }
+    }
+  }
+  // f(j, slot, whether it is of the run, its key): in order; every lane calls it.
+  template <class F>
+  __device__ __forceinline__ void each(F&& f) const {
+    const int lane = threadIdx.x & 63;
+    if constexpr (J > 0) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        if (first + 64 * j >= end) break;
+        f(j, first + 64 * j + lane, first + 64 * j + lane < end, key[j]);
+      }
+    } else {
+      for (int i = first; i < end; i += 64) {
+        const bool in = i + lane < end;
+        f(0, i + lane, in, in ? keys.at(i + lane) : 0u);
+      }
+    }
+  }
+};
+
+template <int J>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
   __shared__ uint32_t hist[2048];
   __shared__ int part[kWaves];
-  __shared__ uint32_t found[2];
+  __shared__ uint32_t found[3];
   __shared__ int list[kList];
   const int b = blockIdx.x / a.c.kv, h = blockIdx.x - b * a.c.kv;
   const int n = a.c.length(a.length, b);
@@ -77,7 +137,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
   const int64_t row = int64_t(blockIdx.x) * a.row_stride, orow = int64_t(blockIdx.x) * a.out_stride;
   const float* w = a.weight + row;
   const int32_t* pos = a.position ? a.position + row : nullptr;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
   if (h == 0 && tid == 0) as_global_mut(a.length_out)[b] = m;
   auto put = [&](int i, int src) {
     as_global_mut(a.kept)[orow + i] = src;
@@ -94,22 +154,25 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
     return;
   }
   const Keys keys{w, pos, a.recent_from ? as_global(a.recent_from)[b] : 0, a.recent_from != nullptr};
+  const Run<J> run(keys, n);
 
   // the m-th largest key, 11, 11 and 10 bits at a time: of the keys with the
-  // bits found so far, `want` are to be taken
+  // bits found so far, `want` are to be taken.  Where that is all of them, the
+  // bits that follow decide nothing.
   uint32_t prefix = 0;
   int want = m, shift = 32;
 #pragma unroll
   for (int r = 0; r < 3; ++r) {
     const int bits = r < 2 ? 11 : 10;
+    const int above = shift;
     shift -= bits;
     hist[tid] = 0;
     hist[tid + 1024] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += kThreads) {
-      const uint32_t k = keys.at(i);
-      if (r == 0 || (k >> (shift + bits)) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1)], 1u);
-    }
+    run.each([&](int, int, bool in, uint32_t k) {
+      if (in && (r == 0 || (k >> (above & 31)) == prefix))
+        atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1)], 1u);
+    });
     __syncthreads();
     // thread t: bins 2047 - 2 t and 2046 - 2 t, from the largest down
     const int c0 = hist[2047 - 2 * tid], c1 = hist[2046 - 2 * tid];
@@ -121,41 +184,37 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
     }
     int total;
     const int before = waves_before(__shfl(upto, 63, 64), part, total) + upto - c0 - c1;
-    if (before < want && before + c0 >= want) {
-      found[0] = 2047 - 2 * tid;
-      found[1] = want - before;
-    } else if (before + c0 < want && before + c0 + c1 >= want) {
-      found[0] = 2046 - 2 * tid;
-      found[1] = want - before - c0;
+    const bool first = before < want && before + c0 >= want;
+    if (first || (before + c0 < want && before + c0 + c1 >= want)) {
+      found[0] = first ? 2047 - 2 * tid : 2046 - 2 * tid;
+      found[1] = first ? want - before : want - before - c0;
+      found[2] = first ? c0 : c1;
     }
     __syncthreads();
     prefix = prefix << bits | found[0];
     want = found[1];
+    if (found[2] == static_cast<uint32_t>(want)) break;
   }
-  // kept: every key above prefix, and the first `want` that equal it.  Each
-  // wave takes a run of slots, 64 at a time.
-  const int seg = ((n + kWaves - 1) / kWaves + 63) / 64 * 64;
-  const int s0 = wave * seg, s1 = s0 + seg < n ? s0 + seg : n;
+  // kept: every key above prefix (in its bits), and the first `want` that
+  // equal it
   const uint64_t below = (1ull << lane) - 1;
   int equal = 0;
-  for (int i = s0; i < s1; i += 64)
-    equal += __popcll(__ballot(i + lane < s1 && keys.at(i + lane) == prefix));
+  run.each([&](int, int, bool in, uint32_t k) { equal += __popcll(__ballot(in && (k >> shift) == prefix)); });
   int total;
   const int equal0 = waves_before(equal, part, total);
   // holes (slots below m given up) and movers (kept slots past it)
   auto scan = [&](auto&& each) {
     int eq = equal0;
-    for (int i = s0; i < s1; i += 64) {
-      const bool in = i + lane < s1;
-      const uint32_t k = in ? keys.at(i + lane) : 0;
-      const uint64_t e = __ballot(in && k == prefix);
-      const bool keep = in && (k > prefix || (k == prefix && eq + __popcll(e & below) < want));
+    run.each([&](int j, int i, bool in, uint32_t k) {
+      const uint32_t top = k >> shift;
+      const uint64_t e = __ballot(in && top == prefix);
+      const bool keep = in && (top > prefix || (top == prefix && eq + __popcll(e & below) < want));
       eq += __popcll(e);
-      each(i + lane, in && !keep && i + lane < m, keep && i + lane >= m, keep && i + lane < m);
-    }
+      each(j, i, in && !keep && i < m, keep && i >= m, keep && i < m);
+    });
   };
   int holes = 0, movers = 0;
-  scan([&](int, bool hole, bool mover, bool) {
+  scan([&](int, int, bool hole, bool mover, bool) {
     holes += __popcll(__ballot(hole));
     movers += __popcll(__ballot(mover));
   });
@@ -165,7 +224,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
   for (int base = 0; base == 0 || base < moves; base += kList) {
     __syncthreads();
     int rank = mover0 - base;
-    scan([&](int i, bool, bool mover, bool) {
+    scan([&](int, int i, bool, bool mover, bool) {
       const uint64_t who = __ballot(mover);
       const int at = rank + __popcll(who & below);
       if (mover && at >= 0 && at < kList) list[at] = i;
@@ -173,51 +232,116 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
     });
     __syncthreads();
     rank = hole0 - base;
-    scan([&](int i, bool hole, bool, bool stays) {
+    scan([&](int, int i, bool hole, bool, bool stays) {
       const uint64_t who = __ballot(hole);
       const int at = rank + __popcll(who & below);
-      if (hole && at >= 0 && at < kList) put(i, list[at]);
-      if (stays && base == 0) put(i, i);
+      int src = -1;
+      if (hole && at >= 0 && at < kList) src = list[at];
+      if (stays && base == 0) src = i;
+      if (src >= 0) as_global_mut(a.kept)[orow + i] = src;
       rank += __popcll(who);
     });
   }
-}
-
-constexpr int kMoveRows = 64;  // new rows per workgroup
-
-// LPR lanes of 16 bytes per row (8-byte rows of 8 int8 values do not exist:
-// head_dim is a multiple of 8, of 16 in int8).
-__global__ __launch_bounds__(256) void evict_move_kernel(Evict a, int lpr) {
-  const int chunks = (a.keep + kMoveRows - 1) / kMoveRows;
-  const int ch = blockIdx.x % chunks, bh = blockIdx.x / chunks;
-  const int b = bh / a.c.kv, h = bh - b * a.c.kv;
-  const int n = a.c.length(a.length, b);
-  if (n <= a.keep) return;
-  const int end = (ch + 1) * kMoveRows < a.keep ? (ch + 1) * kMoveRows : a.keep;
-  const int piece = threadIdx.x % lpr;
-  for (int i = ch * kMoveRows + threadIdx.x / lpr; i < end; i += 256 / lpr) {
-    const int src = as_global(a.kept)[int64_t(bh) * a.out_stride + i];
-    if (src == i) continue;
-    const int it = a.c.by_page.div(i), st = a.c.by_page.div(src);
-    const int ip = as_global(a.c.table)[int64_t(b) * a.c.width + it];
-    const int sp = as_global(a.c.table)[int64_t(b) * a.c.width + st];
-    if (ip < 0 || ip >= a.c.pages || sp < 0 || sp >= a.c.pages) continue;
-    const int io = i - it * a.c.page_size, so = src - st * a.c.page_size;
-    const int64_t e = a.bytes / a.c.dim;
-    const int64_t to = (a.c.at(ip, h) + int64_t(io) * a.c.dim) * e;
-    const int64_t from = (a.c.at(sp, h) + int64_t(so) * a.c.dim) * e;
-    for (int p = 16 * piece; p < a.bytes; p += 16 * lpr) {
-      const u32x4 x = *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(a.c.k) + from + p);
-      const u32x4 y = *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(a.c.v) + from + p);
-      *reinterpret_cast<SHERRY_GLOBAL u32x4*>(as_global_mut(a.c.k) + to + p) = x;
-      *reinterpret_cast<SHERRY_GLOBAL u32x4*>(as_global_mut(a.c.v) + to + p) = y;
+  if (!a.weight_out && !a.position_out) return;
+  // the kept rows' weights and positions, eight a thread at once
+  __syncthreads();
+  constexpr int AT = 8;
+  for (int i0 = tid; i0 < m; i0 += AT * kThreads) {
+    int src[AT];
+    float x[AT];
+    int32_t p[AT];
+#pragma unroll
+    for (int u = 0; u < AT; ++u) {
+      const int i = i0 + u * kThreads;
+      src[u] = as_global(a.kept)[orow + (i < m ? i : i0)];
     }
-    if (a.c.ks && piece == 0) {
-      const int64_t t = a.c.scale_at(ip, h) + io, f = a.c.scale_at(sp, h) + so;
-      as_global_mut(a.c.ks)[t] = as_global(a.c.ks)[f];
-      as_global_mut(a.c.vs)[t] = as_global(a.c.vs)[f];
+#pragma unroll
+    for (int u = 0; u < AT; ++u) {
+      x[u] = as_global(w)[src[u]];
+      p[u] = pos ? as_global(pos)[src[u]] : src[u];
+    }
+#pragma unroll
+    for (int u = 0; u < AT; ++u) {
+      const int i = i0 + u * kThreads;
+      if (i >= m) break;
+      if (a.weight_out) as_global_mut(a.weight_out)[orow + i] = x[u];
+      if (a.position_out) as_global_mut(a.position_out)[orow + i] = p[u];
     }
   }
+}
+
+constexpr int kMoveAt = 4;  // rows in flight per thread
+
+// LPR lanes of 16 bytes per row (rows of 8 bytes do not exist: head_dim is a
+// multiple of 8, of 16 in int8), 256 / LPR * kMoveAt new rows per workgroup.
+template <int LPR>
+__global__ __launch_bounds__(256) void evict_move_kernel(Evict a) {
+  constexpr int ROWS = 256 / LPR, PER = ROWS * kMoveAt;
+  const int chunks = (a.keep + PER - 1) / PER;
+  const int bh = blockIdx.x / chunks, ch = blockIdx.x - bh * chunks;
+  const int b = bh / a.c.kv, h = bh - b * a.c.kv;
+  const int n = a.c.length(a.length, b);
+  const int p = 16 * (threadIdx.x % LPR), i0 = ch * PER + threadIdx.x / LPR;
+  const int e = a.bytes / a.c.dim;
+  const int64_t trow = int64_t(b) * a.c.width;
+  int src[kMoveAt];
+#pragma unroll
+  for (int u = 0; u < kMoveAt; ++u) {
+    const int i = i0 + u * ROWS;
+    src[u] = i < a.keep ? as_global(a.kept)[int64_t(bh) * a.out_stride + i] : i;
+  }
+  if (n <= a.keep) return;
+  bool live[kMoveAt];
+  int64_t to[kMoveAt], from[kMoveAt];  // elements
+  u32x4 x[kMoveAt], y[kMoveAt];
+  float sx[kMoveAt], sy[kMoveAt];
+  int64_t sto[kMoveAt], sfrom[kMoveAt];
+#pragma unroll
+  for (int u = 0; u < kMoveAt; ++u) {
+    const int i = i0 + u * ROWS;
+    live[u] = src[u] != i;
+    const int at = live[u] ? i : 0, was = live[u] ? src[u] : 0;
+    const int it = a.c.by_page.div(at), st = a.c.by_page.div(was);
+    int ip = as_global(a.c.table)[trow + it], sp = as_global(a.c.table)[trow + st];
+    live[u] = live[u] && ip >= 0 && ip < a.c.pages && sp >= 0 && sp < a.c.pages;
+    if (!live[u]) ip = sp = 0;
+    const int io = at - it * a.c.page_size, so = was - st * a.c.page_size;
+    to[u] = a.c.at(ip, h) + int64_t(io) * a.c.dim;
+    from[u] = a.c.at(sp, h) + int64_t(so) * a.c.dim;
+    sto[u] = a.c.scale_at(ip, h) + io;
+    sfrom[u] = a.c.scale_at(sp, h) + so;
+  }
+  const bool in = p < a.bytes, scale = a.c.ks && p == 0;
+#pragma unroll
+  for (int u = 0; u < kMoveAt; ++u) {
+    if (!live[u]) continue;
+    if (in) {
+      x[u] = *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(a.c.k) + from[u] * e + p);
+      y[u] = *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(a.c.v) + from[u] * e + p);
+    }
+    if (scale) {
+      sx[u] = as_global(a.c.ks)[sfrom[u]];
+      sy[u] = as_global(a.c.vs)[sfrom[u]];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kMoveAt; ++u) {
+    if (!live[u]) continue;
+    if (in) {
+      *reinterpret_cast<SHERRY_GLOBAL u32x4*>(as_global_mut(a.c.k) + to[u] * e + p) = x[u];
+      *reinterpret_cast<SHERRY_GLOBAL u32x4*>(as_global_mut(a.c.v) + to[u] * e + p) = y[u];
+    }
+    if (scale) {
+      as_global_mut(a.c.ks)[sto[u]] = sx[u];
+      as_global_mut(a.c.vs)[sto[u]] = sy[u];
+    }
+  }
+}
+
+template <int LPR>
+int launch_move(const Evict& a, hipStream_t s) {
+  const int64_t blocks = int64_t(a.c.batch) * a.c.kv * ceil_div(a.keep, 256 / LPR * kMoveAt);
+  return launch(evict_move_kernel<LPR>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
 }
 
 }  // namespace
@@ -226,13 +350,17 @@ int launch_evict(const sherry_cache_desc& c, const sherry_evict_desc& d, hipStre
   const Evict a{cache_of(c), d.length, d.weight, d.position, d.recent_from, d.length_out, d.kept,
                 d.weight_out, d.position_out, d.row_stride, d.out_stride, d.keep,
                 c.head_dim * type_bytes(c.type)};
-  const int64_t heads = int64_t(c.batch) * c.kv_heads;
-  const int rc = launch(evict_select_kernel, dim3(static_cast<unsigned>(heads)), dim3(kThreads), 0, s, a);
-  if (rc != SHERRY_OK || d.keep >= a.c.rows) return rc;  // (a sequence that fits keep moves nothing)
-  int lpr = 1;
-  while (lpr < 32 && 16 * lpr < a.bytes) lpr *= 2;
-  return launch(evict_move_kernel, dim3(static_cast<unsigned>(heads * ceil_div(d.keep, kMoveRows))),
-                dim3(256), 0, s, a, lpr);
+  const dim3 grid(static_cast<unsigned>(int64_t(c.batch) * c.kv_heads)), block(kThreads);
+  const int64_t rows = a.c.rows;
+  const int rc = rows <= 4 * kThreads    ? launch(evict_select_kernel<4>, grid, block, 0, s, a)
+                 : rows <= 16 * kThreads ? launch(evict_select_kernel<16>, grid, block, 0, s, a)
+                 : rows <= 48 * kThreads ? launch(evict_select_kernel<48>, grid, block, 0, s, a)
+                                         : launch(evict_select_kernel<0>, grid, block, 0, s, a);
+  if (rc != SHERRY_OK || d.keep >= rows) return rc;  // (a sequence that fits keep moves nothing)
+  if (a.bytes <= 64) return launch_move<4>(a, s);
+  if (a.bytes <= 128) return launch_move<8>(a, s);
+  if (a.bytes <= 256) return launch_move<16>(a, s);
+  return launch_move<32>(a, s);
 }
 
 }  // namespace sherry
