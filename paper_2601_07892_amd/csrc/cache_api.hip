@@ -99,8 +99,9 @@ int check_evict(const sherry_cache_desc* c, const sherry_evict_desc* a) {
   if (a->keep < 1 || a->keep > SHERRY_MAX_CACHE_ROWS || a->row_stride < cache_rows(c) ||
       a->out_stride < a->keep)
     return SHERRY_E_SHAPE;
-  // (the moving launch: one workgroup per 32 or more new rows)
-  if (int64_t(c->batch) * c->kv_heads * ceil_div(a->keep, 32) > INT32_MAX) return SHERRY_E_SHAPE;
+  // (the moving launch: one workgroup per 32 or more new rows, and per 1024)
+  if (int64_t(c->batch) * c->kv_heads * (ceil_div(a->keep, 32) + ceil_div(a->keep, 1024)) > INT32_MAX)
+    return SHERRY_E_SHAPE;
   if (!aligned(a->length, 4) || !aligned(a->weight, 4) || !aligned(a->position, 4) ||
       !aligned(a->recent_from, 4) || !aligned(a->length_out, 4) || !aligned(a->kept, 4) ||
       !aligned(a->weight_out, 4) || !aligned(a->position_out, 4))

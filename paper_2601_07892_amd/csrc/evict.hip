@@ -5,8 +5,9 @@
 // largest key (a radix select over the fp32 weights as ordered integers,
 // protected rows above all) and writes, for every new row, its former slot:
 // rows kept below the new length stay, the j-th kept row past it goes to the
-// j-th slot given up below it.  move: copies those rows; sources lie past the
-// new length and destinations below it, so the copies need no order.
+// j-th slot given up below it.  move: copies those rows, and every new row's
+// weight and position; sources lie past the new length and destinations below
+// it, so the copies need no order.
 //
 // What bounds it: the rows that move are read and written once, the weights
 // and positions read; below some thousand rows the two launches.
@@ -44,10 +45,6 @@ struct Keys {
   const int32_t* pos;
   int from;
   bool recent;
-  __device__ __forceinline__ uint32_t at(int i) const {
-    if (recent && (pos ? as_global(pos)[i] : i) >= from) return 0xFFFFFFFFu;
-    return weight_key(as_global(w)[i]);
-  }
 };
 
 // Exclusive sum of one value per wave, over the workgroup's waves in order;
@@ -66,47 +63,56 @@ __device__ __forceinline__ int waves_before(int v, int* part, int& total) {
   return before;
 }
 
-// Each wave takes a run of slots, 64 at a time, and keeps their keys: J per
+// Each wave takes a run of slots, in chunks of 64, and keeps their keys: J per
 // lane, for sequences of up to 1024 J rows; J = 0 reads them again in every pass.
 template <int J>
 struct Run {
   const Keys& keys;
   int first, end;  // of this wave
+  int last;        // of the sequence
   uint32_t key[J > 0 ? J : 1];
 
-  __device__ __forceinline__ Run(const Keys& k, int n) : keys(k) {
-    const int seg = J > 0 ? 64 * J : ((n + kWaves - 1) / kWaves + 63) / 64 * 64;
-    // (short sequences are spread over the waves too)
-    const int even = ((n + kWaves - 1) / kWaves + 63) / 64 * 64;
-    const int use = even < seg ? even : seg;
-    first = static_cast<int>(threadIdx.x >> 6) * use;
-    end = first + use < n ? first + use : n;
+  __device__ __forceinline__ Run(const Keys& k, int n) : keys(k), last(n - 1) {
+    const int seg = ((n + kWaves - 1) / kWaves + 63) / 64 * 64;
+    first = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6) * seg);
+    end = __builtin_amdgcn_readfirstlane(first + seg < n ? first + seg : n);
     if constexpr (J > 0) {
-      // (every load goes out, so that none waits for another's branch)
-      float w[J];
-      int32_t p[J];
-      const int last = n - 1;
+      constexpr int AT = J < 16 ? J : 16;
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const int i = first + 64 * j + static_cast<int>(threadIdx.x & 63);
-        w[j] = as_global(keys.w)[i < last ? i : last];
-      }
-      if (keys.recent && keys.pos) {
+      for (int j0 = 0; j0 < J; j0 += AT) {
+        uint32_t k16[AT];
+        load<AT>(first + 64 * j0, k16);
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-          const int i = first + 64 * j + static_cast<int>(threadIdx.x & 63);
-          p[j] = as_global(keys.pos)[i < last ? i : last];
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const int i = first + 64 * j + static_cast<int>(threadIdx.x & 63);
-        const bool recent = keys.recent && (keys.pos ? p[j] : i) >= keys.from;
-        key[j] = recent ? 0xFFFFFFFFu : weight_key(w[j]);
+        for (int u = 0; u < AT; ++u) key[j0 + u] = k16[u];
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
-  // f(j, slot, whether it is of the run, its key): in order; every lane calls it.
+  // Keys of AT chunks from slot i0 on (past the last slot, that of the last):
+  // every load goes out, so that none waits for another's branch.
+  template <int AT>
+  __device__ __forceinline__ void load(int i0, uint32_t (&k)[AT]) const {
+    const int lane = threadIdx.x & 63;
+    float w[AT];
+    int32_t p[AT];
+#pragma unroll
+    for (int u = 0; u < AT; ++u) {
+      const int i = i0 + 64 * u + lane;
+      w[u] = as_global(keys.w)[i < last ? i : last];
+      p[u] = i;
+    }
+    if (keys.recent && keys.pos) {
+#pragma unroll
+      for (int u = 0; u < AT; ++u) {
+        const int i = i0 + 64 * u + lane;
+        p[u] = as_global(keys.pos)[i < last ? i : last];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < AT; ++u)
+      k[u] = keys.recent && p[u] >= keys.from ? 0xFFFFFFFFu : weight_key(w[u]);
+  }
+  // f(chunk, slot, whether it is of the run, its key): in order; every lane calls it.
   template <class F>
   __device__ __forceinline__ void each(F&& f) const {
     const int lane = threadIdx.x & 63;
@@ -117,13 +123,30 @@ struct Run {
         f(j, first + 64 * j + lane, first + 64 * j + lane < end, key[j]);
       }
     } else {
-      for (int i = first; i < end; i += 64) {
-        const bool in = i + lane < end;
-        f(0, i + lane, in, in ? keys.at(i + lane) : 0u);
+      constexpr int AT = 16;  // chunks whose loads go out together
+      for (int i0 = first; i0 < end; i0 += 64 * AT) {
+        uint32_t k[AT];
+        load<AT>(i0, k);
+#pragma unroll
+        for (int u = 0; u < AT; ++u) {
+          const int i = i0 + 64 * u;
+          if (i >= end) break;
+          f((i - first) / 64, i + lane, i + lane < end, k[u]);
+        }
       }
     }
   }
 };
+
+__device__ __forceinline__ int wave_scan_int(int v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(v, o, 64);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
 
 template <int J>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
@@ -139,20 +162,10 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
   const int32_t* pos = a.position ? a.position + row : nullptr;
   const int tid = threadIdx.x, lane = tid & 63;
   if (h == 0 && tid == 0) as_global_mut(a.length_out)[b] = m;
-  auto put = [&](int i, int src) {
-    as_global_mut(a.kept)[orow + i] = src;
-    if (a.weight_out) as_global_mut(a.weight_out)[orow + i] = as_global(w)[src];
-    if (a.position_out) as_global_mut(a.position_out)[orow + i] = pos ? as_global(pos)[src] : src;
-  };
-  for (int i = m + tid; i < a.keep; i += kThreads) {
-    as_global_mut(a.kept)[orow + i] = -1;
-    if (a.weight_out) as_global_mut(a.weight_out)[orow + i] = 0.0f;
-    if (a.position_out) as_global_mut(a.position_out)[orow + i] = 0;
-  }
-  if (n <= a.keep) {
-    for (int i = tid; i < n; i += kThreads) put(i, i);
-    return;
-  }
+  // past the end -1; a sequence that fits stays as it is
+  for (int i = (n <= a.keep ? 0 : m) + tid; i < a.keep; i += kThreads)
+    as_global_mut(a.kept)[orow + i] = i < m ? i : -1;
+  if (n <= a.keep) return;
   const Keys keys{w, pos, a.recent_from ? as_global(a.recent_from)[b] : 0, a.recent_from != nullptr};
   const Run<J> run(keys, n);
 
@@ -176,12 +189,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
     __syncthreads();
     // thread t: bins 2047 - 2 t and 2046 - 2 t, from the largest down
     const int c0 = hist[2047 - 2 * tid], c1 = hist[2046 - 2 * tid];
-    int upto = c0 + c1;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += v;
-    }
+    const int upto = wave_scan_int(c0 + c1);
     int total;
     const int before = waves_before(__shfl(upto, 63, 64), part, total) + upto - c0 - c1;
     const bool first = before < want && before + c0 >= want;
@@ -198,75 +206,89 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
   // kept: every key above prefix (in its bits), and the first `want` that
   // equal it
   const uint64_t below = (1ull << lane) - 1;
-  int equal = 0;
-  run.each([&](int, int, bool in, uint32_t k) { equal += __popcll(__ballot(in && (k >> shift) == prefix)); });
-  int total;
-  const int equal0 = waves_before(equal, part, total);
-  // holes (slots below m given up) and movers (kept slots past it)
-  auto scan = [&](auto&& each) {
-    int eq = equal0;
+  const bool ties = found[2] != static_cast<uint32_t>(want);
+  int total, eq = 0;
+  if (ties) {
+    int equal = 0;
+    run.each([&](int, int, bool in, uint32_t k) { equal += __popcll(__ballot(in && (k >> shift) == prefix)); });
+    eq = waves_before(equal, part, total);
+  }
+  // f(chunk, slot of lane 0, lanes of the chunk that are kept)
+  auto chunks = [&](auto&& f) {
+    int seen = eq;
     run.each([&](int j, int i, bool in, uint32_t k) {
       const uint32_t top = k >> shift;
-      const uint64_t e = __ballot(in && top == prefix);
-      const bool keep = in && (top > prefix || (top == prefix && eq + __popcll(e & below) < want));
-      eq += __popcll(e);
-      each(j, i, in && !keep && i < m, keep && i >= m, keep && i < m);
+      bool keep = in && top >= prefix;
+      if (ties) {
+        const uint64_t e = __ballot(in && top == prefix);
+        keep = keep && (top > prefix || seen + __popcll(e & below) < want);
+        seen += __popcll(e);
+      }
+      f(j, i - lane, __ballot(keep));
     });
   };
-  int holes = 0, movers = 0;
-  scan([&](int, int, bool hole, bool mover, bool) {
-    holes += __popcll(__ballot(hole));
-    movers += __popcll(__ballot(mover));
+  // Kept slots past m (movers) go to slots below m that are not (holes).  The
+  // wave's kept lanes, one chunk a lane, give every chunk its first mover's and
+  // first hole's number.
+  auto below_m = [&](int i0) {  // lanes of a chunk whose slots are below m (and the run's end)
+    const int k = (m < run.end ? m : run.end) - i0;
+    return k <= 0 ? 0ull : k >= 64 ? ~0ull : (1ull << k) - 1;
+  };
+  int n_moves = 0, n_holes = 0;  // of the wave
+  uint64_t mine = 0;             // J > 0: chunk lane's kept lanes
+  chunks([&](int j, int i0, uint64_t kept) {
+    const uint64_t low = below_m(i0);
+    n_moves += __popcll(kept & ~low);
+    n_holes += __popcll(~kept & low);
+    if (J > 0 && lane == j) mine = kept;
   });
-  int moves, moves2;
-  const int hole0 = waves_before(holes, part, moves);
-  const int mover0 = waves_before(movers, part, moves2);
+  int moves, holes;
+  const int mover0 = waves_before(n_moves, part, moves);
+  const int hole0 = waves_before(n_holes, part, holes);
+  int my_moves = 0, my_holes = 0;  // J > 0: before chunk `lane` of the wave
+  if constexpr (J > 0) {
+    const uint64_t low = below_m(run.first + 64 * lane);
+    const int c = __popcll(mine & ~low), d = __popcll(~mine & low);
+    my_moves = wave_scan_int(c) - c;
+    my_holes = wave_scan_int(d) - d;
+  }
+  // every chunk's kept lanes again, with the numbers of its first mover and hole
+  auto again = [&](auto&& f) {
+    if constexpr (J > 0) {
+      const int count = (run.end - run.first + 63) / 64;
+      for (int j = 0; j < count; ++j) {
+        const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(mine >> 32), j);
+        const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(mine), j);
+        const uint64_t kept = uint64_t(hi) << 32 | lo;
+        f(run.first + 64 * j, kept, mover0 + __builtin_amdgcn_readlane(my_moves, j),
+          hole0 + __builtin_amdgcn_readlane(my_holes, j));
+      }
+    } else {
+      int r = mover0, q = hole0;
+      chunks([&](int, int i0, uint64_t kept) {
+        f(i0, kept, r, q);
+        const uint64_t low = below_m(i0);
+        r += __popcll(kept & ~low);
+        q += __popcll(~kept & low);
+      });
+    }
+  };
   for (int base = 0; base == 0 || base < moves; base += kList) {
     __syncthreads();
-    int rank = mover0 - base;
-    scan([&](int, int i, bool, bool mover, bool) {
-      const uint64_t who = __ballot(mover);
-      const int at = rank + __popcll(who & below);
-      if (mover && at >= 0 && at < kList) list[at] = i;
-      rank += __popcll(who);
+    again([&](int i0, uint64_t kept, int r, int) {
+      const uint64_t who = kept & ~below_m(i0);
+      const int at = r - base + __popcll(who & below);
+      if ((who >> lane & 1) && at >= 0 && at < kList) list[at] = i0 + lane;
     });
     __syncthreads();
-    rank = hole0 - base;
-    scan([&](int, int i, bool hole, bool, bool stays) {
-      const uint64_t who = __ballot(hole);
-      const int at = rank + __popcll(who & below);
+    again([&](int i0, uint64_t kept, int, int q) {
+      const uint64_t low = below_m(i0), who = ~kept & low;
+      const int at = q - base + __popcll(who & below);
       int src = -1;
-      if (hole && at >= 0 && at < kList) src = list[at];
-      if (stays && base == 0) src = i;
-      if (src >= 0) as_global_mut(a.kept)[orow + i] = src;
-      rank += __popcll(who);
+      if ((who >> lane & 1) && at >= 0 && at < kList) src = list[at];
+      if ((kept & low) >> lane & 1) src = base == 0 ? i0 + lane : -1;
+      if (src >= 0) as_global_mut(a.kept)[orow + i0 + lane] = src;
     });
-  }
-  if (!a.weight_out && !a.position_out) return;
-  // the kept rows' weights and positions, eight a thread at once
-  __syncthreads();
-  constexpr int AT = 8;
-  for (int i0 = tid; i0 < m; i0 += AT * kThreads) {
-    int src[AT];
-    float x[AT];
-    int32_t p[AT];
-#pragma unroll
-    for (int u = 0; u < AT; ++u) {
-      const int i = i0 + u * kThreads;
-      src[u] = as_global(a.kept)[orow + (i < m ? i : i0)];
-    }
-#pragma unroll
-    for (int u = 0; u < AT; ++u) {
-      x[u] = as_global(w)[src[u]];
-      p[u] = pos ? as_global(pos)[src[u]] : src[u];
-    }
-#pragma unroll
-    for (int u = 0; u < AT; ++u) {
-      const int i = i0 + u * kThreads;
-      if (i >= m) break;
-      if (a.weight_out) as_global_mut(a.weight_out)[orow + i] = x[u];
-      if (a.position_out) as_global_mut(a.position_out)[orow + i] = p[u];
-    }
   }
 }
 
@@ -274,9 +296,39 @@ constexpr int kMoveAt = 4;  // rows in flight per thread
 
 // LPR lanes of 16 bytes per row (rows of 8 bytes do not exist: head_dim is a
 // multiple of 8, of 16 in int8), 256 / LPR * kMoveAt new rows per workgroup.
+// Past `copies` workgroups, the new rows' weights and positions, 256 * kMoveAt of
+// them per workgroup.
 template <int LPR>
-__global__ __launch_bounds__(256) void evict_move_kernel(Evict a) {
+__global__ __launch_bounds__(256) void evict_move_kernel(Evict a, int copies) {
   constexpr int ROWS = 256 / LPR, PER = ROWS * kMoveAt;
+  if (static_cast<int>(blockIdx.x) >= copies) {
+    constexpr int ALL = 256 * kMoveAt;
+    const int chunks = (a.keep + ALL - 1) / ALL, blk = static_cast<int>(blockIdx.x) - copies;
+    const int bh = blk / chunks, i0 = (blk - bh * chunks) * ALL + threadIdx.x;
+    const int64_t row = int64_t(bh) * a.row_stride, orow = int64_t(bh) * a.out_stride;
+    int src[kMoveAt];
+    float w[kMoveAt];
+    int32_t pos[kMoveAt];
+#pragma unroll
+    for (int u = 0; u < kMoveAt; ++u) {
+      const int i = i0 + 256 * u;
+      src[u] = i < a.keep ? as_global(a.kept)[orow + i] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kMoveAt; ++u) {
+      const int64_t at = row + (src[u] < 0 ? 0 : src[u]);
+      w[u] = a.weight_out ? as_global(a.weight)[at] : 0.0f;
+      pos[u] = a.position_out && a.position ? as_global(a.position)[at] : src[u];
+    }
+#pragma unroll
+    for (int u = 0; u < kMoveAt; ++u) {
+      const int i = i0 + 256 * u;
+      if (i >= a.keep) break;
+      if (a.weight_out) as_global_mut(a.weight_out)[orow + i] = src[u] < 0 ? 0.0f : w[u];
+      if (a.position_out) as_global_mut(a.position_out)[orow + i] = src[u] < 0 ? 0 : pos[u];
+    }
+    return;
+  }
   const int chunks = (a.keep + PER - 1) / PER;
   const int bh = blockIdx.x / chunks, ch = blockIdx.x - bh * chunks;
   const int b = bh / a.c.kv, h = bh - b * a.c.kv;
@@ -284,11 +336,12 @@ __global__ __launch_bounds__(256) void evict_move_kernel(Evict a) {
   const int p = 16 * (threadIdx.x % LPR), i0 = ch * PER + threadIdx.x / LPR;
   const int e = a.bytes / a.c.dim;
   const int64_t trow = int64_t(b) * a.c.width;
+  const int64_t orow = int64_t(bh) * a.out_stride;
   int src[kMoveAt];
 #pragma unroll
   for (int u = 0; u < kMoveAt; ++u) {
     const int i = i0 + u * ROWS;
-    src[u] = i < a.keep ? as_global(a.kept)[int64_t(bh) * a.out_stride + i] : i;
+    src[u] = i < a.keep ? as_global(a.kept)[orow + i] : i;
   }
   if (n <= a.keep) return;
   bool live[kMoveAt];
@@ -340,8 +393,13 @@ __global__ __launch_bounds__(256) void evict_move_kernel(Evict a) {
 
 template <int LPR>
 int launch_move(const Evict& a, hipStream_t s) {
-  const int64_t blocks = int64_t(a.c.batch) * a.c.kv * ceil_div(a.keep, 256 / LPR * kMoveAt);
-  return launch(evict_move_kernel<LPR>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
+  const int64_t heads = int64_t(a.c.batch) * a.c.kv;
+  // (with room for every row nothing moves)
+  const int64_t copies = a.keep < a.c.rows ? heads * ceil_div(a.keep, 256 / LPR * kMoveAt) : 0;
+  const int64_t outs = a.weight_out || a.position_out ? heads * ceil_div(a.keep, 256 * kMoveAt) : 0;
+  if (copies + outs == 0) return SHERRY_OK;
+  return launch(evict_move_kernel<LPR>, dim3(static_cast<unsigned>(copies + outs)), dim3(256), 0, s, a,
+                static_cast<int>(copies));
 }
 
 }  // namespace
@@ -354,9 +412,9 @@ int launch_evict(const sherry_cache_desc& c, const sherry_evict_desc& d, hipStre
   const int64_t rows = a.c.rows;
   const int rc = rows <= 4 * kThreads    ? launch(evict_select_kernel<4>, grid, block, 0, s, a)
                  : rows <= 16 * kThreads ? launch(evict_select_kernel<16>, grid, block, 0, s, a)
-                 : rows <= 48 * kThreads ? launch(evict_select_kernel<48>, grid, block, 0, s, a)
+                 : rows <= 64 * kThreads ? launch(evict_select_kernel<64>, grid, block, 0, s, a)
                                          : launch(evict_select_kernel<0>, grid, block, 0, s, a);
-  if (rc != SHERRY_OK || d.keep >= rows) return rc;  // (a sequence that fits keep moves nothing)
+  if (rc != SHERRY_OK) return rc;
   if (a.bytes <= 64) return launch_move<4>(a, s);
   if (a.bytes <= 128) return launch_move<8>(a, s);
   if (a.bytes <= 256) return launch_move<16>(a, s);
