@@ -4,8 +4,9 @@
 //   y_a = a c - b s,  y_b = b c + a s  in fp32, each operation rounded
 //
 // What bounds it: the bytes of the tokens' q, k and v rows, read and written
-// once; a decode batch's few hundred rows cost one launch.  A row takes
-// DP / 4 lanes of four values, so that its absolute maximum (int8) is a
+// once; a decode batch's few hundred rows cost one launch.  A workgroup takes
+// rows of one token, whose place in the cache is then found by scalar loads; a
+// row takes DP / 4 lanes of four values, so that its absolute maximum (int8) is a
 // reduction inside a wave, and its rotation partner is read from the row
 // again, out of the caches.
 #include "cache_internal.h"
@@ -28,42 +29,50 @@ struct Append {
   int32_t* position;
   int64_t row_stride, q_stride, k_stride, v_stride, q_out_stride;
   int tokens, heads, type, cache_type, rope_rows, rot, pairs;
+  FastDiv by_parts;  // workgroups per token
 };
 
-template <bool VEC>
-__device__ __forceinline__ float4 load4(const void* p, int64_t i, int type) {
-  if constexpr (VEC) {
-    if (type == SHERRY_F32)
-      return *reinterpret_cast<const SHERRY_GLOBAL float4*>(as_global(static_cast<const float*>(p)) + i);
-    typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+
+// TYPE: SHERRY_F32, _F16 or _BF16 of q, k, v and q_out.  VEC: their rows and the
+// angles' start at multiples of four values.
+template <int TYPE>
+__device__ __forceinline__ float load1(const void* p, int64_t i) {
+  return load_as_f32(p, i, TYPE);
+}
+template <int TYPE, bool VEC>
+__device__ __forceinline__ float4 load4(const void* p, int64_t i) {
+  if constexpr (!VEC) {
+    return make_float4(load1<TYPE>(p, i), load1<TYPE>(p, i + 1), load1<TYPE>(p, i + 2), load1<TYPE>(p, i + 3));
+  } else if constexpr (TYPE == SHERRY_F32) {
+    return *reinterpret_cast<const SHERRY_GLOBAL float4*>(as_global(static_cast<const float*>(p)) + i);
+  } else {
     const u16x4 h = *reinterpret_cast<const SHERRY_GLOBAL u16x4*>(as_global(static_cast<const uint16_t*>(p)) + i);
-    return type == SHERRY_BF16
+    return TYPE == SHERRY_BF16
                ? make_float4(from_bf16(h[0]), from_bf16(h[1]), from_bf16(h[2]), from_bf16(h[3]))
                : make_float4(from_f16(h[0]), from_f16(h[1]), from_f16(h[2]), from_f16(h[3]));
-  } else {
-    return make_float4(load_as_f32(p, i, type), load_as_f32(p, i + 1, type),
-                       load_as_f32(p, i + 2, type), load_as_f32(p, i + 3, type));
   }
 }
 
 // Values d .. d + 3 of a row at element `at`, rotated.
-template <bool VEC>
+template <int TYPE, bool VEC>
 __device__ __forceinline__ float4 rotated(const Append& a, const void* p, int64_t at, int d, int pos) {
-  const float4 x = load4<VEC>(p, at + d, a.type);
+  const float4 x = load4<TYPE, VEC>(p, at + d);
   if (!a.cos || d >= a.rot) return x;
   const int half = a.rot >> 1;
   const float* cs = a.cos + int64_t(pos) * half;
   const float* sn = a.sin + int64_t(pos) * half;
   if (VEC && !a.pairs && half % 4 == 0) {
-    // the four partners are together
-    const int i = d < half ? d : d - half;
-    const float4 w = load4<VEC>(p, at + (d < half ? d + half : i), a.type);
+    // the four partners are together; their products are added or subtracted,
+    // which is the same as adding those of the negated sine
+    const bool first = d < half;
+    const int i = first ? d : d - half;
+    const float4 w = load4<TYPE, VEC>(p, at + (first ? d + half : i));
     const float4 c = *reinterpret_cast<const SHERRY_GLOBAL float4*>(as_global(cs) + i);
     const float4 s = *reinterpret_cast<const SHERRY_GLOBAL float4*>(as_global(sn) + i);
-    return d < half ? make_float4(x.x * c.x - w.x * s.x, x.y * c.y - w.y * s.y, x.z * c.z - w.z * s.z,
-                                  x.w * c.w - w.w * s.w)
-                    : make_float4(x.x * c.x + w.x * s.x, x.y * c.y + w.y * s.y, x.z * c.z + w.z * s.z,
-                                  x.w * c.w + w.w * s.w);
+    const float sg = first ? -1.0f : 1.0f;
+    return make_float4(x.x * c.x + w.x * (sg * s.x), x.y * c.y + w.y * (sg * s.y),
+                       x.z * c.z + w.z * (sg * s.z), x.w * c.w + w.w * (sg * s.w));
   }
   float r[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
@@ -73,59 +82,56 @@ __device__ __forceinline__ float4 rotated(const Append& a, const void* p, int64_
     const bool first = a.pairs ? (j & 1) == 0 : j < half;
     const int i = a.pairs ? j >> 1 : first ? j : j - half;
     const int other = a.pairs ? j ^ 1 : first ? j + half : i;
-    const float w = load_as_f32(p, at + other, a.type) * as_global(sn)[i];
+    const float w = load1<TYPE>(p, at + other) * as_global(sn)[i];
     const float v = r[e] * as_global(cs)[i];
     r[e] = first ? v - w : v + w;
   }
   return make_float4(r[0], r[1], r[2], r[3]);
 }
 
-template <bool VEC>
-__device__ __forceinline__ void store4(void* p, int64_t i, int type, float4 v) {
-  if (VEC && type == SHERRY_F32) {
+__device__ __forceinline__ u16x4 to_16(int type, float4 v) {
+  return type == SHERRY_BF16 ? u16x4{to_bf16(v.x), to_bf16(v.y), to_bf16(v.z), to_bf16(v.w)}
+                             : u16x4{to_f16(v.x), to_f16(v.y), to_f16(v.z), to_f16(v.w)};
+}
+template <int TYPE, bool VEC>
+__device__ __forceinline__ void store4(void* p, int64_t i, float4 v) {
+  if constexpr (!VEC) {
+    store_from_f32(p, i, TYPE, v.x);
+    store_from_f32(p, i + 1, TYPE, v.y);
+    store_from_f32(p, i + 2, TYPE, v.z);
+    store_from_f32(p, i + 3, TYPE, v.w);
+  } else if constexpr (TYPE == SHERRY_F32) {
     *reinterpret_cast<SHERRY_GLOBAL float4*>(as_global_mut(static_cast<float*>(p)) + i) = v;
-  } else if (VEC) {
-    typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
-    const u16x4 h = type == SHERRY_BF16 ? u16x4{to_bf16(v.x), to_bf16(v.y), to_bf16(v.z), to_bf16(v.w)}
-                                        : u16x4{to_f16(v.x), to_f16(v.y), to_f16(v.z), to_f16(v.w)};
-    *reinterpret_cast<SHERRY_GLOBAL u16x4*>(as_global_mut(static_cast<uint16_t*>(p)) + i) = h;
   } else {
-    store_from_f32(p, i, type, v.x);
-    store_from_f32(p, i + 1, type, v.y);
-    store_from_f32(p, i + 2, type, v.z);
-    store_from_f32(p, i + 3, type, v.w);
+    *reinterpret_cast<SHERRY_GLOBAL u16x4*>(as_global_mut(static_cast<uint16_t*>(p)) + i) = to_16(TYPE, v);
   }
 }
 
-// One row (a head of q, k or v of one token) per LPR lanes.
-template <int LPR, bool VEC>
+// 256 / LPR rows (heads of q, k, v) of one token per workgroup, one per LPR lanes.
+template <int LPR, int TYPE, bool VEC>
 __global__ __launch_bounds__(256) void append_kernel(Append a) {
-  constexpr int RPB = 256 / LPR;
-  const int per = a.heads + 2 * a.c.kv;  // rows of a token: q, k, v heads
-  const int64_t row = int64_t(blockIdx.x) * RPB + threadIdx.x / LPR;
+  const int t = a.by_parts.div(blockIdx.x), part = blockIdx.x - t * a.by_parts.d;
+  const int r = part * (256 / LPR) + threadIdx.x / LPR;
   const int d = 4 * (threadIdx.x % LPR);
-  if (row >= int64_t(a.tokens) * per) return;
-  const int t = static_cast<int>(row / per), r = static_cast<int>(row - int64_t(t) * per);
-  const int seq = as_global(a.seq)[t], slot = as_global(a.slot)[t], pos = as_global(a.pos)[t];
+  const int seq = as_const(a.seq)[t], slot = as_const(a.slot)[t], pos = as_const(a.pos)[t];
   if (seq < 0 || seq >= a.c.batch || slot < 0 || slot >= a.c.rows) return;
   if (a.cos && (pos < 0 || pos >= a.rope_rows)) return;
   const int in_table = a.c.by_page.div(slot);
-  const int page = as_global(a.c.table)[int64_t(seq) * a.c.width + in_table];
-  if (page < 0 || page >= a.c.pages) return;
-  // (all of a row's lanes are here or none)
+  const int page = as_const(a.c.table)[int64_t(seq) * a.c.width + in_table];
+  if (page < 0 || page >= a.c.pages || r >= a.heads + 2 * a.c.kv) return;
   const bool in = d < a.c.dim;
   if (r < a.heads) {
     if (in)
-      store4<VEC>(a.q_out, int64_t(t) * a.q_out_stride + int64_t(r) * a.c.dim + d, a.type,
-                  rotated<VEC>(a, a.q, int64_t(t) * a.q_stride + int64_t(r) * a.c.dim, d, pos));
+      store4<TYPE, VEC>(a.q_out, int64_t(t) * a.q_out_stride + r * a.c.dim + d,
+                        rotated<TYPE, VEC>(a, a.q, int64_t(t) * a.q_stride + r * a.c.dim, d, pos));
     return;
   }
   const bool is_k = r < a.heads + a.c.kv;
   const int h = r - a.heads - (is_k ? 0 : a.c.kv);
   float4 x = make_float4(0, 0, 0, 0);
   if (in)
-    x = is_k ? rotated<VEC>(a, a.k, int64_t(t) * a.k_stride + int64_t(h) * a.c.dim, d, pos)
-             : load4<VEC>(a.v, int64_t(t) * a.v_stride + int64_t(h) * a.c.dim + d, a.type);
+    x = is_k ? rotated<TYPE, VEC>(a, a.k, int64_t(t) * a.k_stride + h * a.c.dim, d, pos)
+             : load4<TYPE, VEC>(a.v, int64_t(t) * a.v_stride + h * a.c.dim + d);
   const int off = slot - in_table * a.c.page_size;
   char* pool = is_k ? a.c.k : a.c.v;
   const int64_t at = a.c.at(page, h) + int64_t(off) * a.c.dim + d;
@@ -139,7 +145,8 @@ __global__ __launch_bounds__(256) void append_kernel(Append a) {
           top == 0.0f ? 0u : quant4(x, s, 1.0f / s);
     if (d == 0) as_global_mut(is_k ? a.c.ks : a.c.vs)[a.c.scale_at(page, h) + off] = s;
   } else if (in) {
-    store4<true>(pool, at, a.cache_type, x);
+    *reinterpret_cast<SHERRY_GLOBAL u16x4*>(as_global_mut(reinterpret_cast<uint16_t*>(pool)) + at) =
+        to_16(a.cache_type, x);
   }
   if (is_k && d == 0) {
     const int64_t w = (int64_t(seq) * a.c.kv + h) * a.row_stride + slot;
@@ -148,12 +155,20 @@ __global__ __launch_bounds__(256) void append_kernel(Append a) {
   }
 }
 
+template <int LPR, int TYPE>
+int launch_type(const Append& a, bool vec, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(int64_t(a.tokens) * a.by_parts.d));
+  return vec ? launch(append_kernel<LPR, TYPE, true>, grid, dim3(256), 0, s, a)
+             : launch(append_kernel<LPR, TYPE, false>, grid, dim3(256), 0, s, a);
+}
 template <int LPR>
-int launch_lanes(const Append& a, bool vec, hipStream_t s) {
-  const int64_t rows = int64_t(a.tokens) * (a.heads + 2 * a.c.kv);
-  const dim3 grid(static_cast<unsigned>(ceil_div(rows, 256 / LPR)));
-  return vec ? launch(append_kernel<LPR, true>, grid, dim3(256), 0, s, a)
-             : launch(append_kernel<LPR, false>, grid, dim3(256), 0, s, a);
+int launch_lanes(Append a, bool vec, hipStream_t s) {
+  a.by_parts = FastDiv::of(static_cast<uint32_t>(ceil_div(a.heads + 2 * a.c.kv, 256 / LPR)));
+  switch (a.type) {
+    case SHERRY_F32: return launch_type<LPR, SHERRY_F32>(a, vec, s);
+    case SHERRY_F16: return launch_type<LPR, SHERRY_F16>(a, vec, s);
+    default: return launch_type<LPR, SHERRY_BF16>(a, vec, s);
+  }
 }
 
 }  // namespace
@@ -164,7 +179,7 @@ int launch_append(const sherry_cache_desc& c, const sherry_append_desc& d, hipSt
   const Append a{cache_of(c), d.q, d.k, d.v, d.q_out, d.seq, d.slot, d.pos, d.cos, d.sin, d.weight,
                  d.position, d.row_stride, d.q_stride ? d.q_stride : qrow, d.k_stride ? d.k_stride : row,
                  d.v_stride ? d.v_stride : row, d.q_out_stride ? d.q_out_stride : qrow, d.tokens, heads,
-                 d.type, c.type, d.rope_rows, d.rot_dim, d.pairing == SHERRY_ROPE_PAIRS};
+                 d.type, c.type, d.rope_rows, d.rot_dim, d.pairing == SHERRY_ROPE_PAIRS, FastDiv{1, 0, 0}};
   // four values at once where every row starts at a multiple of them
   const uintptr_t bytes = 4 * static_cast<uintptr_t>(type_bytes(d.type));
   auto whole = [&](const void* p, int64_t stride) {

@@ -95,17 +95,6 @@ __device__ __forceinline__ Span span_of(const Attend& a, int b) {
   return Span{last && n > a.window ? n - a.window : 0, n};
 }
 
-// Inclusive sums over the lanes (steps inside 16 lanes, then across them).
-__device__ __forceinline__ int wave_scan(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);  // from 1, 2, 4, 8 lanes below
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, true);  // lane 15 of the row below
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, true);  // lane 31
-  return v;
-}
-
 // What a sequence costs a workgroup besides its tiles (finding it, its q, the
 // first loads, the sums' way out), in tiles.  Without it a workgroup that
 // gets many short sequences ends the launch.

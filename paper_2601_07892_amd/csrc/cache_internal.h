@@ -83,6 +83,17 @@ __device__ __forceinline__ void store_from_f32(void* p, int64_t i, int type, flo
   else as_global_mut(static_cast<uint16_t*>(p))[i] = type == SHERRY_BF16 ? to_bf16(x) : to_f16(x);
 }
 
+// Inclusive sums over the lanes (steps inside 16 lanes, then across them).
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);  // from 1, 2, 4, 8 lanes below
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, true);  // lane 15 of the row below
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, true);  // lane 31
+  return v;
+}
+
 size_t attend_workspace(const sherry_cache_desc& c, const sherry_attend_desc& a);
 int launch_attend(const sherry_cache_desc& c, const sherry_attend_desc& a, hipStream_t s);
 int launch_append(const sherry_cache_desc& c, const sherry_append_desc& a, hipStream_t s);

@@ -48,19 +48,14 @@ struct Keys {
 };
 
 // Exclusive sum of one value per wave, over the workgroup's waves in order;
-// total: of all.
+// total: of all.  part: kWaves integers that no other call uses.
 __device__ __forceinline__ int waves_before(int v, int* part, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  __syncthreads();
   if (lane == 0) part[wave] = v;
   __syncthreads();
-  int before = 0;
-  total = 0;
-  for (int i = 0; i < kWaves; ++i) {
-    if (i < wave) before += part[i];
-    total += part[i];
-  }
-  return before;
+  const int upto = wave_scan(lane < kWaves ? part[lane] : 0);
+  total = __builtin_amdgcn_readlane(upto, kWaves - 1);
+  return wave ? __builtin_amdgcn_readlane(upto, __builtin_amdgcn_readfirstlane(wave) - 1) : 0;
 }
 
 // Each wave takes a run of slots, in chunks of 64, and keeps their keys: J per
@@ -138,20 +133,10 @@ struct Run {
   }
 };
 
-__device__ __forceinline__ int wave_scan_int(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
-  }
-  return v;
-}
-
 template <int J>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
   __shared__ uint32_t hist[2048];
-  __shared__ int part[kWaves];
+  __shared__ int part[6][kWaves];
   __shared__ uint32_t found[3];
   __shared__ int list[kList];
   const int b = blockIdx.x / a.c.kv, h = blockIdx.x - b * a.c.kv;
@@ -189,9 +174,9 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
     __syncthreads();
     // thread t: bins 2047 - 2 t and 2046 - 2 t, from the largest down
     const int c0 = hist[2047 - 2 * tid], c1 = hist[2046 - 2 * tid];
-    const int upto = wave_scan_int(c0 + c1);
+    const int upto = wave_scan(c0 + c1);
     int total;
-    const int before = waves_before(__shfl(upto, 63, 64), part, total) + upto - c0 - c1;
+    const int before = waves_before(__builtin_amdgcn_readlane(upto, 63), part[r], total) + upto - c0 - c1;
     const bool first = before < want && before + c0 >= want;
     if (first || (before + c0 < want && before + c0 + c1 >= want)) {
       found[0] = first ? 2047 - 2 * tid : 2046 - 2 * tid;
@@ -211,7 +196,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
   if (ties) {
     int equal = 0;
     run.each([&](int, int, bool in, uint32_t k) { equal += __popcll(__ballot(in && (k >> shift) == prefix)); });
-    eq = waves_before(equal, part, total);
+    eq = waves_before(equal, part[3], total);
   }
   // f(chunk, slot of lane 0, lanes of the chunk that are kept)
   auto chunks = [&](auto&& f) {
@@ -243,14 +228,14 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
     if (J > 0 && lane == j) mine = kept;
   });
   int moves, holes;
-  const int mover0 = waves_before(n_moves, part, moves);
-  const int hole0 = waves_before(n_holes, part, holes);
+  const int mover0 = waves_before(n_moves, part[4], moves);
+  const int hole0 = waves_before(n_holes, part[5], holes);
   int my_moves = 0, my_holes = 0;  // J > 0: before chunk `lane` of the wave
   if constexpr (J > 0) {
     const uint64_t low = below_m(run.first + 64 * lane);
     const int c = __popcll(mine & ~low), d = __popcll(~mine & low);
-    my_moves = wave_scan_int(c) - c;
-    my_holes = wave_scan_int(d) - d;
+    my_moves = wave_scan(c) - c;
+    my_holes = wave_scan(d) - d;
   }
   // every chunk's kept lanes again, with the numbers of its first mover and hole
   auto again = [&](auto&& f) {
