@@ -214,23 +214,29 @@ struct WdExtra<NoEpi, PN> {};
 template <int PN>
 struct WdExtra<Epi, PN> {
   float4 bias, gate[PN], residual[PN];
-  static __device__ __forceinline__ float4 four(const float* p, int left, bool whole) {
-    if (whole) return *reinterpret_cast<const SHERRY_GLOBAL float4*>(as_global(p));
-    float v[4];
+  // `left` rows of a piece, in one read (pieces: all four or none) or one by one
+  static __device__ __forceinline__ float4 four(const float* p, int left, bool pieces) {
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (pieces) {
+      if (left <= 0) return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      return *reinterpret_cast<const SHERRY_GLOBAL float4*>(as_global(p));
+    }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = u < left ? as_global(p)[u] : 0.0f;
+    for (int u = 0; u < 4; ++u)
+      if (u < left) v[u] = as_global(p)[u];
     return make_float4(v[0], v[1], v[2], v[3]);
   }
-  __device__ __forceinline__ void load(const Epi& e, int t, int row, int m, int n, bool whole) {
-    const int left = whole ? 4 : n - row;  // rows of the piece that exist
-    if (e.bias) bias = four(e.bias + row, left, whole);
+  // (whole: every token and row of the block exists)
+  __device__ __forceinline__ void load(const Epi& e, int t, int row, int m, int n, bool whole, bool pieces) {
+    const int left = whole ? 4 : n - row;
+    if (e.bias) bias = four(e.bias + row, left, pieces);
 #pragma unroll
     for (int i = 0; i < PN; ++i) {
       const int tok = t + 8 * i;
-      const int in = tok < m ? left : 0;
-      if (e.gate) gate[i] = four(e.gate + int64_t(tok) * e.gate_ld + row, in, whole);
+      const int in = whole ? 4 : tok < m ? left : 0;
+      if (e.gate) gate[i] = four(e.gate + int64_t(tok) * e.gate_ld + row, in, pieces);
       if (e.residual)
-        residual[i] = four(e.residual + int64_t(tok) * e.residual_ld + row, in, whole);
+        residual[i] = four(e.residual + int64_t(tok) * e.residual_ld + row, in, pieces);
     }
   }
   // (one step after the other over all pieces: each activation's code stands once)
@@ -566,16 +572,17 @@ __device__ __forceinline__ void wd_block(const WdProblem& p, int g, int8_t* lds,
   };
   const bool whole = p.m >= G::TOK && (r + 1) * kTileRows <= p.n && (p.n % 4 == 0) &&
                      (reinterpret_cast<uintptr_t>(p.y) % 16 == 0) &&
-                     (!acc_out || reinterpret_cast<uintptr_t>(acc_out) % 16 == 0) && epi_pieces(epi);
+                     (!acc_out || reinterpret_cast<uintptr_t>(acc_out) % 16 == 0);
   const bool vec = (p.n % 4 == 0) && (reinterpret_cast<uintptr_t>(p.y) % 16 == 0) &&
                    (!acc_out || reinterpret_cast<uintptr_t>(acc_out) % 16 == 0);
+  const bool pieces = vec && epi_pieces(epi);
   // what an epilogue reads of a block, a block ahead of its stores (a wait for a
   // load between the stores would wait for those before it)
   WdExtra<E, PN> extra[2];
   auto fetch = [&](int b) {
     if constexpr (E::kUse) {
       const int row = r * kTileRows + 32 * (hs + b % HN) + 4 * c4;
-      extra[b & 1].load(epi, 32 * (b / HN) + tokb + (lane >> 3), row, p.m, p.n, whole);
+      extra[b & 1].load(epi, 32 * (b / HN) + tokb + (lane >> 3), row, p.m, p.n, whole, pieces);
     }
   };
   fetch(0);
@@ -607,11 +614,12 @@ __device__ __forceinline__ void wd_block(const WdProblem& p, int g, int8_t* lds,
       float* yp = as_global_mut(p.y) + int64_t(32 * tb + tokb + (lane >> 3)) * p.n + row;
 #pragma unroll
       for (int i = 0; i < PN; ++i, yp += int64_t(8) * p.n) {
-        if (whole) {
-          *reinterpret_cast<float4*>(yp) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        const int tok = 32 * tb + tokb + (lane >> 3) + 8 * i;
+        if (pieces) {
+          if (whole || (tok < p.m && row < p.n))
+            *reinterpret_cast<float4*>(yp) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
           continue;
         }
-        const int tok = 32 * tb + tokb + (lane >> 3) + 8 * i;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
           if (tok < p.m && row + u < p.n) yp[u] = o[4 * i + u];
