@@ -162,6 +162,11 @@ class Decoder:
         self.x.copy_(self.embed[tokens])
         for layer in self.layers:
             layer.step(self.norm)
+        self.advance()
+        return self.norm(self.x) @ self.head.t()
+
+    def advance(self):
+        """Every sequence is a row longer; past the budget by a page, all are cut."""
         self.length += 1
         self.attended += 1
         self.pos += 1
@@ -173,7 +178,6 @@ class Decoder:
             self.length.copy_(self.length_out)
             self.attended.copy_(self.length_out + 1)
             self.rows_used = self.budget
-        return self.norm(self.x) @ self.head.t()
 
 
 def main(argv=None):
