@@ -619,7 +619,7 @@ typedef struct sherry_attend_desc {
   const void* q;         /* device, [batch][heads][head_dim] of type, 16-byte */
                          /* aligned; query head i reads key-value head i /    */
                          /* (heads / kv_heads)                                */
-  void* out;             /* device, as q                                      */
+  void* out;             /* device, as q; may not overlap it                  */
   const int32_t* length; /* device, int32 [batch]: rows of each sequence      */
                          /* (below 0: none; past the table: all of it)        */
   const uint8_t* mask;   /* device, [batch][mask_stride], or NULL: rows with  */
@@ -650,7 +650,8 @@ typedef struct sherry_attend_desc {
 size_t sherry_cache_attend_workspace(const sherry_cache_desc* cache,
                                      const sherry_attend_desc* args);
 
-/* out = sum_r p_r v_r, p = softmax over the rows left in of scale * q . k_r; a
+/* Attention needs batch * table_width * page_size < 2^36 (SHERRY_E_SHAPE).
+ * out = sum_r p_r v_r, p = softmax over the rows left in of scale * q . k_r; a
  * token with no row left in (or only scores of -infinity) gives 0.  Rows left
  * out never reach the result, whatever they hold; a NaN or an infinity in the
  * others makes the results that it enters NaN or infinite.  Scores, statistics and

@@ -51,7 +51,9 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr int kWaves = 4;
 constexpr int kMinTiles = kWaves;  // tiles of the shortest run: one per wave
 // Up to this many tiles of capacity a workgroup takes a sequence whole, and
-// nothing is left to join: WHOLEUS
+// nothing is left to join (one sequence of 300 rows of 8 heads: 64 values 7.3 us
+// against 6.3 and 3.0 for the join, 128 values 10.7 against 8.6 and 3.4; of 600
+// rows 14.4 against 8.6 and 3.4, so no further).
 constexpr int kWholeTiles = 16;
 constexpr int kCus = 256;
 constexpr int kTile = 32;          // rows per wave and step
@@ -231,9 +233,10 @@ __device__ __forceinline__ float sum_over_blocks(float v) {
 }
 
 // Waves per SIMD, and workgroups per CU, that the registers allow without
-// spilling (more of them, spilling, were slower throughout: 16 sequences of 4000
-// to 8000 rows of 64 values 32 us with three, 39 with four; tiles of 64 rows
-// 34 .. 43).
+// spilling: 96 to 128 KB of loads per CU are then in flight.  More waves, spilling,
+// were slower (16 sequences of 4000 to 8000 rows of 64 values: 32 us with three,
+// 39 with four; 4 of 130000 rows of 128 values: 319 with two, 360 with three), and
+// so were tiles of 64 rows (34 to 43 us, 341).
 __host__ __device__ constexpr int waves_for(int dp) { return dp == 64 ? 3 : dp == 128 ? 2 : 1; }
 
 // CT: cache type; NT: terms of q and p; DP: head_dim rounded up to 64, 128 or
@@ -661,7 +664,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
       if constexpr (G::I8) {
         float big = 0.0f;  // of the tile's V scales
 #pragma unroll
-        for (int i = 0; i < 8; ++i) big = fmaxf(big, vsc[i]);
+        for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(vsc[i]));
         big = max_over_blocks(big);
         const int e = static_cast<int>(__float_as_uint(big) >> 23) - 127;
         vt = e > ve ? (e < 127 ? e : 127) : ve;

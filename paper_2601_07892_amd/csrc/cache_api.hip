@@ -84,6 +84,8 @@ int check_attend_shape(const sherry_cache_desc* c, const sherry_attend_desc* a) 
   if ((a->mask && a->mask_stride < cache_rows(c)) ||
       ((a->position || a->weight) && a->row_stride < cache_rows(c)))
     return SHERRY_E_SHAPE;
+  // (all rows in tiles of 32, and a few more per sequence, are counted in 32 bits)
+  if (int64_t(c->batch) * (ceil_div(cache_rows(c), 32) + 16) > INT32_MAX) return SHERRY_E_SHAPE;
   // (the joining launch: one workgroup per sequence and head, and for weight one
   // per sequence, key-value head and 1024 rows)
   if (int64_t(c->batch) * (a->heads + c->kv_heads * ceil_div(cache_rows(c), 1024)) > INT32_MAX)

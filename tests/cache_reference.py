@@ -65,14 +65,14 @@ class Cache:
 
     def rows64(self, name, b, h, n):
         """float64 [n][dim] of the first n rows (absent pages: NaN)."""
-        v = self.view(name)
-        out = np.full((n, self.dim), np.nan)
-        for r in range(n):
-            p = self.table[b, r // self.page]
-            if 0 <= p < self.pages:
-                x = v[p, h, r % self.page].double().numpy()
-                out[r] = x if self.scale[name] is None else x * float(self.scale[name][p, h, r % self.page])
-        return out
+        pages = self.table[b, :-(-n // self.page)].astype(np.int64)
+        there = (pages >= 0) & (pages < self.pages)
+        at = torch.from_numpy(np.where(there, pages, 0))
+        x = self.view(name)[at, h].double().numpy()
+        if self.scale[name] is not None:
+            x = x * self.scale[name][at.numpy(), h].astype(np.float64)[..., None]
+        x[~there] = np.nan
+        return x.reshape(-1, self.dim)[:n]
 
 
 def attend64(c, q, lens, scale, window=0, mask=None, position=None, q_pos=None):
@@ -84,9 +84,8 @@ def attend64(c, q, lens, scale, window=0, mask=None, position=None, q_pos=None):
     for b in range(batch):
         n = max(0, min(int(lens[b]), c.rows))
         for h in range(c.kv):
-            use = np.ones(n, bool)
-            for r in range(n):
-                use[r] &= 0 <= c.table[b, r // c.page] < c.pages
+            pages = c.table[b].astype(np.int64)
+            use = np.repeat((pages >= 0) & (pages < c.pages), c.page)[:n]
             if window and position is not None:
                 use &= position[b, h, :n].astype(np.int64) > int(q_pos[b]) - window
             elif window:

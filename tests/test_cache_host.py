@@ -94,6 +94,14 @@ def test_attend_refused(kw, status):
     assert L.sherry_cache_attend(_cache(), _attend(**kw), None) == status
 
 
+def test_attend_rows_refused():
+    """More rows in all than are counted."""
+    c = _cache(batch=128, page_size=1 << 20, table_width=1 << 10)
+    assert L.sherry_cache_attend(c, _attend(), None) == S
+    assert L.sherry_cache_attend_workspace(c, _attend()) == 0
+    assert sh.sherry_cache_attend_workspace(_cache(batch=32, page_size=1 << 20, table_width=1 << 10), _attend()) > 0
+
+
 def test_attend_workspace():
     """Grows with the splits and, for weight, with the scores; exactly that much
     is enough for the call (one byte less is refused)."""

@@ -190,6 +190,20 @@ def test_attend_window_edges(dev, ref, window):
     Attend(dev, ref, c, q, "f32", lens, window).check(ref)
 
 
+def test_attend_int8_scales_of_any_size(dev, ref):
+    """V scales that rise and fall by powers of ten from row to row, zeros and
+    negative ones among them; K scales that make some rows dominate."""
+    rng = np.random.default_rng(14)
+    lens = [700, 90, 33]
+    c = ref.Cache(rng, 3, 44, 2, 16, 64, "i8")
+    c.scale["v"] = (10.0 ** rng.uniform(-12, 12, c.scale["v"].shape)).astype(np.float32)
+    c.scale["v"][rng.random(c.scale["v"].shape) < 0.1] = 0
+    c.scale["v"][rng.random(c.scale["v"].shape) < 0.3] *= -1
+    c.scale["k"][rng.random(c.scale["k"].shape) < 0.1] *= 10
+    q = rng.standard_normal((3, 8, 64)).astype(np.float32)
+    Attend(dev, ref, c, q, "f32", lens).check(ref)
+
+
 @pytest.mark.parametrize("page", [16, 10])
 @pytest.mark.parametrize("cache", ["bf16", "i8"])
 def test_attend_absent_pages_and_wrong_lengths(dev, ref, page, cache):
@@ -258,6 +272,24 @@ def test_attend_long_and_many(dev, ref):
     c = ref.Cache(rng, 150, 6, 2, 16, 64, "bf16", None)
     q = rng.standard_normal((150, 4, 64)).astype(np.float32)
     Attend(dev, ref, c, q, "f32", lens, weight=np.zeros((150, 2, c.rows), np.float32)).check(ref)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_attend_any_lengths(dev, ref, seed):
+    """Random batches: which workgroups take which parts of which sequences
+    follows from the lengths alone."""
+    rng = np.random.default_rng(1000 + seed)
+    batch, kv, group = int(rng.integers(1, 200)), int(rng.choice([1, 2, 3, 40])), int(rng.choice([1, 2, 5]))
+    top = int(rng.choice([40, 600, 3000]) / (4 if kv == 40 else 1))
+    lens = np.where(rng.random(batch) < 0.3, 0, np.exp(rng.random(batch) * np.log(top + 1)).astype(int))
+    lens[rng.integers(0, batch)] = top
+    page = int(rng.choice([16, 32, 11]))
+    c = ref.Cache(rng, batch, -(-top // page), kv, page, int(rng.choice([16, 96, 144])),
+                  str(rng.choice(["bf16", "f16", "i8"])))
+    q = rng.standard_normal((batch, kv * group, c.dim)).astype(np.float32)
+    _case("attend any", seed, batch, kv, group, top, page, c.dim, c.kind)
+    weight = np.zeros((batch, kv, c.rows), np.float32) if seed % 3 == 0 else None
+    Attend(dev, ref, c, q, "f32", lens, int(rng.choice([0, 0, 100])), weight=weight).check(ref)
 
 
 def test_attend_offsets_past_32_bits(dev, ref):
