@@ -11,6 +11,13 @@
 //
 // What bounds it: the rows that move are read and written once, the weights
 // and positions read; below some thousand rows the two launches.
+//
+// Measured: 16 sequences of 1000 to 16384 rows cut to 4096, 8 heads of 128 f16
+// values: select 20 us, most of it the longest sequence's passes over the keys in
+// registers and LDS (a workgroup per sequence and head; several would need a
+// launch between the passes); move 38 us for 150 MB read and written, 4.0 TB/s,
+// where a copy reaches 4.9.  8 sequences of 2304 rows of 64 values cut to 2048:
+// 7.4 and 5.5 us.
 #include "cache_internal.h"
 
 namespace sherry {
@@ -60,6 +67,8 @@ __device__ __forceinline__ int waves_before(int v, int* part, int& total) {
 
 // Each wave takes a run of slots, in chunks of 64, and keeps their keys: J per
 // lane, for sequences of up to 1024 J rows; J = 0 reads them again in every pass.
+// Sequences of 2304 rows: 7.4 us with J = 4, 15.7 with 64, 14.6 with 0; of up to
+// 16384 20 with 16, 27 with 64, 29 with 0; of 60000 63 with 64, of 100000 145 with 0.
 template <int J>
 struct Run {
   const Keys& keys;
@@ -277,7 +286,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(Evict a) {
   }
 }
 
-constexpr int kMoveAt = 4;  // rows in flight per thread
+constexpr int kMoveAt = 4;  // rows in flight per thread (2 and 8: the same 37 to 39 us)
 
 // LPR lanes of 16 bytes per row (rows of 8 bytes do not exist: head_dim is a
 // multiple of 8, of 16 in int8), 256 / LPR * kMoveAt new rows per workgroup.

@@ -544,7 +544,9 @@ __device__ __forceinline__ void gemv_block(const uint8_t* w_, const X& xsrc, Pre
     swo[j] = (ws.rows && t < tpb * M * 64 && r0 < R && row0 < n) ? as_global(ws.rows)[row0]
                                                                   : ws.tensor;
   }
-  // and so is what an epilogue reads
+  // and so is what an epilogue reads (8192 x 2048, one token in fp32, silu and
+  // gate: 5.0 us, 2.7 MB; what bounds it is the row's quantization and the wait for
+  // the first unit, as without an epilogue)
   EpiValues ev[E::kUse ? kOut : 1];
   if constexpr (E::kUse) {
 #pragma unroll
