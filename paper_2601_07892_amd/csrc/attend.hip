@@ -29,13 +29,17 @@
 //    eight rows into the V^T operands.  The sums have query head l % 16 in lane
 //    l again, so the running maximum rescales them lane by lane.
 //
-// Precision.  Cached values are exact in the operands (int8 rows as f16
-// integers, their scales applied to the scores and the probabilities).  q and
-// p are split into terms of bf16 (or, for f16 and int8 caches, f16) whose
-// products are summed in fp32: three bf16 terms hold all 24 bits, two 16; two
-// f16 terms 22 (q is scaled by a power of two per head, p by 2^14 over the
-// largest scale of V so far, so that their low terms stay normal).  fp32 inputs
-// take three and two, 16-bit inputs two.
+// Precision.  Cached values are exact in the operands (rows of int8 K as they
+// are, of V as f16 integers; their scales are applied to the scores and the
+// probabilities).  q and p are split into terms of bf16 (or, for f16 caches and p
+// over int8 V, f16) whose products are summed in fp32: three bf16 terms hold all 24
+// bits, two 16; two f16 terms 22 (p is scaled by 2^14 over the largest scale of V
+// so far, so that its low term stays normal).  fp32 inputs take three and two,
+// 16-bit inputs two.  Over int8 K q is three int8 digits, rounded at 2^-22 of its
+// head's power of two, and their products are summed as integers (two f16 terms
+// against K converted to f16 took 71 us instead of 64 for 64 sequences of 4000
+// rows of 64 values, 119 instead of 100 for 256, 112 instead of 110 for 128).  q is
+// scaled by that power of two over every cache.
 //
 // Measured (kernel trace; a streaming read of 2 GiB reaches 7.05 TB/s):
 //  * 4 sequences of 130000 rows, 32 query heads over 8 of 128 bf16 values, 2.13
@@ -44,9 +48,10 @@
 //    27 us and 4.6.  Sequences of one length of the same bytes take 23; the rest is
 //    those that begin and end inside a run.
 //  * 16 sequences of 2000 to 9000 rows, 32 heads over 8 of 128 int8 values, a
-//    window, a mask and weights: 43 us and 7.1.  2.9 times the vector instructions
-//    of the case before (conversions, scales, masks, stored scores), which bound
-//    it: a cache of the same type without them, 64 sequences of 4000 rows, 5.2 TB/s.
+//    window, a mask and weights: 43 us and 7.1, without the three 35.  Some 10 us are
+//    a workgroup's beginning and end; conversions of V, scales, masks and stored
+//    scores make more than twice the vector instructions per byte of the case before.
+//    64 sequences of 4000 rows, 0.54 GB, without them: 100 to 104 us, 5.3 TB/s.
 //  * one sequence of 300 rows: 7.0 us in one launch, all of it latency (length, table,
 //    K, V, and the waves' sums, each after the other).
 #include <type_traits>
@@ -56,6 +61,7 @@
 namespace sherry {
 namespace {
 
+typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
@@ -170,6 +176,10 @@ __device__ __forceinline__ v4f mfma(const u32x4& a, const u32x4& b, const v4f& c
                                                    __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
 }
 
+__device__ __forceinline__ v4i mfma_i8(const u32x4& a, const u32x4& b, const v4i& c) {
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, a), __builtin_bit_cast(v4i, b), c, 0, 0, 0);
+}
+
 // The upper (bf16: value) halves of two words.
 __device__ __forceinline__ uint32_t upper(uint32_t hi, uint32_t lo) {
   return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
@@ -210,21 +220,10 @@ __device__ __forceinline__ void split(const float (&x)[8], u32x4 (&t)[NT]) {
     }
 }
 
-// Pairs of int8 as f16 (exact).  With its sign bit flipped a byte is u = x +
-// 128.  K: below a byte 0x64 it is the low byte of the f16 value 1024 + u.
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ u32x4 bytes_f16(uint32_t w0, uint32_t w1) {
-  u32x4 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t w = (i < 2 ? w0 : w1) ^ 0x80808080u;
-    const uint32_t pair = __builtin_amdgcn_perm(0x64646464u, w, i & 1 ? 0x04030402u : 0x04010400u);
-    r[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, pair) - v2h{1152, 1152});
-  }
-  return r;
-}
-// V: byte i of lo and of hi (sign bits flipped) as the f16 values x 2^-9: u alone
-// is the subnormal u 2^-24, and u 2^-24 * 2^15 - 128 * 2^-9 is one operation.
+// int8 V: byte i of lo and of hi, x + 128 = u with its sign bit flipped, as the f16
+// values x 2^-9 (exact): u alone is the subnormal u 2^-24, and u 2^-24 * 2^15 -
+// 128 * 2^-9 is one operation.
 constexpr int kByteDown = 9;
 template <int i>
 __device__ __forceinline__ uint32_t byte_pair_f16(uint32_t hi, uint32_t lo) {
@@ -240,6 +239,12 @@ __device__ __forceinline__ float max_over_blocks(float v) {
   v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
   const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ uint32_t max_over_blocks(uint32_t v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  v = a[0] > a[1] ? a[0] : a[1];
+  const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return b[0] > b[1] ? b[0] : b[1];
 }
 __device__ __forceinline__ float sum_over_blocks(float v) {
   v += __shfl_xor(v, 16, 64);
@@ -272,6 +277,12 @@ struct Cfg {
   static constexpr int CH = DP / 16;           // values per lane and row of V
   static constexpr int VW = CH * E / 4;        // as words
   static constexpr int VP = VW > 4 ? 2 : 1;    // pieces (of 8 values) they are read in
+  static constexpr int QT = I8 ? 3 : NT;       // terms of q
+  static constexpr int QS = I8 ? KL : KS;      // and MFMA steps of their operands
+  // Tiles in flight per wave: int8 rows are half as many bytes, and leave the
+  // registers for two (64 sequences of 4000 rows 100 us against 110 with 128 values,
+  // 59 against 64 with 64, 95 against 100 with 256; with a mask 102 against 111).
+  static constexpr int DEEP = I8 && !ANY ? 2 : 1;
 };
 
 // d of value j of MFMA step s in the lanes of block g.
@@ -377,7 +388,8 @@ struct Rows {
             4 * l, 0, 0);
     }
   }
-  __device__ __forceinline__ void finish(int tile) {
+  // (not on: a tile of no rows)
+  __device__ __forceinline__ void finish(int tile, bool on) {
     const int p0 = tile * kTile;
     bool ok = next_on;
     if constexpr (G::MORE) {
@@ -394,7 +406,7 @@ struct Rows {
       // (scalar: the rows from begin to end, and of pages that exist)
       const uint32_t from = begin > p0 ? ~0u << (begin - p0) : ~0u;
       const uint32_t to = end - p0 < kTile ? (1u << (end - p0)) - 1 : ~0u;
-      valid = from & to;
+      valid = on ? from & to : 0;
       if constexpr (G::MORE) valid &= static_cast<uint32_t>(__ballot(ok));
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -524,10 +536,10 @@ __device__ __forceinline__ void load_q(const Attend& a, int b, int head0, int he
 // The same in terms, and the factor of its scores in units of ln 2.
 template <class G>
 __device__ __forceinline__ float split_q(const Attend& a, const u32x4 (&raw)[G::KS][2],
-                                         u32x4 (&qf)[G::NT][G::KS]) {
+                                         u32x4 (&qf)[G::QT][G::QS]) {
   float factor = a.scale * kLog2e;
   float q[G::KS][8];
-  float top = 0.0f;
+  uint32_t most = 0;  // the largest magnitude's bits (of a NaN the most)
 #pragma unroll
   for (int s = 0; s < G::KS; ++s)
 #pragma unroll
@@ -538,26 +550,49 @@ __device__ __forceinline__ float split_q(const Attend& a, const u32x4 (&raw)[G::
         const uint16_t x = static_cast<uint16_t>(raw[s][0][i >> 1] >> (16 * (i & 1)));
         q[s][i] = a.type == SHERRY_BF16 ? from_bf16(x) : from_f16(x);
       }
-      top = fmaxf(top, fabsf(q[s][i]));
+      const uint32_t bits = __float_as_uint(q[s][i]) & 0x7FFFFFFFu;
+      most = bits > most ? bits : most;
     }
-  if constexpr (G::F16) {
-    // q / 2^e in [-2, 2): exact, and far from f16's limits
-    top = max_over_blocks(top);
-    const int e = (__float_as_uint(top) >> 23) & 255;
-    const bool use = e > 0 && e < 254;
-    const float down = use ? __uint_as_float(static_cast<uint32_t>(254 - e) << 23) : 1.0f;
-    factor *= use ? __uint_as_float(static_cast<uint32_t>(e) << 23) : 1.0f;
+  // q / 2^e in [-2, 2): exact, and far from the terms' and the scores' limits
+  most = max_over_blocks(most);
+  constexpr uint32_t kTiny = 0x00400000u;  // 2^-127
+  const uint32_t e = most >> 23 < 254 ? most >> 23 : 254;
+  const float down = __uint_as_float(e < 254 ? (254 - e) << 23 : kTiny);
+  factor *= __uint_as_float(e > 0 ? e << 23 : kTiny);
 #pragma unroll
-    for (int s = 0; s < G::KS; ++s)
+  for (int s = 0; s < G::KS; ++s)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) q[s][i] *= down;
-  }
+    for (int i = 0; i < 8; ++i) q[s][i] *= down;
+  if constexpr (G::I8) {
+    // as integers over 2^21, in three signed digits of base 256: the bytes of
+    // their sum with 128 in every place, less 128
+    factor *= most < 0x7F800000u ? 0x1p-21f : __uint_as_float(0x7FC00000u);  // (not finite: NaN)
 #pragma unroll
-  for (int s = 0; s < G::KS; ++s) {
-    u32x4 t[G::NT];
-    split<G::F16, G::NT>(q[s], t);
+    for (int s = 0; s < G::QS; ++s)
 #pragma unroll
-    for (int i = 0; i < G::NT; ++i) qf[i][s] = t[i];
+      for (int w = 0; w < 4; ++w) {
+        uint32_t u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)  // rounded in the last place of a float of 2^23
+          u[i] = __float_as_uint(__builtin_fmaf(q[2 * s + (w >> 1)][4 * (w & 1) + i], 0x1p21f, 0x1.8p23f)) -
+                 0x4B400000u + 0x00808080u;
+        // bytes 0 and 1 of each pair, then byte by byte
+        const uint32_t a01 = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u);
+        const uint32_t a23 = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);
+        const uint32_t b01 = __builtin_amdgcn_perm(u[1], u[0], 0x0C0C0602u);
+        const uint32_t b23 = __builtin_amdgcn_perm(u[3], u[2], 0x0C0C0602u);
+        qf[2][s][w] = lower(a23, a01) ^ 0x80808080u;
+        qf[1][s][w] = upper(a23, a01) ^ 0x80808080u;
+        qf[0][s][w] = lower(b23, b01) ^ 0x80808080u;
+      }
+  } else {
+#pragma unroll
+    for (int s = 0; s < G::KS; ++s) {
+      u32x4 t[G::NT];
+      split<G::F16, G::NT>(q[s], t);
+#pragma unroll
+      for (int i = 0; i < G::NT; ++i) qf[i][s] = t[i];
+    }
   }
   return factor;
 }
@@ -599,7 +634,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
     const int t0 = begin / kTile + n0, t1 = begin / kTile + n1;
 
     // q first, then the first tile's rows, so that their latencies overlap
-    u32x4 qraw[G::KS][2], qf[NT][G::KS];
+    u32x4 qraw[G::KS][2], qf[G::QT][G::QS];
     load_q<G>(a, b, head0, heads, qraw);
     Rows<G> rows(a, b, h, begin, end);
     float* score = nullptr;  // of this lane's head, and its rows of a tile
@@ -613,50 +648,85 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
     // int8: V's scales are held over 2^ve, the largest of them so far
     int ve = -126;
 
-    uint32_t kr[2][G::KL * 4], vr[8][G::VW];
-    float ksc[8], vsc[8];
-    int tile = t0 + wave;
-    if (tile < t1) {
-      rows.start(tile);
-      rows.finish(tile);
-      rows.load_k(kr);
-      if constexpr (G::I8) rows.load_scales(a.c.ks, ksc);
-      rows.load_v(vr);
-      if constexpr (G::I8) rows.load_scales(a.c.vs, vsc);
-      if (tile + kWaves < t1) rows.start(tile + kWaves);
+    // Tile i's rows are read into slot i % D while those of the D tiles before it
+    // are used.  With D > 1 every load goes out (past t1 of no rows), so that a
+    // wait counts the same loads on every path.
+    constexpr int D = G::DEEP;
+    uint32_t kr[D][2][G::KL * 4], vr[D][8][G::VW], valids[D];
+    float kscs[D][8], vscs[D][8];
+    bool hole[D];
+    const int mine_first = t0 + wave;
+    auto inside = [&](int i) { return D == 1 || i < t1 ? i : mine_first; };
+    auto start = [&](int i) {
+      if (D > 1 || i < t1) rows.start(inside(i));
+    };
+    auto fetch_k = [&](auto slot, int i) {
+      constexpr int u = decltype(slot)::value;
+      rows.finish(inside(i), D == 1 || i < t1);
+      valids[u] = rows.valid;
+      hole[u] = !G::I8 && !G::ANY && rows.holes();
+      start(i + kWaves);
+      rows.load_k(kr[u]);
+      if constexpr (G::I8) rows.load_scales(a.c.ks, kscs[u]);
+    };
+    auto fetch_v = [&](auto slot) {
+      constexpr int u = decltype(slot)::value;
+      rows.load_v(vr[u]);
+      if constexpr (G::I8) rows.load_scales(a.c.vs, vscs[u]);
+    };
+    if (mine_first < t1) {
+      rows.start(mine_first);
+      for_each([&](auto slot) {
+        fetch_k(slot, mine_first + decltype(slot)::value * kWaves);
+        fetch_v(slot);
+      }, std::make_integer_sequence<int, D>{});
     }
     const float factor = split_q<G>(a, qraw, qf);
-    for (; tile < t1; tile += kWaves) {
-      const uint32_t valid = rows.valid;
-      const bool holes = !G::I8 && !G::ANY && rows.holes();
-      const int next = tile + kWaves;
-      v4f s[2];
+    auto step = [&](auto slot, int tile) {
+      constexpr int u = decltype(slot)::value;
+      auto& k = kr[u];
+      auto& v = vr[u];
+      float(&ksc)[8] = kscs[u];
+      float(&vsc)[8] = vscs[u];
+      const uint32_t valid = valids[u];
+      const bool holes = hole[u];
+      const int next = tile + D * kWaves;
+      const bool more = D > 1 || next < t1;
+      float x[8];
+      if constexpr (G::I8) {
+        // K's bytes as they lie, a product per digit of q: exact, up to 2^22
+        v4i s[3][2] = {};
 #pragma unroll
-      for (int t = 0; t < 2; ++t) s[t] = v4f{0, 0, 0, 0};
+        for (int st = 0; st < G::QS; ++st)
 #pragma unroll
-      for (int st = 0; st < G::KS; ++st)
+          for (int t = 0; t < 2; ++t) {
+            u32x4 kf;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          u32x4 kf;
-          if constexpr (G::I8) {
-            kf = bytes_f16(kr[t][2 * st], kr[t][2 * st + 1]);
-          } else {
+            for (int i = 0; i < 4; ++i) kf[i] = k[t][4 * st + i];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) kf[i] = kr[t][4 * st + i];
+            for (int i = 0; i < 3; ++i) s[i][t] = mfma_i8(kf, qf[i][st], s[i][t]);
           }
 #pragma unroll
-          for (int i = NT - 1; i >= 0; --i) s[t] = mfma<G::F16>(kf, qf[i][st], s[t]);
+        for (int i = 0; i < 8; ++i) {
+          auto digit = [&](int d) { return static_cast<float>(s[d][i >> 2][i & 3]); };
+          x[i] = __builtin_fmaf(__builtin_fmaf(digit(0), 256.0f, digit(1)), 256.0f, digit(2)) * (factor * ksc[i]);
         }
-      float x[8];
+      } else {
+        v4f s[2] = {};
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        x[i] = s[i >> 2][i & 3] * (G::I8 ? factor * ksc[i] : factor);
-      if (next < t1) {
-        rows.finish(next);
-        rows.load_k(kr);
-        if constexpr (G::I8) rows.load_scales(a.c.ks, ksc);
-        if (next + kWaves < t1) rows.start(next + kWaves);
+        for (int st = 0; st < G::KS; ++st)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            u32x4 kf;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) kf[i] = k[t][4 * st + i];
+#pragma unroll
+            for (int i = NT - 1; i >= 0; --i) s[t] = mfma<G::F16>(kf, qf[i][st], s[t]);
+          }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3] * factor;
       }
+      if (more) fetch_k(slot, next);
       uint32_t mine = 0xFF;  // bit i: row of x[i] is attended to
       if (valid != 0xFFFFFFFFu) {
         mine = ((valid >> (4 * g)) & 0xF) | (((valid >> (16 + 4 * g)) & 0xF) << 4);
@@ -702,7 +772,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int i = 0; i < G::VW; ++i) vr[j][i] = (mine >> j) & 1 ? vr[j][i] : 0;
+          for (int i = 0; i < G::VW; ++i) v[j][i] = (mine >> j) & 1 ? v[j][i] : 0;
       }
       const float low = base - kUp, vdown = G::I8 ? ldexpf(1.0f, -ve) : 1.0f;
       float p[8];
@@ -718,7 +788,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int i = 0; i < G::VW; ++i) vr[j][i] ^= 0x80808080u;
+          for (int i = 0; i < G::VW; ++i) v[j][i] ^= 0x80808080u;
       }
       auto value = [&](auto ec) {
         constexpr int e = decltype(ec)::value;
@@ -726,23 +796,28 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if constexpr (G::I8)
-            vf[i] = byte_pair_f16<e & 3>(vr[2 * i + 1][e >> 2], vr[2 * i][e >> 2]);
+            vf[i] = byte_pair_f16<e & 3>(v[2 * i + 1][e >> 2], v[2 * i][e >> 2]);
           else
-            vf[i] = e & 1 ? upper(vr[2 * i + 1][e >> 1], vr[2 * i][e >> 1])
-                          : lower(vr[2 * i + 1][e >> 1], vr[2 * i][e >> 1]);
+            vf[i] = e & 1 ? upper(v[2 * i + 1][e >> 1], v[2 * i][e >> 1])
+                          : lower(v[2 * i + 1][e >> 1], v[2 * i][e >> 1]);
         }
 #pragma unroll
         for (int i = NT - 1; i >= 0; --i) o[e] = mfma<G::F16>(vf, pf[i], o[e]);
       };
       for_each(value, std::make_integer_sequence<int, G::CH>{});
-      if (next < t1) {
-        rows.load_v(vr);
-        if constexpr (G::I8) rows.load_scales(a.c.vs, vsc);
+      if (more) fetch_v(slot);
+    };
+    for (int tile = mine_first; tile < t1; tile += D * kWaves) {
+      step(std::integral_constant<int, 0>{}, tile);
+      if constexpr (D > 1) {
+        if (tile + kWaves >= t1) break;
+        step(std::integral_constant<int, 1>{}, tile + kWaves);
       }
     }
 
     // the four waves' sums at their common maximum
     l = sum_over_blocks(l);
+    if (m == kMinusInf && l != l) m = 0.0f;  // scores of NaN alone, which have no maximum
     if (g == 0) stat[wave][n] = make_float2(m, l);
     __syncthreads();
     float top = kMinusInf;

@@ -259,6 +259,46 @@ def test_attend_values_that_are_not_finite(dev, ref):
     assert np.all(np.isfinite(rest)) and np.all(np.isfinite(got[2]))
 
 
+@pytest.mark.parametrize("lens", [[33, 1, 40], [1025, 2000, 4097]])
+@pytest.mark.parametrize("cache", ["i8", "f16", "bf16"])
+def test_attend_nan_alone_in_its_tile(dev, ref, cache, lens):
+    """A NaN in the last row, which no other row shares a tile with."""
+    rng = np.random.default_rng(16)
+    c = ref.Cache(rng, 3, max(lens) // 16 + 1, 2, 16, 64, cache)
+    for b in (0, 1):
+        r = lens[b] - 1
+        page = int(c.table[b, r // 16])
+        if cache == "i8":
+            c.scale["k"][page, 1, r % 16] = np.nan
+        else:
+            c.view("k")[page, 1, r % 16, 9] = float("nan")
+    got = Attend(dev, ref, c, rng.standard_normal((3, 4, 64)).astype(np.float32), "f32", lens).run()
+    assert np.all(np.isnan(got[:2, 2:]))
+    assert np.all(np.isfinite(got[:2, :2])) and np.all(np.isfinite(got[2]))
+
+
+@pytest.mark.parametrize("cache", ["i8", "f16", "bf16"])
+def test_attend_q_of_any_size(dev, ref, cache):
+    """Heads whose q are near the ends of fp32, or zero, with a scale that makes
+    ordinary scores of them; a NaN or an infinity in q is its head's alone."""
+    rng = np.random.default_rng(15)
+    lens = [200, 33, 1]
+    c = ref.Cache(rng, 3, 13, 2, 16, 128, cache)
+    q = rng.standard_normal((3, 8, 128)).astype(np.float32)
+    q[:, 3] = 0
+    q[1, 2] /= 100
+    top = np.float32(3.4e38 / np.abs(q).max())
+    for by in (top, np.float32(2.0 ** 100), np.float32(2.0 ** -100)):
+        Attend(dev, ref, c, q * by, "f32", lens, scale=0.0884 / float(by)).check(ref)
+    q[0, 1, 17] = float("nan")
+    q[1, 6, 127] = float("inf")
+    q[2, 0, 0] = float("-inf")
+    got = Attend(dev, ref, c, q, "f32", lens).run()
+    for b, head in ((0, 1), (1, 6), (2, 0)):
+        assert not np.any(np.isfinite(got[b, head]))
+        assert np.all(np.isfinite(np.delete(got[b], head, axis=0)))
+
+
 def test_attend_long_and_many(dev, ref):
     """A long sequence beside short ones (many splits of one), and more
     sequences than one wave counts."""
