@@ -263,9 +263,10 @@ __host__ __device__ constexpr int waves_for(int dp) { return dp == 64 ? 3 : dp =
 // lies in one page and its rows are read through one buffer resource).
 // MORE: mask, position or weight are given.
 // What each buys, against the general form on the same input: pages of multiples of
-// 16 rows 322 us against 356 (4 sequences of 130000 rows), 26.8 against 29.6 (32
-// short ones); no mask, position or weight 26.8 against 29.0, 7.0 against 7.9 (one
-// sequence of 300 rows).
+// 16 rows 7.3 us against 8.4 (one sequence of 300 rows), 320 against 327 (4 of
+// 130000), 61 against 70 (16 of 4000 to 8000, 256 values), 65 against 95 (64 of
+// 4000, int8, 64 values); no mask, position or weight 26.8 against 29.0 (32 short
+// ones), 7.0 against 7.9 (the one of 300 rows).
 template <int CT_, int NT_, int DP_, bool ANY_, bool MORE_>
 struct Cfg {
   static constexpr int CT = CT_, NT = NT_, DP = DP_;
@@ -296,6 +297,9 @@ __device__ __forceinline__ int v_dim(int n, int e) {
   return G::VP == 2 ? 128 * (e >> 3) + 8 * n + (e & 7) : G::CH * n + e;
 }
 
+// (Loads of K and V stream: each line is used once.  Left in the caches they took
+// 354 us instead of 320 for 4 sequences of 130000 rows, 29.7 instead of 27.3 for the
+// 32 short ones; with pages of 20 rows 66 instead of 61.)
 template <int W>
 __device__ __forceinline__ void buffer_words(uint32_t* to, __amdgpu_buffer_rsrc_t r, int off) {
   if constexpr (W == 4) {
@@ -316,15 +320,15 @@ __device__ __forceinline__ void global_words(uint32_t* to, const char* p, bool i
   for (int i = 0; i < W; ++i) to[i] = 0;
   if (!in) return;
   if constexpr (W == 4) {
-    const u32x4 v = *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(p));
+    const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(p)));
 #pragma unroll
     for (int i = 0; i < 4; ++i) to[i] = v[i];
   } else if constexpr (W == 2) {
-    const u32x2 v = *reinterpret_cast<const SHERRY_GLOBAL u32x2*>(as_global(p));
+    const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const SHERRY_GLOBAL u32x2*>(as_global(p)));
     to[0] = v[0];
     to[1] = v[1];
   } else {
-    to[0] = *reinterpret_cast<const SHERRY_GLOBAL uint32_t*>(as_global(p));
+    to[0] = __builtin_nontemporal_load(reinterpret_cast<const SHERRY_GLOBAL uint32_t*>(as_global(p)));
   }
 }
 
