@@ -655,9 +655,8 @@ size_t sherry_cache_attend_workspace(const sherry_cache_desc* cache,
  * token with no row left in (or only scores of -infinity) gives 0.  Rows left
  * out never reach the result, whatever they hold; a NaN or an infinity in the
  * others makes the results that it enters NaN or infinite.  Scores, statistics and
- * sums are in fp32; with fp32 q the products keep q and the probabilities to
- * 22 bits and more (over f16 and int8 caches of a head's largest value), else the
- * probabilities to 16. */
+ * sums are in fp32; the products keep q and the probabilities to 22 bits and more
+ * (over f16 and int8 caches of a head's largest value). */
 int sherry_cache_attend(const sherry_cache_desc* cache, const sherry_attend_desc* args,
                         void* stream);
 

@@ -34,8 +34,10 @@
 // probabilities).  q and p are split into terms of bf16 (or, for f16 caches and p
 // over int8 V, f16) whose products are summed in fp32: three bf16 terms hold all 24
 // bits, two 16; two f16 terms 22 (p is scaled by 2^14 over the largest scale of V
-// so far, so that its low term stays normal).  fp32 inputs take three and two,
-// 16-bit inputs two.  Over int8 K q is three int8 digits, rounded at 2^-22 of its
+// so far, so that its low term stays normal).  Over bf16 caches p takes three (with
+// two the outputs of bf16 q were 1e-5 off before their own rounding) and q as many
+// as hold it: one of bf16, two of f16, three of fp32.  Over f16 caches both take
+// two.  Over int8 K q is three int8 digits, rounded at 2^-22 of its
 // head's power of two, and their products are summed as integers (two f16 terms
 // against K converted to f16 took 71 us instead of 64 for 64 sequences of 4000
 // rows of 64 values, 119 instead of 100 for 256, 112 instead of 110 for 128).  q is
@@ -258,7 +260,7 @@ __device__ __forceinline__ float sum_over_blocks(float v) {
 // so were tiles of 64 rows (34 to 43 us, 341).
 __host__ __device__ constexpr int waves_for(int dp) { return dp == 64 ? 3 : dp == 128 ? 2 : 1; }
 
-// CT: cache type; NT: terms of q and p; DP: head_dim rounded up to 64, 128 or
+// CT: cache type; QT, NT: terms of q and of p; DP: head_dim rounded up to 64, 128 or
 // 256; ANY: pages of any size (else page_size % 16 == 0, so that a half tile
 // lies in one page and its rows are read through one buffer resource).
 // MORE: mask, position or weight are given.
@@ -267,9 +269,9 @@ __host__ __device__ constexpr int waves_for(int dp) { return dp == 64 ? 3 : dp =
 // 130000), 61 against 70 (16 of 4000 to 8000, 256 values), 65 against 95 (64 of
 // 4000, int8, 64 values); no mask, position or weight 26.8 against 29.0 (32 short
 // ones), 7.0 against 7.9 (the one of 300 rows).
-template <int CT_, int NT_, int DP_, bool ANY_, bool MORE_>
+template <int CT_, int QT_, int NT_, int DP_, bool ANY_, bool MORE_>
 struct Cfg {
-  static constexpr int CT = CT_, NT = NT_, DP = DP_;
+  static constexpr int CT = CT_, QT = QT_, NT = NT_, DP = DP_;
   static constexpr int EU = waves_for(DP);
   static constexpr bool ANY = ANY_, MORE = MORE_, F16 = CT != SHERRY_BF16, I8 = CT == SHERRY_I8;
   static constexpr int E = I8 ? 1 : 2;         // bytes per value
@@ -278,8 +280,7 @@ struct Cfg {
   static constexpr int CH = DP / 16;           // values per lane and row of V
   static constexpr int VW = CH * E / 4;        // as words
   static constexpr int VP = VW > 4 ? 2 : 1;    // pieces (of 8 values) they are read in
-  static constexpr int QT = I8 ? 3 : NT;       // terms of q
-  static constexpr int QS = I8 ? KL : KS;      // and MFMA steps of their operands
+  static constexpr int QS = I8 ? KL : KS;      // MFMA steps of q's operands
   // Tiles in flight per wave: int8 rows are half as many bytes, and leave the
   // registers for two (64 sequences of 4000 rows 100 us against 110 with 128 values,
   // 59 against 64 with 64, 95 against 100 with 256; with a mask 102 against 111).
@@ -592,10 +593,10 @@ __device__ __forceinline__ float split_q(const Attend& a, const u32x4 (&raw)[G::
   } else {
 #pragma unroll
     for (int s = 0; s < G::KS; ++s) {
-      u32x4 t[G::NT];
-      split<G::F16, G::NT>(q[s], t);
+      u32x4 t[G::QT];
+      split<G::F16, G::QT>(q[s], t);
 #pragma unroll
-      for (int i = 0; i < G::NT; ++i) qf[i][s] = t[i];
+      for (int i = 0; i < G::QT; ++i) qf[i][s] = t[i];
     }
   }
   return factor;
@@ -699,6 +700,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
       float x[8];
       if constexpr (G::I8) {
         // K's bytes as they lie, a product per digit of q: exact, up to 2^22
+        static_assert(G::QT == 3, "digits");
         v4i s[3][2] = {};
 #pragma unroll
         for (int st = 0; st < G::QS; ++st)
@@ -725,7 +727,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
 #pragma unroll
             for (int i = 0; i < 4; ++i) kf[i] = k[t][4 * st + i];
 #pragma unroll
-            for (int i = NT - 1; i >= 0; --i) s[t] = mfma<G::F16>(kf, qf[i][st], s[t]);
+            for (int i = G::QT - 1; i >= 0; --i) s[t] = mfma<G::F16>(kf, qf[i][st], s[t]);
           }
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3] * factor;
@@ -1008,18 +1010,18 @@ int launch_cfg(const Attend& a, hipStream_t s) {
   if (a.weight) blocks += int64_t(a.c.batch) * a.c.kv * ceil_div(a.c.rows, kWeightRows);
   return launch(attend_join_kernel<G::DP, G::F16>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
 }
-template <int CT, int NT, int DP>
+template <int CT, int QT, int NT, int DP>
 int launch_pages(const Attend& a, hipStream_t s) {
   const bool more = a.mask || a.position || a.weight;
   if (a.c.page_size % 16 == 0)
-    return more ? launch_cfg<Cfg<CT, NT, DP, false, true>>(a, s) : launch_cfg<Cfg<CT, NT, DP, false, false>>(a, s);
-  return more ? launch_cfg<Cfg<CT, NT, DP, true, true>>(a, s) : launch_cfg<Cfg<CT, NT, DP, true, false>>(a, s);
+    return more ? launch_cfg<Cfg<CT, QT, NT, DP, false, true>>(a, s) : launch_cfg<Cfg<CT, QT, NT, DP, false, false>>(a, s);
+  return more ? launch_cfg<Cfg<CT, QT, NT, DP, true, true>>(a, s) : launch_cfg<Cfg<CT, QT, NT, DP, true, false>>(a, s);
 }
-template <int CT, int NT>
+template <int CT, int QT, int NT>
 int launch_dim(const Attend& a, hipStream_t s) {
-  if (a.c.dim <= 64) return launch_pages<CT, NT, 64>(a, s);
-  if (a.c.dim <= 128) return launch_pages<CT, NT, 128>(a, s);
-  return launch_pages<CT, NT, 256>(a, s);
+  if (a.c.dim <= 64) return launch_pages<CT, QT, NT, 64>(a, s);
+  if (a.c.dim <= 128) return launch_pages<CT, QT, NT, 128>(a, s);
+  return launch_pages<CT, QT, NT, 256>(a, s);
 }
 
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
@@ -1073,11 +1075,12 @@ int launch_attend(const sherry_cache_desc& c, const sherry_attend_desc& d, hipSt
                  d.q_stride ? d.q_stride : row, d.out_stride ? d.out_stride : row, d.mask_stride,
                  d.row_stride, sh.score_stride, d.heads, sh.group, sh.gtiles, sh.gmax, d.type,
                  d.window, sh.columns, sh.whole, d.scale};
-  const bool f32 = d.type == SHERRY_F32;
-  switch (c.type) {
-    case SHERRY_F16: return launch_dim<SHERRY_F16, 2>(a, s);
-    case SHERRY_BF16: return f32 ? launch_dim<SHERRY_BF16, 3>(a, s) : launch_dim<SHERRY_BF16, 2>(a, s);
-    default: return launch_dim<SHERRY_I8, 2>(a, s);
+  if (c.type == SHERRY_F16) return launch_dim<SHERRY_F16, 2, 2>(a, s);
+  if (c.type == SHERRY_I8) return launch_dim<SHERRY_I8, 3, 2>(a, s);
+  switch (d.type) {
+    case SHERRY_F32: return launch_dim<SHERRY_BF16, 3, 3>(a, s);
+    case SHERRY_F16: return launch_dim<SHERRY_BF16, 2, 3>(a, s);
+    default: return launch_dim<SHERRY_BF16, 1, 3>(a, s);
   }
 }
 

@@ -138,3 +138,15 @@ def test_gpu_cases_reach_every_shape():
             if not all(g for _, _, _, g in shapes):
                 beside.add(v)
     assert got == {SHORT, PAIR, THIN} and with_groups == {SHORT, PAIR, HALF, MID} == beside
+
+
+def test_epilogue_cases_reach_every_shape():
+    """The shapes that the GPU cases of the products with an epilogue run."""
+    pytest.importorskip("torch")
+    import test_gpu_epilogue_shapes as epi
+    assert {v for v, in ask(*(("wide_pick",) + s for s in epi.LONE))} == {LONG, MID, HALF, QUARTER, SHORT, TINY}
+    pieces = [-(-k // 128) % 4 == 0 for _, _, k in epi.LONE_GROUP]
+    picks = ask(*(("wide_pick_group",) + s + (int(p),) for s, p in zip(epi.LONE_GROUP, pieces)))
+    assert {v for (v,), p in zip(picks, pieces) if not p} == {MID, HALF, PAIR, TINY}
+    assert {v for (v,), p in zip(picks, pieces) if p} >= {MID, HALF, SHORT}
+    assert {v for v, in picks} == {MID, HALF, SHORT, TINY, PAIR}
