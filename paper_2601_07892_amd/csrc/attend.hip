@@ -82,6 +82,7 @@ constexpr int kMaxGroup = 256;       // query heads per key-value head
 constexpr int kOutside = 0x7FFFFFF0;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kMinusInf = -__builtin_huge_valf();
+constexpr float kLowest = -3.40282347e38f;  // the least finite value
 
 struct Attend {
   Cache c;
@@ -96,7 +97,9 @@ struct Attend {
   int2* parts;   // [batch]: a sequence's first part and how many it has
   float2* stat;  // [part][y][gmax]: maximum (of scores in units of ln 2) and sum
   float* sums;   // [part][y][gmax][DP]
-  float* score;  // [batch][heads][score_stride], in units of ln 2 (weight only)
+  // [batch][heads][score_stride], in units of ln 2 (weight only): -infinity of rows
+  // that are left out, and of these alone (kLowest of attended ones)
+  float* score;
   int64_t q_stride, out_stride, mask_stride, row_stride, score_stride;
   int heads, group, gtiles, gmax, type, window, columns;
   bool whole;    // column w is sequence w
@@ -734,11 +737,17 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
       }
       if (more) fetch_k(slot, next);
       uint32_t mine = 0xFF;  // bit i: row of x[i] is attended to
+      float kept[8];         // the scores as they are stored
+      if constexpr (G::MORE) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) kept[i] = fmaxf(x[i], kLowest);  // (of a NaN its head's sum tells)
+      }
       if (valid != 0xFFFFFFFFu) {
         mine = ((valid >> (4 * g)) & 0xF) | (((valid >> (16 + 4 * g)) & 0xF) << 4);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           x[i] = (mine >> i) & 1 ? x[i] : kMinusInf;
+          if constexpr (G::MORE) kept[i] = (mine >> i) & 1 ? kept[i] : kMinusInf;
           if constexpr (G::I8) vsc[i] = (mine >> i) & 1 ? vsc[i] : 0.0f;
         }
       }
@@ -747,7 +756,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
 #pragma unroll
         for (int t = 0; t < 2; ++t)
           *reinterpret_cast<SHERRY_GLOBAL v4f*>(as_global_mut(to) + 16 * t) =
-              v4f{x[4 * t], x[4 * t + 1], x[4 * t + 2], x[4 * t + 3]};
+              v4f{kept[4 * t], kept[4 * t + 1], kept[4 * t + 2], kept[4 * t + 3]};
       }
       float top = x[0];
 #pragma unroll
@@ -972,7 +981,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a) {
     l = m == kMinusInf ? 0.0f : l * factor_at(m, top);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
-    // a row's probability is 2^(x - max) / sum; nothing attended to: 0
+    // a row's probability is 2^(x - max) / sum; nothing attended to: 0 (a sum
+    // that is NaN makes every attended row's weight NaN)
     if (lane == 0) lse[i] = l == 0.0f ? make_float2(0.0f, 0.0f) : make_float2(top, kUp / l);
   }
   // four rows per thread at once
@@ -994,8 +1004,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a) {
 #pragma unroll 4
   for (int i = 0; i < a.group; ++i)
 #pragma unroll
-    for (int j = 0; j < AT; ++j)
-      p[j] += __builtin_amdgcn_exp2f(as_global(from)[i * a.score_stride + (r[j] < 0 ? r0 : r[j])] - lse[i].x) * lse[i].y;
+    for (int j = 0; j < AT; ++j) {
+      const float x = as_global(from)[i * a.score_stride + (r[j] < 0 ? r0 : r[j])];
+      const float add = __builtin_amdgcn_exp2f(x - lse[i].x) * lse[i].y;
+      p[j] += x == kMinusInf ? 0.0f : add;  // (left out)
+    }
 #pragma unroll
   for (int j = 0; j < AT; ++j)
     if (r[j] >= 0) as_global_mut(to)[r[j]] = w[j] + p[j];

@@ -34,3 +34,69 @@ def test_attend_16_bit_results_are_rounded_once(dev, ref, kind, cache):
         assert past.max() <= TOL["f32"], (past.max(), (past > TOL["f32"]).sum())
     # the rows' weights come from the scores, which a q of 16 bits loses nothing of
     assert _rel(a.dw.double().cpu().numpy(), p) <= TOL["f32"]
+
+
+@pytest.mark.parametrize("cache", ["bf16", "f16", "i8"])
+@pytest.mark.parametrize("page", [16, 10])
+@pytest.mark.parametrize("what", ["mask", "window_positions", "absent"])
+def test_attend_weights_of_rows_left_out_beside_a_nan(dev, ref, cache, page, what):
+    """A NaN in one attended row makes its head's weights NaN, but the weight of
+    a row that is left out is not touched, bit for bit."""
+    _case("attend nan weights", cache, page, what)
+    rng = np.random.default_rng(page)
+    lens = [300, 1200, 40]
+    c = ref.Cache(rng, 3, -(-1200 // page), 2, page, 64, cache)
+    use = np.zeros((3, 2, c.rows), bool)
+    for b, n in enumerate(lens):
+        use[b, :, :n] = True
+    mask = position = q_pos = None
+    window = 0
+    if what == "mask":
+        mask = (rng.random((3, c.rows)) < 0.6).astype(np.uint8)
+        use &= mask[:, None] != 0
+    elif what == "window_positions":
+        window, q_pos = 500, np.full(3, c.rows, np.int32)
+        position = rng.permuted(np.tile(np.arange(c.rows, dtype=np.int32), (3, 2, 1)), axis=-1)
+        use &= position > c.rows - window
+    else:
+        for b, p in ((0, 1), (0, 4), (1, 0), (1, 37), (2, 1)):
+            c.table[b, p] = -1 - p
+            use[b, :, p * page:(p + 1) * page] = False
+    for b in range(3):  # key-value head 1 of each sequence
+        r = int(np.flatnonzero(use[b, 1])[-1])
+        if cache == "i8":
+            c.scale["k"][int(c.table[b, r // page]), 1, r % page] = np.nan
+        else:
+            c.view("k")[int(c.table[b, r // page]), 1, r % page, 5] = float("nan")
+    q = rng.standard_normal((3, 8, 64)).astype(np.float32)
+    start = rng.random((3, 2, c.rows)).astype(np.float32)
+    a = Attend(dev, ref, c, q, "f32", lens, window, mask, position, q_pos, start)
+    got = a.run()
+    w = a.dw.cpu().numpy()
+    assert np.array_equal(w[~use], start[~use])
+    assert np.all(np.isnan(w[:, 1][use[:, 1]])) and np.all(np.isnan(got[:, 4:]))
+    want, p = ref.attend64(c, a.q, lens, a.scale, window, mask, position, q_pos)
+    assert _rel(got[:, :4], want[:, :4]) <= TOL["f32"]
+    # (the sums of weights in fp32: a unit of 1 from each rounding)
+    assert np.max(np.abs(w[:, 0] - start[:, 0] - p[:, 0])) <= 2e-6
+
+
+def test_attend_weights_of_scores_past_the_range(dev, ref):
+    """Attended scores of -infinity: weight 0 beside finite ones, and none at all
+    where there are no others; NaN beside a NaN."""
+    rng = np.random.default_rng(32)
+    lens = [700, 700, 700]
+    c = ref.Cache(rng, 3, 44, 1, 16, 64, "bf16")
+    c.view("k")[:] = c.view("k").abs() + 0.5
+    for b, r in ((0, 333), (2, 40)):
+        c.view("k")[int(c.table[b, r // 16]), 0, r % 16] = 0  # score 0
+    c.view("k")[int(c.table[2, 20]), 0, 3, 7] = float("nan")
+    q = -(np.abs(rng.standard_normal((3, 4, 64))) + 0.5).astype(np.float32)
+    a = Attend(dev, ref, c, q, "f32", lens, scale=1e37, weight=np.zeros((3, 1, c.rows), np.float32))
+    got = a.run()
+    w = a.dw.cpu().numpy()[:, 0, :700]
+    one = np.zeros(700, np.float32)
+    one[333] = 4
+    assert np.array_equal(w[0], one) and np.array_equal(w[1], 0 * one) and np.all(np.isnan(w[2]))
+    v = c.rows64("v", 0, 0, 700)[333]
+    assert _rel(got[0], np.tile(v, (4, 1))) <= TOL["f32"] and np.all(got[1] == 0) and np.all(np.isnan(got[2]))
