@@ -83,6 +83,10 @@ constexpr int kOutside = 0x7FFFFFF0;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kMinusInf = -__builtin_huge_valf();
 constexpr float kLowest = -3.40282347e38f;  // the least finite value
+// p is held times 2^kUp in f16, where its low term would be subnormal, its sum is
+// not.  (In the exponent, exp2(x - (max - 14)), it was lost in the rounding of max -
+// 14 where that is large.)
+constexpr int kUp = 14;
 
 struct Attend {
   Cache c;
@@ -648,13 +652,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
     float* score = nullptr;  // of this lane's head, and its rows of a tile
     if (G::MORE && a.weight)
       score = a.score + (int64_t(b) * a.heads + head0 + (n < heads ? n : 0)) * a.score_stride + 4 * g;
-    constexpr float kUp = G::F16 ? 14.0f : 0.0f;  // p is held times 2^14 in f16
     v4f o[G::CH];
 #pragma unroll
     for (int e = 0; e < G::CH; ++e) o[e] = v4f{0, 0, 0, 0};
     float m = kMinusInf, l = 0.0f;
     // int8: V's scales are held over 2^ve, the largest of them so far
-    int ve = -126;
+    int ve = kUp - 126;  // (2^(kUp - ve) is a finite factor)
 
     // Tile i's rows are read into slot i % D while those of the D tiles before it
     // are used.  With D > 1 every load goes out (past t1 of no rows), so that a
@@ -789,13 +792,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
 #pragma unroll
           for (int i = 0; i < G::VW; ++i) v[j][i] = (mine >> j) & 1 ? v[j][i] : 0;
       }
-      const float low = base - kUp, vdown = G::I8 ? ldexpf(1.0f, -ve) : 1.0f;
+      const float scale_p = G::I8 ? ldexpf(1.0f, kUp - ve) : ldexpf(1.0f, kUp);
       float p[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(x[i] - low);
+        p[i] = __builtin_amdgcn_exp2f(x[i] - base);
         l += p[i];
-        if constexpr (G::I8) p[i] *= vsc[i] * vdown;
+        if constexpr (G::I8) p[i] *= vsc[i] * scale_p;
+        else if constexpr (G::F16) p[i] *= scale_p;
       }
       u32x4 pf[NT];
       split<G::F16, NT>(p, pf);
@@ -839,7 +843,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) top = fmaxf(top, stat[i][n].x);
     float down = m == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
-    if constexpr (G::I8) down = ldexpf(down, ve + kByteDown);
+    if constexpr (G::I8) down = ldexpf(down, ve + kByteDown - kUp);
+    else if constexpr (G::F16) down = ldexpf(down, -kUp);
     if (n < heads) {
 #pragma unroll
       for (int e = 0; e < G::CH; ++e)
@@ -896,7 +901,7 @@ constexpr int kWeightRows = 1024;  // rows of weight per workgroup
 
 // Blocks [0, batch * heads): the query heads' outputs, the parts of their
 // sequence joined; then, for weight, [batch][kv][rows / kWeightRows].
-template <int DP, bool F16>
+template <int DP>
 __global__ __launch_bounds__(256) void attend_join_kernel(Attend a) {
   constexpr int PER = DP / 64;
   __shared__ float red[4][DP];
@@ -966,7 +971,6 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a) {
   const int r1 = (ch + 1) * kWeightRows < sp.end ? (ch + 1) * kWeightRows : sp.end;
   if (r0 >= r1) return;
   const int2 parts = as_global(a.parts)[b];
-  constexpr float kUp = F16 ? 16384.0f : 1.0f;  // (f16: the sums are held times 2^14)
   for (int i = wave; i < a.group; i += 4) {
     const int hd = (h * a.gtiles + i / 16) * a.gmax + i % 16;
     float m = kMinusInf, l = 0.0f;
@@ -983,7 +987,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a) {
     for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
     // a row's probability is 2^(x - max) / sum; nothing attended to: 0 (a sum
     // that is NaN makes every attended row's weight NaN)
-    if (lane == 0) lse[i] = l == 0.0f ? make_float2(0.0f, 0.0f) : make_float2(top, kUp / l);
+    if (lane == 0) lse[i] = l == 0.0f ? make_float2(0.0f, 0.0f) : make_float2(top, 1.0f / l);
   }
   // four rows per thread at once
   constexpr int AT = kWeightRows / 256;
@@ -1021,7 +1025,7 @@ int launch_cfg(const Attend& a, hipStream_t s) {
   if (rc != SHERRY_OK || a.whole) return rc;
   int64_t blocks = int64_t(a.c.batch) * a.heads;
   if (a.weight) blocks += int64_t(a.c.batch) * a.c.kv * ceil_div(a.c.rows, kWeightRows);
-  return launch(attend_join_kernel<G::DP, G::F16>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
+  return launch(attend_join_kernel<G::DP>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
 }
 template <int CT, int QT, int NT, int DP>
 int launch_pages(const Attend& a, hipStream_t s) {

@@ -100,3 +100,51 @@ def test_attend_weights_of_scores_past_the_range(dev, ref):
     assert np.array_equal(w[0], one) and np.array_equal(w[1], 0 * one) and np.all(np.isnan(w[2]))
     v = c.rows64("v", 0, 0, 700)[333]
     assert _rel(got[0], np.tile(v, (4, 1))) <= TOL["f32"] and np.all(got[1] == 0) and np.all(np.isnan(got[2]))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "f16", "i8"])
+@pytest.mark.parametrize("power", [24, 25, 26, 27, 28, 60])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_attend_large_scores(dev, ref, cache, power, sign):
+    """Largest scores of +-2^power and up to twice that, in units of ln 2, in rows
+    of equal keys: the softmax is even over these, exactly, so a head's weights sum
+    to 1 and its outputs are the rows' mean."""
+    _case("attend large scores", cache, power, sign)
+    rng = np.random.default_rng(power)
+    lens = [900, 90, 33]
+    c = ref.Cache(rng, 3, 57, 2, 16, 64, cache)
+    c.view("k")[:] = 0
+    other = 0.5 if sign > 0 else 2.0  # of the top rows' score
+    if cache == "i8":
+        c.view("k")[..., 0] = 64
+        c.scale["k"][:] = other / 64
+    else:
+        c.view("k")[..., 0] = other
+    for b, n in enumerate(lens):
+        for h in range(2):
+            for r in rng.choice(n, 7, replace=False):
+                page = int(c.table[b, r // 16])
+                if cache == "i8":
+                    c.scale["k"][page, h, r % 16] = 1 / 64
+                else:
+                    c.view("k")[page, h, r % 16, 0] = 1
+    q = np.zeros((3, 16, 64), np.float32)
+    q[..., 0] = sign * 2.0 ** power * (1 + rng.random((3, 16))) * np.log(2)
+    a = Attend(dev, ref, c, q, "f32", lens, scale=1.0, weight=np.zeros((3, 2, c.rows), np.float32))
+    got = a.run()
+    want, p = ref.attend64(c, a.q, lens, 1.0)
+    assert np.all(np.isfinite(got)) and _rel(got, want) <= TOL["f32"]
+    assert _rel(a.dw.double().cpu().numpy(), p) <= TOL["f32"]
+    assert np.allclose(p.sum(-1), 8)  # (of the reference: 8 heads a group)
+    plain = Attend(dev, ref, c, q, "f32", lens, scale=1.0).run()
+    assert np.all(np.isfinite(plain)) and _rel(plain, want) <= TOL["f32"]
+
+
+@pytest.mark.parametrize("low,high", [(-37, -32), (30, 34)])
+def test_attend_int8_scales_near_the_ends(dev, ref, low, high):
+    """V scales near the least and the largest normal numbers."""
+    rng = np.random.default_rng(37)
+    lens = [700, 90, 33]
+    c = ref.Cache(rng, 3, 44, 2, 16, 64, "i8")
+    c.scale["v"] = (10.0 ** rng.uniform(low, high, c.scale["v"].shape)).astype(np.float32)
+    Attend(dev, ref, c, rng.standard_normal((3, 8, 64)).astype(np.float32), "f32", lens).check(ref)
