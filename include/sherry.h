@@ -582,7 +582,9 @@ typedef struct sherry_append_desc {
                          /* NULL (heads is then ignored)                      */
   const void* k;         /* device, [tokens][kv_heads][head_dim] of type      */
   const void* v;         /* device, as k                                      */
-  void* q_out;           /* device, as q: q rotated; may be q                 */
+  void* q_out;           /* device, as q: q rotated; may be q itself with the */
+                         /* same stride (else, with several tokens,           */
+                         /* SHERRY_E_SHAPE), and may not overlap it otherwise */
   const int32_t* seq;    /* device, int32 [tokens]: the token's sequence      */
   const int32_t* slot;   /* device, int32 [tokens]: its row there             */
   const int32_t* pos;    /* device, int32 [tokens]: its rotary position       */

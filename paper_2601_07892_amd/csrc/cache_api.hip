@@ -58,6 +58,11 @@ int check_append(const sherry_cache_desc* c, const sherry_append_desc* a) {
   if ((a->k_stride && a->k_stride < row) || (a->v_stride && a->v_stride < row) ||
       (a->q && ((a->q_stride && a->q_stride < qrow) || (a->q_out_stride && a->q_out_stride < qrow))))
     return SHERRY_E_SHAPE;
+  // in place every token's row has to lie where it is read: another stride would
+  // write rows that other workgroups have yet to read
+  if (a->q && a->q_out == a->q && a->tokens > 1 &&
+      (a->q_stride ? a->q_stride : qrow) != (a->q_out_stride ? a->q_out_stride : qrow))
+    return SHERRY_E_SHAPE;
   // (the most workgroups of the launch: one per token and four rows)
   if (a->tokens * (ceil_div((a->q ? a->heads : 0) + 2 * c->kv_heads, 4)) > INT32_MAX) return SHERRY_E_SHAPE;
   const uintptr_t e = static_cast<uintptr_t>(type_bytes(a->type));

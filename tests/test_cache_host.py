@@ -176,3 +176,19 @@ def test_descriptor_sizes():
     for cls, n in ((sh.sherry_epilogue, 48), (sh.sherry_cache_desc, 80), (sh.sherry_append_desc, 152),
                    (sh.sherry_attend_desc, 120), (sh.sherry_evict_desc, 88)):
         assert ctypes.sizeof(cls) == n
+
+
+@pytest.mark.parametrize("strides", [(600, 0), (0, 600), (600, 520), (512, 600)])
+def test_append_in_place_with_other_strides_refused(strides):
+    """q_out = q and rows that lie elsewhere: a token's output would be another
+    token's unread row."""
+    d = _append(q_stride=strides[0], q_out_stride=strides[1])
+    assert L.sherry_cache_append(_cache(), d, None) == S
+    d.q_out = FAKE + 4 * 600 * 3  # apart: passes that check (and fails a later one)
+    d.pos = FAKE + 2
+    assert L.sherry_cache_append(_cache(), d, None) == A
+    d = _append(q_stride=strides[0], q_out_stride=strides[1], tokens=1, pos=FAKE + 2)  # one row: no other
+    assert L.sherry_cache_append(_cache(), d, None) == A
+    for same in ((0, 512), (512, 0), (600, 600)):
+        d = _append(q_stride=same[0], q_out_stride=same[1], pos=FAKE + 2)
+        assert L.sherry_cache_append(_cache(), d, None) == A
