@@ -597,8 +597,8 @@ typedef struct sherry_append_desc {
                          /* position is not NULL                              */
   int64_t q_stride, k_stride, v_stride, q_out_stride; /* elements from token  */
                          /* to token; 0: contiguous                           */
-  int32_t tokens;        /* >= 1                                              */
-  int32_t heads;
+  int32_t tokens;        /* 1 .. SHERRY_MAX_M                                 */
+  int32_t heads;         /* 1 .. 256 * 4096                                   */
   int32_t type;          /* of q, k, v and q_out: SHERRY_F32, _F16 or _BF16   */
   int32_t rope_rows;     /* positions in cos and sin                          */
   int32_t rot_dim;       /* even, 2 .. head_dim; later values are not rotated */
@@ -639,7 +639,7 @@ typedef struct sherry_attend_desc {
   int64_t q_stride, out_stride; /* elements from token to token, a multiple   */
                          /* of 8; 0: contiguous                               */
   int64_t mask_stride, row_stride; /* >= table_width * page_size where used   */
-  int32_t heads;         /* a multiple of kv_heads                            */
+  int32_t heads;         /* a multiple of kv_heads, at most 256 times it      */
   int32_t type;          /* of q and out: SHERRY_F32, _F16 or _BF16           */
   int32_t window;        /* 0: all rows; else the last window rows, or with   */
                          /* position the rows with position > q_pos - window  */

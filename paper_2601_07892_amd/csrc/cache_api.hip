@@ -12,7 +12,7 @@ static_assert(sizeof(sherry_evict_desc) == 88, "sherry_evict_desc layout");
 
 namespace {
 
-constexpr int kMaxHeads = 4096, kMaxBatch = 16384, kMaxGroup = 256;
+constexpr int kMaxHeads = 4096, kMaxBatch = 65535, kMaxGroup = 256;
 
 inline bool aligned(const void* p, uintptr_t a) {
   return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0;  // (NULL is)

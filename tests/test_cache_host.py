@@ -192,3 +192,20 @@ def test_append_in_place_with_other_strides_refused(strides):
     for same in ((0, 512), (512, 0), (600, 600)):
         d = _append(q_stride=same[0], q_out_stride=same[1], pos=FAKE + 2)
         assert L.sherry_cache_append(_cache(), d, None) == A
+
+
+def test_limits_of_the_header():
+    """The largest values that the header names pass, the next ones do not."""
+    def size(cache, **kw):
+        return L.sherry_cache_attend_workspace(_cache(**cache), _attend(**kw))
+    assert size(dict(batch=65535)) > 0 and size(dict(batch=65536)) == 0
+    assert size(dict(kv_heads=4096), heads=4096) > 0 and size(dict(kv_heads=4097), heads=4097) == 0
+    assert size({}, heads=2 * 256) > 0 and size({}, heads=2 * 257) == 0
+    assert size(dict(head_dim=256)) > 0 and size(dict(head_dim=264)) == 0
+    top = dict(page_size=1 << 20, table_width=1 << 10)
+    assert size(top) > 0 and size(dict(top, table_width=(1 << 10) + 1)) == 0
+    late = dict(pos=FAKE + 2)  # fails the last of the checks
+    assert L.sherry_cache_append(_cache(batch=65535), _append(**late), None) == A
+    assert L.sherry_cache_append(_cache(), _append(heads=256 * 4096, tokens=1, **late), None) == A
+    assert L.sherry_cache_append(_cache(), _append(heads=256 * 4096 + 1, tokens=1, **late), None) == S
+    assert L.sherry_cache_evict(_cache(batch=65535), _evict(kept=FAKE + 1), None) == A

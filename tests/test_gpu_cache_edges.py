@@ -148,3 +148,40 @@ def test_attend_int8_scales_near_the_ends(dev, ref, low, high):
     c = ref.Cache(rng, 3, 44, 2, 16, 64, "i8")
     c.scale["v"] = (10.0 ** rng.uniform(low, high, c.scale["v"].shape)).astype(np.float32)
     Attend(dev, ref, c, rng.standard_normal((3, 8, 64)).astype(np.float32), "f32", lens).check(ref)
+
+
+def test_cache_of_65535_sequences(dev, ref):
+    """The most sequences that a cache may have: all of them appended to, attended to
+    and cut down."""
+    import paper_2601_07892_amd as sh
+    rng = np.random.default_rng(33)
+    batch, dim = 65535, 16
+    c = ref.Cache(rng, batch, 1, 1, 8, dim, "f16")
+    lens = rng.integers(0, 8, batch)
+    q = rng.standard_normal((batch, 1, dim)).astype(np.float32)
+    x = torch.from_numpy(rng.standard_normal((batch, 1, dim)).astype(np.float32)).to(dev)
+    a = Attend(dev, ref, c, q, "f32", lens + 1, weight=np.zeros((batch, 1, 8), np.float32))
+    d = sh.sherry_append_desc()
+    seq = torch.arange(batch, dtype=torch.int32, device=dev)
+    slot = torch.from_numpy(lens.astype(np.int32)).to(dev)
+    d.k = d.v = x.data_ptr()
+    d.seq, d.slot, d.pos, d.tokens = seq.data_ptr(), slot.data_ptr(), slot.data_ptr(), batch
+    sh.sherry_cache_append(a.cd, d)
+    torch.cuda.synchronize()
+    page = torch.from_numpy(c.table[:, 0]).long()
+    for name in "kv":
+        c.view(name)[page, 0, torch.from_numpy(lens)] = x[:, 0].cpu().half()
+        assert torch.equal(c.d[name].cpu(), c.pool[name])
+    for w in (True, False):
+        if not w:
+            a = Attend(dev, ref, c, q, "f32", lens + 1)
+        got = a.run()
+        k, v = (c.view(n)[page, 0].double().numpy() for n in "kv")
+        s = np.einsum("bd,brd->br", a.q[:, 0].astype(np.float64), k) * a.scale
+        s[np.arange(8) > lens[:, None]] = -np.inf
+        p = np.exp(s - s.max(-1, keepdims=True))
+        p /= p.sum(-1, keepdims=True)
+        assert _rel(got[:, 0], np.einsum("br,brd->bd", p, v)) <= TOL["f32"]
+        if w:
+            assert _rel(a.dw.double().cpu().numpy()[:, 0], p) <= TOL["f32"]
+    _evict(dev, ref, rng, "f16", list(lens + 1), 3, 1, dim, 8, recent=1)
