@@ -612,7 +612,9 @@ typedef struct sherry_append_desc {
  * whose seq, slot, page or (with cos) pos is out of range is left out
  * entirely.  No two tokens may have the same seq and slot.  Input rows are
  * aligned to their element.  cache->table and the rows that exist are not
- * changed; lengths are the caller's. */
+ * changed; lengths are the caller's.  Calls of 2^32 threads and more are refused
+ * (SHERRY_E_SHAPE): a token takes 256 for every 16 rows of q, k and v of up to 64
+ * values, 8 of up to 128, 4 of more. */
 int sherry_cache_append(const sherry_cache_desc* cache, const sherry_append_desc* args,
                         void* stream);
 
@@ -652,7 +654,9 @@ typedef struct sherry_attend_desc {
 size_t sherry_cache_attend_workspace(const sherry_cache_desc* cache,
                                      const sherry_attend_desc* args);
 
-/* Attention needs batch * table_width * page_size < 2^36 (SHERRY_E_SHAPE).
+/* Attention needs batch * table_width * page_size < 2^36, and, where the table
+ * has more than 512 rows or weight is given, batch * heads and for weight batch *
+ * kv_heads * ceil(table_width * page_size / 1024) together < 2^24 (SHERRY_E_SHAPE).
  * out = sum_r p_r v_r, p = softmax over the rows left in of scale * q . k_r; a
  * token with no row left in (or only scores of -infinity) gives 0.  Rows left
  * out never reach the result, whatever they hold; a NaN or an infinity in the
@@ -690,7 +694,10 @@ typedef struct sherry_evict_desc {
  * that were given up, so the cache is compacted in place with the fewest
  * moves, and pages past ceil(length_out / page_size) are free.  k, v and the
  * scales are moved in the pages (a move from or to an absent page is left
- * out); weight and position are only read, and no output may overlap them. */
+ * out); weight and position are only read, and no output may overlap them.  batch *
+ * kv_heads is at most 2^22 - 1, and batch * kv_heads * ceil(keep / R) + batch *
+ * kv_heads * ceil(keep / 1024) less than 2^24, R = 256 for rows of up to 64 bytes, 128
+ * of up to 128, 64 of up to 256, else 32 (SHERRY_E_SHAPE). */
 int sherry_cache_evict(const sherry_cache_desc* cache, const sherry_evict_desc* args,
                        void* stream);
 

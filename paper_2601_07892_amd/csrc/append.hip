@@ -168,9 +168,13 @@ int launch_type(const Append& a, bool vec, hipStream_t s) {
   return vec ? launch(append_kernel<LPR, TYPE, true>, grid, dim3(256), 0, s, a)
              : launch(append_kernel<LPR, TYPE, false>, grid, dim3(256), 0, s, a);
 }
+int lanes_per_row(int dim) { return dim <= 64 ? 16 : dim <= 128 ? 32 : 64; }
+// Workgroups per token.
+int64_t parts_of(int heads, int kv, int lanes) { return ceil_div(heads + 2 * kv, 256 / lanes); }
+
 template <int LPR>
 int launch_lanes(Append a, bool vec, hipStream_t s) {
-  a.by_parts = FastDiv::of(static_cast<uint32_t>(ceil_div(a.heads + 2 * a.c.kv, 256 / LPR)));
+  a.by_parts = FastDiv::of(static_cast<uint32_t>(parts_of(a.heads, a.c.kv, LPR)));
   switch (a.type) {
     case SHERRY_F32: return launch_type<LPR, SHERRY_F32>(a, vec, s);
     case SHERRY_F16: return launch_type<LPR, SHERRY_F16>(a, vec, s);
@@ -179,6 +183,10 @@ int launch_lanes(Append a, bool vec, hipStream_t s) {
 }
 
 }  // namespace
+
+int64_t append_threads(const sherry_cache_desc& c, const sherry_append_desc& d) {
+  return 256 * d.tokens * parts_of(d.q ? d.heads : 0, c.kv_heads, lanes_per_row(c.head_dim));
+}
 
 int launch_append(const sherry_cache_desc& c, const sherry_append_desc& d, hipStream_t s) {
   const int heads = d.q ? d.heads : 0;
@@ -195,9 +203,11 @@ int launch_append(const sherry_cache_desc& c, const sherry_append_desc& d, hipSt
   const bool vec = whole(a.k, a.k_stride) && whole(a.v, a.v_stride) &&
                    (!heads || (whole(a.q, a.q_stride) && whole(a.q_out, a.q_out_stride))) &&
                    reinterpret_cast<uintptr_t>(a.cos) % 16 == 0 && reinterpret_cast<uintptr_t>(a.sin) % 16 == 0;
-  if (c.head_dim <= 64) return launch_lanes<16>(a, vec, s);
-  if (c.head_dim <= 128) return launch_lanes<32>(a, vec, s);
-  return launch_lanes<64>(a, vec, s);
+  switch (lanes_per_row(c.head_dim)) {
+    case 16: return launch_lanes<16>(a, vec, s);
+    case 32: return launch_lanes<32>(a, vec, s);
+    default: return launch_lanes<64>(a, vec, s);
+  }
 }
 
 }  // namespace sherry

@@ -1018,13 +1018,17 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a) {
     if (r[j] >= 0) as_global_mut(to)[r[j]] = w[j] + p[j];
 }
 
+// Workgroups of the joining launch.
+int64_t join_groups(int64_t batch, int64_t heads, int64_t kv, int64_t rows, bool weight) {
+  return batch * (heads + (weight ? kv * ceil_div(rows, kWeightRows) : 0));
+}
+
 template <class G>
 int launch_cfg(const Attend& a, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(a.c.kv * a.gtiles), static_cast<unsigned>(a.columns));
   const int rc = launch(attend_kernel<G>, grid, dim3(64 * kWaves), 0, s, a);
   if (rc != SHERRY_OK || a.whole) return rc;
-  int64_t blocks = int64_t(a.c.batch) * a.heads;
-  if (a.weight) blocks += int64_t(a.c.batch) * a.c.kv * ceil_div(a.c.rows, kWeightRows);
+  const int64_t blocks = join_groups(a.c.batch, a.heads, a.c.kv, a.c.rows, a.weight != nullptr);
   return launch(attend_join_kernel<G::DP>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
 }
 template <int CT, int QT, int NT, int DP>
@@ -1075,6 +1079,12 @@ Shape shape_of(const sherry_cache_desc& c, const sherry_attend_desc& d) {
 }
 
 }  // namespace
+
+int64_t attend_threads(const sherry_cache_desc& c, const sherry_attend_desc& d) {
+  const Shape s = shape_of(c, d);  // (the first launch: at most 2^16 workgroups in x and in y)
+  const int64_t rows = int64_t(c.table_width) * c.page_size;
+  return s.whole ? 0 : 256 * join_groups(c.batch, d.heads, c.kv_heads, rows, d.weight != nullptr);
+}
 
 size_t attend_workspace(const sherry_cache_desc& c, const sherry_attend_desc& d) {
   return shape_of(c, d).bytes();

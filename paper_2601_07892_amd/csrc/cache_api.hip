@@ -63,8 +63,7 @@ int check_append(const sherry_cache_desc* c, const sherry_append_desc* a) {
   if (a->q && a->q_out == a->q && a->tokens > 1 &&
       (a->q_stride ? a->q_stride : qrow) != (a->q_out_stride ? a->q_out_stride : qrow))
     return SHERRY_E_SHAPE;
-  // (the most workgroups of the launch: one per token and four rows)
-  if (a->tokens * (ceil_div((a->q ? a->heads : 0) + 2 * c->kv_heads, 4)) > INT32_MAX) return SHERRY_E_SHAPE;
+  if (!fits_grid(append_threads(*c, *a))) return SHERRY_E_SHAPE;
   const uintptr_t e = static_cast<uintptr_t>(type_bytes(a->type));
   if (!aligned(a->q, e) || !aligned(a->k, e) || !aligned(a->v, e) || !aligned(a->q_out, e) ||
       !aligned(a->seq, 4) || !aligned(a->slot, 4) || !aligned(a->pos, 4) || !aligned(a->cos, 4) ||
@@ -91,10 +90,7 @@ int check_attend_shape(const sherry_cache_desc* c, const sherry_attend_desc* a) 
     return SHERRY_E_SHAPE;
   // (all rows in tiles of 32, and a few more per sequence, are counted in 32 bits)
   if (int64_t(c->batch) * (ceil_div(cache_rows(c), 32) + 16) > INT32_MAX) return SHERRY_E_SHAPE;
-  // (the joining launch: one workgroup per sequence and head, and for weight one
-  // per sequence, key-value head and 1024 rows)
-  if (int64_t(c->batch) * (a->heads + c->kv_heads * ceil_div(cache_rows(c), 1024)) > INT32_MAX)
-    return SHERRY_E_SHAPE;
+  if (!fits_grid(attend_threads(*c, *a))) return SHERRY_E_SHAPE;
   return SHERRY_OK;
 }
 
@@ -106,9 +102,7 @@ int check_evict(const sherry_cache_desc* c, const sherry_evict_desc* a) {
   if (a->keep < 1 || a->keep > SHERRY_MAX_CACHE_ROWS || a->row_stride < cache_rows(c) ||
       a->out_stride < a->keep)
     return SHERRY_E_SHAPE;
-  // (the moving launch: one workgroup per 32 or more new rows, and per 1024)
-  if (int64_t(c->batch) * c->kv_heads * (ceil_div(a->keep, 32) + ceil_div(a->keep, 1024)) > INT32_MAX)
-    return SHERRY_E_SHAPE;
+  if (!fits_grid(evict_threads(*c, *a))) return SHERRY_E_SHAPE;
   if (!aligned(a->length, 4) || !aligned(a->weight, 4) || !aligned(a->position, 4) ||
       !aligned(a->recent_from, 4) || !aligned(a->length_out, 4) || !aligned(a->kept, 4) ||
       !aligned(a->weight_out, 4) || !aligned(a->position_out, 4))

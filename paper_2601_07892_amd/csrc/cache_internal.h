@@ -94,6 +94,12 @@ __device__ __forceinline__ int wave_scan(int v) {
   return v;
 }
 
+// Threads of a call's largest launch; a grid holds 2^32 - 1.
+int64_t append_threads(const sherry_cache_desc& c, const sherry_append_desc& a);
+int64_t attend_threads(const sherry_cache_desc& c, const sherry_attend_desc& a);
+int64_t evict_threads(const sherry_cache_desc& c, const sherry_evict_desc& a);
+inline bool fits_grid(int64_t threads) { return threads <= int64_t(UINT32_MAX); }
+
 size_t attend_workspace(const sherry_cache_desc& c, const sherry_attend_desc& a);
 int launch_attend(const sherry_cache_desc& c, const sherry_attend_desc& a, hipStream_t s);
 int launch_append(const sherry_cache_desc& c, const sherry_append_desc& a, hipStream_t s);

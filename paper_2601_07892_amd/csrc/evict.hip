@@ -385,18 +385,36 @@ __global__ __launch_bounds__(256) void evict_move_kernel(Evict a, int copies) {
   }
 }
 
+int lanes_per_row(int bytes) { return bytes <= 64 ? 4 : bytes <= 128 ? 8 : bytes <= 256 ? 16 : 32; }
+// Workgroups of the moving launch: those that copy rows (with room for every row
+// nothing moves), and those that write weights and positions.
+int64_t copy_groups(int64_t heads, int keep, int64_t rows, int lanes) {
+  return keep < rows ? heads * ceil_div(keep, 256 / lanes * kMoveAt) : 0;
+}
+int64_t out_groups(int64_t heads, int keep, bool outs) {
+  return outs ? heads * ceil_div(keep, 256 * kMoveAt) : 0;
+}
+
 template <int LPR>
 int launch_move(const Evict& a, hipStream_t s) {
   const int64_t heads = int64_t(a.c.batch) * a.c.kv;
-  // (with room for every row nothing moves)
-  const int64_t copies = a.keep < a.c.rows ? heads * ceil_div(a.keep, 256 / LPR * kMoveAt) : 0;
-  const int64_t outs = a.weight_out || a.position_out ? heads * ceil_div(a.keep, 256 * kMoveAt) : 0;
+  const int64_t copies = copy_groups(heads, a.keep, a.c.rows, LPR);
+  const int64_t outs = out_groups(heads, a.keep, a.weight_out || a.position_out);
   if (copies + outs == 0) return SHERRY_OK;
   return launch(evict_move_kernel<LPR>, dim3(static_cast<unsigned>(copies + outs)), dim3(256), 0, s, a,
                 static_cast<int>(copies));
 }
 
 }  // namespace
+
+int64_t evict_threads(const sherry_cache_desc& c, const sherry_evict_desc& d) {
+  const int64_t heads = int64_t(c.batch) * c.kv_heads, rows = int64_t(c.table_width) * c.page_size;
+  const int lanes = lanes_per_row(c.head_dim * type_bytes(c.type));
+  const int64_t move = 256 * (copy_groups(heads, d.keep, rows, lanes) +
+                              out_groups(heads, d.keep, d.weight_out || d.position_out));
+  const int64_t select = kThreads * heads;
+  return move > select ? move : select;
+}
 
 int launch_evict(const sherry_cache_desc& c, const sherry_evict_desc& d, hipStream_t s) {
   const Evict a{cache_of(c), d.length, d.weight, d.position, d.recent_from, d.length_out, d.kept,
@@ -409,10 +427,12 @@ int launch_evict(const sherry_cache_desc& c, const sherry_evict_desc& d, hipStre
                  : rows <= 64 * kThreads ? launch(evict_select_kernel<64>, grid, block, 0, s, a)
                                          : launch(evict_select_kernel<0>, grid, block, 0, s, a);
   if (rc != SHERRY_OK) return rc;
-  if (a.bytes <= 64) return launch_move<4>(a, s);
-  if (a.bytes <= 128) return launch_move<8>(a, s);
-  if (a.bytes <= 256) return launch_move<16>(a, s);
-  return launch_move<32>(a, s);
+  switch (lanes_per_row(a.bytes)) {
+    case 4: return launch_move<4>(a, s);
+    case 8: return launch_move<8>(a, s);
+    case 16: return launch_move<16>(a, s);
+    default: return launch_move<32>(a, s);
+  }
 }
 
 }  // namespace sherry

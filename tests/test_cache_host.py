@@ -209,3 +209,37 @@ def test_limits_of_the_header():
     assert L.sherry_cache_append(_cache(), _append(heads=256 * 4096, tokens=1, **late), None) == A
     assert L.sherry_cache_append(_cache(), _append(heads=256 * 4096 + 1, tokens=1, **late), None) == S
     assert L.sherry_cache_evict(_cache(batch=65535), _evict(kept=FAKE + 1), None) == A
+
+
+def test_launches_of_more_threads_than_a_grid_holds_refused():
+    """2^32 - 1 threads, 256 a workgroup (1024 in eviction's selection): calls at
+    the limit pass to a later check, the next ones are refused before anything is
+    enqueued."""
+    late = dict(pos=FAKE + 2)
+
+    def append(tokens, heads, **cache):
+        return L.sherry_cache_append(_cache(**cache), _append(tokens=tokens, heads=heads, **late), None)
+    top = (1 << 24) - 1  # workgroups
+    assert append(top, 12) == A and append(top + 1, 12) == S  # 16 rows of 64 values: one a token
+    assert append(top // 2, 13) == A and append(top // 2 + 1, 13) == S
+    assert append(top // 2, 12, head_dim=128) == A and append(top // 2 + 1, 12, head_dim=128) == S
+    assert append(top // 4, 12, head_dim=256) == A and append(top // 4 + 1, 12, head_dim=256) == S
+
+    def attend(rows, batch, heads, kv, weight):
+        c = _cache(batch=batch, kv_heads=kv, table_width=rows // 16)
+        return L.sherry_cache_attend_workspace(c, _attend(heads=heads, weight=FAKE if weight else None, row_stride=rows))
+    assert attend(1024, 65535, 256, 256, False) > 0 and attend(1024, 65535, 257, 257, False) == 0
+    assert attend(512, 65535, 257, 257, False) > 0 and attend(512, 65535, 257, 257, True) == 0
+    assert attend(1024, 65535, 128, 128, True) > 0 and attend(1024, 65535, 129, 129, True) == 0
+    assert attend(8192, 4096, 455, 455, True) > 0 and attend(8192, 4096, 456, 456, True) == 0
+
+    def evict(batch, kv, keep, rows=64, **kw):
+        c = _cache(batch=batch, kv_heads=kv, table_width=rows // 16)
+        return L.sherry_cache_evict(c, _evict(keep=keep, out_stride=1 << 30, row_stride=1 << 30, kept=FAKE + 1, **kw), None)
+    assert evict(1023, 4096, 1) == A and evict(1024, 4096, 1) == S
+    assert evict(65535, 64, 1) == A and evict(65535, 65, 1) == S
+    none = dict(weight_out=None, position_out=None)
+    # rows of 64 bf16 values: 128 kept rows a workgroup; with room for all rows nothing moves
+    assert evict(4096, 4, 1023 * 128, 1 << 20, **none) == A and evict(4096, 4, 1023 * 128 + 1, 1 << 20, **none) == S
+    assert evict(4096, 4, 1024 * 128, 1 << 20, **none) == S and evict(4096, 4, 1024 * 128, 1024 * 128, **none) == A
+    assert evict(4096, 4, 1023 * 1024) == A and evict(4096, 4, 1024 * 1024) == S
