@@ -503,8 +503,12 @@ int sherry_gemv3_batched(const sherry_gemv_desc* descs_dev, int count,
 #define SHERRY_ACT_GELU_TANH 5 /* z (1 + tanh(sqrt(2/pi)(z + 0.044715 z^3)))/2 */
 
 /* y[i][j] = act(p[i][j] + bias[j]) * gate[i][j] + residual[i][j], p the
- * product's fp32 result as sherry_gemm, _channel or _group give it; each step
- * is rounded to fp32.  All NULL and SHERRY_ACT_NONE: the product itself. */
+ * product's fp32 result as sherry_gemm, _channel or _group give it; the bias's
+ * sum z, the gate's product and the residual's sum are rounded to fp32 each.
+ * The relative error of act(z), in units of 2^-24, is at most 1 (RELU2), 8 (SILU
+ * and GELU_TANH) and 16 (GELU) for z >= 0; below 0, as long as the result is past
+ * 2^-116, 8 + 2 |z| (SILU), 16 + 2 z^2 (GELU), 8 + 16 sqrt(2/pi) |z + 0.044715 z^3|
+ * (GELU_TANH).  All NULL and SHERRY_ACT_NONE: the product itself. */
 typedef struct sherry_epilogue {
   const float* bias;       /* device, fp32 [n], 4-byte aligned, or NULL       */
   const float* gate;       /* device, fp32 [m][gate_stride], or NULL          */

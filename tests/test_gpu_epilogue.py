@@ -257,3 +257,38 @@ def test_captured_epilogue(dev):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(y, want))
         assert float(torch.randn(1000, device=dev).sum()) < 1e9
+
+
+@pytest.mark.parametrize("m,f32", [(1, True), (3, False), (40, False)])
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_relative_error(dev, m, f32, act):
+    """act(z) of chosen z (a product of 0 and a bias) within the header's relative
+    bounds, out to where its result is 2^-116: 1 ulp = 2u each of the exp2 and
+    reciprocal units and u of each operation make 8u of silu; gelu adds its
+    polynomial's 1.8u, its argument's 3u and Horner's 2u (16u).  Below 0 an exponent
+    -E (in units of ln 2) whose factors and products are rounded c times adds
+    c E ln 2 u: silu's 1.3 |z|, gelu's 2.3 z^2 / 2, gelu_tanh's 6 w."""
+    import paper_2601_07892_amd as sh
+    from scipy.special import erfc, expit
+    n, k, low = 32768, 128, {"silu": -84, "gelu": -12.5, "gelu_tanh": -9}.get(act, -1e18)
+    rng = np.random.default_rng(5)
+    z = np.concatenate([rng.uniform(max(low, -100), 100, n // 4), rng.uniform(max(low, -13), -1, n // 4), rng.uniform(-2, 2, n // 4),
+                        np.exp(rng.uniform(-20, np.log(-low), n // 8)) * -1, np.exp(rng.uniform(-20, 40, n // 8))]).astype(np.float32)
+    w = torch.from_numpy(sh.sherry_pack(synth.ternary_34(n, k, 15, "zero"))).to(dev)
+    x = torch.zeros((m, k), device=dev) if f32 else torch.zeros((m, k), dtype=torch.int8, device=dev)
+    sx, bias, y = torch.ones(m, device=dev), torch.from_numpy(z).to(dev), torch.empty((m, n), device=dev)
+    e = sh.sherry_epilogue()
+    e.act, e.bias = getattr(sh, "SHERRY_ACT_" + act.upper()), bias.data_ptr()
+    if f32:
+        sh.sherry_gemv_f32_epilogue(w, x, sx, 1.0, None, None, e, y, n, k)
+    else:
+        sh.sherry_gemm_epilogue(w, x, sx, 1.0, None, None, e, y, m, n, k)
+    torch.cuda.synchronize()
+    z = z.astype(np.float64)
+    arg = 2 * np.sqrt(2 / np.pi) * (z + 0.044715 * z ** 3)
+    want = {"gelu": lambda: 0.5 * z * erfc(-z / np.sqrt(2)), "gelu_tanh": lambda: z * expit(arg)}.get(act, lambda: _act(z, act))()
+    under = np.minimum(z, 0)
+    bound = {"none": 0, "relu": 0, "relu2": 1, "silu": 8 - 2 * under, "gelu": 16 + 2 * under ** 2,
+             "gelu_tanh": 8 + 8 * np.maximum(0, -arg)}[act] * U
+    assert np.abs(want[want != 0]).min() > 2.0 ** -116 or act in ("relu", "none")
+    assert np.all(np.abs(y.double().cpu().numpy() - want) <= bound * np.abs(want))
