@@ -185,3 +185,35 @@ def test_cache_of_65535_sequences(dev, ref):
         if w:
             assert _rel(a.dw.double().cpu().numpy()[:, 0], p) <= TOL["f32"]
     _evict(dev, ref, rng, "f16", list(lens + 1), 3, 1, dim, 8, recent=1)
+
+
+@pytest.mark.parametrize("rows", [4000, 15000, 65000, 70000])
+@pytest.mark.parametrize("cache", ["bf16", "i8"])
+def test_evict_in_tables_far_wider_than_the_sequences(dev, ref, rows, cache):
+    """Short sequences in every form that the table's width chooses."""
+    _case("evict wide", rows, cache)
+    lens = [300, 1, 0, 65, 2100, 64]
+    _evict(dev, ref, np.random.default_rng(rows), cache, lens, 60, 2, 32, 16, recent=9, spare=(rows - 2100) // 16)
+
+
+@pytest.mark.parametrize("weights", ["random", "rising", "few"])
+def test_evict_sequences_past_65536_rows(dev, ref, weights):
+    """Keys that no registers hold: random weights, every kept row moved in several
+    lists, and weights of few values."""
+    _case("evict long", weights)
+    rng = np.random.default_rng(35)
+    make = {"random": None, "few": lambda s: rng.integers(0, 3, s).astype(np.float32),
+            "rising": lambda s: np.broadcast_to(np.arange(s[-1], dtype=np.float32), s).copy()}[weights]
+    _evict(dev, ref, rng, "bf16", [90000, 70001], 34000, 1, 8, 64, make, recent=0 if weights == "rising" else 500)
+
+
+@pytest.mark.parametrize("kind,cache,page", [("f32", "bf16", 16), ("bf16", "f16", 64), ("f32", "i8", 12)])
+@pytest.mark.parametrize("weights", [False, True])
+def test_attend_in_tables_far_wider_than_the_sequences(dev, ref, kind, cache, page, weights):
+    _case("attend wide", kind, cache, page, weights)
+    rng = np.random.default_rng(36)
+    lens = [300, 1, 0, 65, 2100, 64]
+    c = ref.Cache(rng, 6, 40000 // page, 2, page, 64, cache)
+    q = rng.standard_normal((6, 8, 64)).astype(np.float32)
+    w = np.zeros((6, 2, c.rows), np.float32) if weights else None
+    Attend(dev, ref, c, q, kind, lens, weight=w).check(ref)
