@@ -614,7 +614,8 @@ typedef struct sherry_append_desc {
  * or with SHERRY_I8 quantized per row as sherry_quantize_act does (s = absmax
  * / 127, clamp(rint(x / s), -127, 127); a zero row gives 0 and 0).  A token
  * whose seq, slot, page or (with cos) pos is out of range is left out
- * entirely.  No two tokens may have the same seq and slot.  Input rows are
+ * entirely.  No two tokens may have the same seq and slot, or, through pages that
+ * sequences share, the same row of a page.  Input rows are
  * aligned to their element.  cache->table and the rows that exist are not
  * changed; lengths are the caller's.  Calls of 2^32 threads and more are refused
  * (SHERRY_E_SHAPE): a token takes 256 for every 16 rows of q, k and v of up to 64
@@ -696,7 +697,11 @@ typedef struct sherry_evict_desc {
  * counts as -infinity).  Kept rows in slots below the new length stay where
  * they are; those past it move, in ascending order, into the slots below it
  * that were given up, so the cache is compacted in place with the fewest
- * moves, and pages past ceil(length_out / page_size) are free.  k, v and the
+ * moves, and pages past ceil(length_out / page_size) are free.  A page that a
+ * sequence of more than keep rows reaches must not stand anywhere else in the table:
+ * its rows move for every sequence that reads it.  (Attention may share pages;
+ * a shared prefix is copied to pages of its own before its sequences are cut down.)
+ * k, v and the
  * scales are moved in the pages (a move from or to an absent page is left
  * out); weight and position are only read, and no output may overlap them.  batch *
  * kv_heads is at most 2^22 - 1, and batch * kv_heads * ceil(keep / R) + batch *
