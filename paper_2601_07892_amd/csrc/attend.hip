@@ -126,26 +126,37 @@ __device__ __forceinline__ Span span_of(const Attend& a, int b) {
 }
 
 // What a sequence costs a workgroup besides its tiles (finding it, its q, the
-// first loads, the sums' way out), in tiles.  Without it a workgroup that
-// gets many short sequences ends the launch (32 sequences of 0 to 8000 rows:
-// 31.8 us without, 29.7 with 3, 27.9 with 6, 27.8 with 10).
-constexpr int kSequence = 6;
-__device__ __forceinline__ int cost_of(int tiles) { return tiles ? tiles + kSequence : 0; }
+// first loads, the sums' way out), in tiles of a cache type and padded head size: a
+// workgroup that gets many short sequences would else end the launch.  Mean time with
+// 0 / 3 / 8 / 10 / 16 / 24 / 32 tiles over that with 6, of four ragged batches each (32
+// sequences of 1 to 8000 rows, 48 of 400 to 4000, 16 of 1 to 30000, 64 of 10 to 1500):
+//   int8  64 values 1.64 / 1.03 / 0.99 / 1.00 / 0.95 / 0.99 / 1.01
+//        128        1.79 / 1.15 / 0.94 / 0.95 / 0.90 / 0.96 / 1.04
+//        256        1.70 / 1.25 / 0.93 / 0.86 / 0.83 / 0.83 / 0.87
+//   bf16  64        1.53 / 1.00 / 1.00 / 1.03 / 1.06 / 1.09 / 1.10
+//        128        1.70 / 1.14 / 1.00 / 1.03 / 1.06 / 1.15 / 1.23
+//        256        1.76 / 1.23 / 0.95 / 0.96 / 1.03 / 1.12 / 1.20
+// and f16 within 0.02 of bf16.
+constexpr int sequence_cost(int type, int dp) { return type == SHERRY_I8 ? 16 : dp == 256 ? 8 : 6; }
 
 // Each workgroup column takes `run` of the sequences' costs, one after the
-// other; a sequence's first kSequence units are no tiles.
+// other; a sequence's first SEQ units (sequence_cost) are no tiles.
 struct Place {
   int b, at;  // sequence, and the unit of its cost, where a column starts; b = -1: nowhere
   int run;
 };
+template <int SEQ>
 __device__ __forceinline__ Place find_place(const Attend& a, int w) {
   const int lane = threadIdx.x & 63;
-  auto cost = [&](int b) { return b < a.c.batch ? cost_of(span_of(a, b).tiles()) : 0; };
+  auto cost = [&](int b) {
+    const int tiles = b < a.c.batch ? span_of(a, b).tiles() : 0;
+    return tiles ? tiles + SEQ : 0;
+  };
   const int n0 = cost(lane), upto0 = wave_scan(n0);
   int total = __builtin_amdgcn_readlane(upto0, 63);
   for (int b = 64; b < a.c.batch; b += 64)
     total += __builtin_amdgcn_readlane(wave_scan(cost(b + lane)), 63);
-  int run = (total + a.columns - 1) / a.columns;
+  int run = static_cast<int>((static_cast<uint32_t>(total) + a.columns - 1) / a.columns);
   run = run < kMinTiles ? kMinTiles : run;
   const int64_t start = int64_t(w) * run;
   if (start >= total) return Place{-1, 0, run};
@@ -279,7 +290,7 @@ __host__ __device__ constexpr int waves_for(int dp) { return dp == 64 ? 3 : dp =
 template <int CT_, int QT_, int NT_, int DP_, bool ANY_, bool MORE_>
 struct Cfg {
   static constexpr int CT = CT_, QT = QT_, NT = NT_, DP = DP_;
-  static constexpr int EU = waves_for(DP);
+  static constexpr int EU = waves_for(DP), SEQ = sequence_cost(CT, DP);
   static constexpr bool ANY = ANY_, MORE = MORE_, F16 = CT != SHERRY_BF16, I8 = CT == SHERRY_I8;
   static constexpr int E = I8 ? 1 : 2;         // bytes per value
   static constexpr int KS = DP / 32;           // MFMA steps of a score
@@ -619,7 +630,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // (uniform values, which the compiler does not see through the wave's sums)
-  const Place place = a.whole ? Place{static_cast<int>(blockIdx.y), 0, 1 << 30} : find_place(a, blockIdx.y);
+  const Place place = a.whole ? Place{static_cast<int>(blockIdx.y), 0, 1 << 30} : find_place<G::SEQ>(a, blockIdx.y);
   const int b_first = __builtin_amdgcn_readfirstlane(place.b);
   if (b_first < 0) return;
   const int h = blockIdx.x / a.gtiles, gt = blockIdx.x - h * a.gtiles;
@@ -634,9 +645,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
     const int end = __builtin_amdgcn_readfirstlane(sp.end);
     const int tiles = __builtin_amdgcn_readfirstlane(sp.tiles());
     // units [at_cost, upto) of the sequence's cost: the tiles among them
-    const int upto = tiles + kSequence < at_cost + left ? tiles + kSequence : at_cost + left;
+    const int upto = tiles + G::SEQ < at_cost + left ? tiles + G::SEQ : at_cost + left;
     left = a.whole ? 0 : left - (upto - at_cost);
-    const int n0 = at_cost > kSequence ? at_cost - kSequence : 0, n1 = upto - kSequence;
+    const int n0 = at_cost > G::SEQ ? at_cost - G::SEQ : 0, n1 = upto - G::SEQ;
     if (n1 <= n0) {  // the run ends before the first tile; or there are none
       if (a.whole)
         for (int i = threadIdx.x; i < heads * a.c.dim; i += 64 * kWaves)
@@ -1065,7 +1076,7 @@ Shape shape_of(const sherry_cache_desc& c, const sherry_attend_desc& d) {
   const int64_t rows = int64_t(c.table_width) * c.page_size, tiles = ceil_div(rows, kTile);
   // as many workgroups as run at once, but no more than full sequences make
   const int64_t groups = kCus * waves_for(dp), fit = y >= groups ? 1 : groups / y;
-  const int64_t most = ceil_div(c.batch * (tiles + kSequence), kMinTiles);
+  const int64_t most = ceil_div(c.batch * (tiles + sequence_cost(c.type, dp)), kMinTiles);
   s.whole = !d.weight && tiles <= kWholeTiles;
   s.columns = s.whole ? c.batch : static_cast<int>(most < fit ? most : fit);
   auto up = [](int64_t n) { return static_cast<size_t>((n + 255) / 256 * 256); };

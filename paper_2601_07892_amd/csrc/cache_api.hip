@@ -88,7 +88,7 @@ int check_attend_shape(const sherry_cache_desc* c, const sherry_attend_desc* a) 
   if ((a->mask && a->mask_stride < cache_rows(c)) ||
       ((a->position || a->weight) && a->row_stride < cache_rows(c)))
     return SHERRY_E_SHAPE;
-  // (all rows in tiles of 32, and a few more per sequence, are counted in 32 bits)
+  // (all rows in tiles of 32, and up to 16 more per sequence, are counted in 31 bits)
   if (int64_t(c->batch) * (ceil_div(cache_rows(c), 32) + 16) > INT32_MAX) return SHERRY_E_SHAPE;
   if (!fits_grid(attend_threads(*c, *a))) return SHERRY_E_SHAPE;
   return SHERRY_OK;
