@@ -12,7 +12,7 @@
 //
 // Measured: 32 tokens of 24 + 16 heads of 128 values into f16 3.2 us, a launch's
 // latency with two dependent reads; a prompt of 2048 tokens of 32 + 16 heads of 64
-// values into int8, 45 MB, 11.6 to 12.8 us, 3.6 TB/s (the inputs are partly
+// values into int8, 45 MB, 11.6 to 13.0 us, 3.5 to 3.9 TB/s (the inputs are partly
 // in the caches).  With rows of any token in a workgroup and the types as
 // arguments these took 3.6 and 14.5; several rows per thread were slower.
 #include "cache_internal.h"

@@ -33,8 +33,8 @@
 // are, of V as f16 integers; their scales are applied to the scores and the
 // probabilities).  q and p are split into terms of bf16 (or, for f16 caches and p
 // over int8 V, f16) whose products are summed in fp32: three bf16 terms hold all 24
-// bits, two 16; two f16 terms 22 (p is scaled by 2^14 over the largest scale of V
-// so far, so that its low term stays normal).  Over bf16 caches p takes three (with
+// bits, two f16 terms 22 (p is scaled by 2^14 over the largest scale of V so far, so
+// that its low term stays normal).  Over bf16 caches p takes three (with
 // two the outputs of bf16 q were 1e-5 off before their own rounding) and q as many
 // as hold it: one of bf16, two of f16, three of fp32.  Over f16 caches both take
 // two.  Over int8 K q is three int8 digits, rounded at 2^-22 of its
@@ -47,14 +47,14 @@
 //  * 4 sequences of 130000 rows, 32 query heads over 8 of 128 bf16 values, 2.13
 //    GB: 322 us and 5 for the join, 6.6 TB/s of the first.  94% of that read.
 //  * 32 sequences of 0 to 8000 rows, 24 heads over 8 of 128 f16 values, 119 MB:
-//    27 us and 4.6.  Sequences of one length of the same bytes take 23; the rest is
-//    those that begin and end inside a run.
+//    27 us and 4.6.  One to eight sequences of one length and the same bytes take
+//    23.5, 32 of 910 rows 27: the rest is sequences that begin and end inside a run.
 //  * 16 sequences of 2000 to 9000 rows, 32 heads over 8 of 128 int8 values, a
-//    window, a mask and weights: 43 us and 7.1, without the three 35.  Some 10 us are
+//    window, a mask and weights: 40 us and 7.2, without the three 33.  Some 10 us are
 //    a workgroup's beginning and end; conversions of V, scales, masks and stored
 //    scores make more than twice the vector instructions per byte of the case before.
-//    64 sequences of 4000 rows, 0.54 GB, without them: 100 to 104 us, 5.3 TB/s.
-//  * one sequence of 300 rows: 7.0 us in one launch, all of it latency (length, table,
+//    64 sequences of 4000 rows, 0.54 GB, without them: 98 to 104 us, 5.2 to 5.5 TB/s.
+//  * one sequence of 300 rows: 7.2 to 7.7 us in one launch, all of it latency (length, table,
 //    K, V, and the waves' sums, each after the other).
 #include <type_traits>
 
@@ -73,8 +73,8 @@ constexpr int kWaves = 4;
 constexpr int kMinTiles = kWaves;  // tiles of the shortest run: one per wave
 // Up to this many tiles of capacity a workgroup takes a sequence whole, and
 // nothing is left to join (one sequence of 300 rows of 8 heads: 64 values 7.3 us
-// against 6.3 and 3.0 for the join, 128 values 10.7 against 8.6 and 3.4; of 600
-// rows 14.4 against 8.6 and 3.4, so no further).
+// against 6.3 and 3.0 for the join, 128 values 11.5 against 8.6 and 3.4; of 600
+// rows 14.4 against 9.0 and 3.1, so no further).
 constexpr int kWholeTiles = 16;
 constexpr int kCus = 256;
 constexpr int kTile = 32;          // rows per wave and step
@@ -283,10 +283,10 @@ __host__ __device__ constexpr int waves_for(int dp) { return dp == 64 ? 3 : dp =
 // lies in one page and its rows are read through one buffer resource).
 // MORE: mask, position or weight are given.
 // What each buys, against the general form on the same input: pages of multiples of
-// 16 rows 7.3 us against 8.4 (one sequence of 300 rows), 320 against 327 (4 of
-// 130000), 61 against 70 (16 of 4000 to 8000, 256 values), 65 against 95 (64 of
-// 4000, int8, 64 values); no mask, position or weight 26.8 against 29.0 (32 short
-// ones), 7.0 against 7.9 (the one of 300 rows).
+// 16 rows 7.5 us against 8.4 (one sequence of 300 rows), 321 against 330 (4 of
+// 130000), 61 against 68 (16 of 4000 to 8000, 256 values), 61 against 95 (64 of
+// 4000, int8, 64 values); no mask, position or weight 27.1 against 28.8 (32 short
+// ones), 7.5 against 8.2 (the one of 300 rows), 61 against 72 (the 64 of int8).
 template <int CT_, int QT_, int NT_, int DP_, bool ANY_, bool MORE_>
 struct Cfg {
   static constexpr int CT = CT_, QT = QT_, NT = NT_, DP = DP_;

@@ -210,12 +210,13 @@ __device__ __forceinline__ bool epi_pieces(const Epi& e) {
 //
 // A gate or residual has y's size, and is read where y's strip is written, once: the
 // product's tail gets longer by that read, and y is not written and read again.
-// 2048 x 14336 x 4096, silu and gate: 131 to 133 us in a loop of calls, where the
-// product alone takes 109 to 114 and the gate's 117 MB 17 at the rate of a
-// streaming read; one block read ahead, since the registers hold no more (269 us
-// with the reads in the block that uses them, their code in a loop).  16 x 2048 x
-// 8192 with group scales, bias and residual 12.5, the product alone 12.1; 37 x
-// 300 x 1204 6.6, a launch's latency.
+// 2048 x 14336 x 4096, silu and gate, on three sets of tensors in turn: 172 us (the
+// fastest call 151), where the product alone takes 129 to 138 (112) and the gate's
+// 117 MB 17 at the rate of a streaming read; over one set in a loop, whose gate is
+// partly in the caches, 131 and 109.  One block is read ahead, since the registers
+// hold no more (269 us with the reads in the block that uses them, their code in a
+// loop).  16 x 2048 x 8192 with group scales, bias and residual 13, the product alone
+// 12.5; 37 x 300 x 1204 6.8 and 6.0, a launch's latency.
 template <class E, int PN>
 struct WdExtra;
 template <int PN>
