@@ -634,7 +634,7 @@ typedef struct sherry_attend_desc {
   const uint8_t* mask;   /* device, [batch][mask_stride], or NULL: rows with  */
                          /* 0 are left out for every head                     */
   const int32_t* position; /* device, int32 [batch][kv_heads][row_stride], or */
-                         /* NULL: what window goes by                         */
+                         /* NULL: what window goes by, values > INT32_MIN     */
   const int32_t* q_pos;  /* device, int32 [batch]: the token's own position   */
                          /* (needed with position and window)                 */
   float* weight;         /* device, fp32 [batch][kv_heads][row_stride], or    */

@@ -358,7 +358,7 @@ struct Rows {
   int b, h, begin, end;
   const uint8_t* mask = nullptr;      // of b; NULL: not given
   const int32_t* position = nullptr;  // of b and h; NULL: no window by them
-  int qmin = 0;                       // rows with position <= qmin are left out
+  int qmin = 0;                       // rows with position <= qmin are left out (at least INT32_MIN)
   // the tile whose look-up finished last
   uint32_t valid = 0;       // bit r: row r of the tile is attended to
   int rows[2] = {0, 0};     // !ANY: rows of each half that are read
@@ -377,7 +377,8 @@ struct Rows {
       if (a.mask) mask = a.mask + int64_t(b) * a.mask_stride;
       if (a.position && a.window) {
         position = a.position + (int64_t(b) * a.c.kv + h) * a.row_stride;
-        qmin = as_const(a.q_pos)[b] - a.window;
+        const int64_t from = int64_t(as_const(a.q_pos)[b]) - a.window;
+        qmin = static_cast<int>(from < INT32_MIN ? INT32_MIN : from);
       }
     }
   }

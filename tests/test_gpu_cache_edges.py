@@ -217,3 +217,19 @@ def test_attend_in_tables_far_wider_than_the_sequences(dev, ref, kind, cache, pa
     q = rng.standard_normal((6, 8, 64)).astype(np.float32)
     w = np.zeros((6, 2, c.rows), np.float32) if weights else None
     Attend(dev, ref, c, q, kind, lens, weight=w).check(ref)
+
+
+@pytest.mark.parametrize("window", [1, 70, 2 ** 31 - 1])
+def test_attend_windows_at_the_ends_of_32_bits(dev, ref, window):
+    """Positions and windows whose difference does not fit 32 bits."""
+    _case("attend window ends", window)
+    rng = np.random.default_rng(38)
+    lens = [100, 100, 40, 100, 33]
+    c = ref.Cache(rng, 5, 7, 2, 16, 64, "bf16")
+    position = rng.integers(-2 ** 31 + 1, 2 ** 31, (5, 2, c.rows)).astype(np.int32)
+    position[:, :, ::3] = rng.integers(-200, 200, position[:, :, ::3].shape)
+    position[3, :, ::5] = 2 ** 31 - 1
+    q_pos = np.array([-5, -2 ** 31, -1, 2 ** 31 - 1, 60], np.int32)
+    q = rng.standard_normal((5, 4, 64)).astype(np.float32)
+    w = np.zeros((5, 2, c.rows), np.float32)
+    Attend(dev, ref, c, q, "f32", lens, window, position=position, q_pos=q_pos, weight=w).check(ref)
