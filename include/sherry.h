@@ -550,6 +550,10 @@ int sherry_gemv_f32_epilogue(const uint8_t* w, const float* x, float* x_scale,
 #define SHERRY_F16 1
 #define SHERRY_BF16 2
 #define SHERRY_I8 3 /* caches only: int8 rows with one fp32 scale per row     */
+#define SHERRY_F8 4 /* caches only: e4m3 codes (3 bits behind the first, -+448, */
+                    /* 0x7F and 0xFF NaN) with a power of two per page and    */
+                    /* head: sherry_cache_extend, _attend, _attend_tokens,    */
+                    /* _fork and _compact take them                           */
 
 #define SHERRY_MAX_HEAD_DIM 256
 #define SHERRY_MAX_CACHE_ROWS (1LL << 30) /* table_width * page_size          */
@@ -557,19 +561,22 @@ int sherry_gemv_f32_epilogue(const uint8_t* w, const float* x, float* x_scale,
 typedef struct sherry_cache_desc {
   void* k;               /* device, [pages][kv_heads][page_size][head_dim],   */
   void* v;               /* of type, 16-byte aligned                          */
-  float* k_scale;        /* device, fp32 [pages][kv_heads][page_size], 16-    */
-  float* v_scale;        /* byte aligned, with SHERRY_I8; else NULL           */
+  float* k_scale;        /* device, fp32 [pages][kv_heads][page_size] with    */
+  float* v_scale;        /* SHERRY_I8, [pages][kv_heads] with SHERRY_F8 (of   */
+                         /* which the exponent alone counts, 2^-126 .. 2^127; */
+                         /* what a code stands for is times it), 16-byte      */
+                         /* aligned; else NULL                                */
   const int32_t* table;  /* device, int32 [batch][table_width]: page of each  */
                          /* page_size rows.  An entry outside [0, pages) that */
                          /* a sequence's length reaches makes its rows absent */
   int64_t page_stride;   /* elements from page to page in k and v, a multiple */
-                         /* of 8 (SHERRY_I8: 16) and at least kv_heads *      */
+                         /* of 8 (SHERRY_I8, _F8: 16) and at least kv_heads * */
                          /* page_size * head_dim; 0: exactly that             */
-  int32_t type;          /* SHERRY_F16, SHERRY_BF16 or SHERRY_I8              */
+  int32_t type;          /* SHERRY_F16, SHERRY_BF16, SHERRY_I8 or SHERRY_F8   */
   int32_t pages;         /* >= 1                                              */
   int32_t kv_heads;      /* 1 .. 4096                                         */
   int32_t page_size;     /* >= 1                                              */
-  int32_t head_dim;      /* a multiple of 8 (SHERRY_I8: 16), 8 .. 256         */
+  int32_t head_dim;      /* a multiple of 8 (SHERRY_I8, _F8: 16), 8 .. 256    */
   int32_t batch;         /* sequences, 1 .. 65535                             */
   int32_t table_width;   /* >= 1; table_width * page_size <=                  */
                          /* SHERRY_MAX_CACHE_ROWS                             */
@@ -617,7 +624,8 @@ typedef struct sherry_append_desc {
  * entirely.  No two tokens may have the same seq and slot, or, through pages that
  * sequences share, the same row of a page.  Input rows are
  * aligned to their element.  cache->table and the rows that exist are not
- * changed; lengths are the caller's.  Calls of 2^32 threads and more are refused
+ * changed; lengths are the caller's.  SHERRY_F8 caches, where a row's power of two
+ * is its page's, are sherry_cache_extend's (SHERRY_E_INVALID here).  Calls of 2^32 threads and more are refused
  * (SHERRY_E_SHAPE): a token takes 256 for every 16 rows of q, k and v of up to 64
  * values, 8 of up to 128, 4 of more. */
 int sherry_cache_append(const sherry_cache_desc* cache, const sherry_append_desc* args,
@@ -667,7 +675,7 @@ size_t sherry_cache_attend_workspace(const sherry_cache_desc* cache,
  * out never reach the result, whatever they hold; a NaN or an infinity in the
  * others makes the results that it enters NaN or infinite.  Scores, statistics and
  * sums are in fp32; the products keep q and the probabilities to 22 bits and more
- * (over f16 and int8 caches of a head's largest value). */
+ * (over f16, int8 and e4m3 caches of a head's largest value). */
 int sherry_cache_attend(const sherry_cache_desc* cache, const sherry_attend_desc* args,
                         void* stream);
 
@@ -700,7 +708,9 @@ typedef struct sherry_evict_desc {
  * moves, and pages past ceil(length_out / page_size) are free.  A page that a
  * sequence of more than keep rows reaches must not stand anywhere else in the table:
  * its rows move for every sequence that reads it.  (Attention may share pages;
- * a shared prefix is copied to pages of its own before its sequences are cut down.)
+ * a shared prefix is copied to pages of its own before its sequences are cut down:
+ * sherry_cache_fork with from_row 0.)  SHERRY_F8 caches, whose rows share a power of
+ * two with their page, are not cut (SHERRY_E_INVALID).
  * k, v and the
  * scales are moved in the pages (a move from or to an absent page is left
  * out); weight and position are only read, and no output may overlap them.  batch *
@@ -709,6 +719,171 @@ typedef struct sherry_evict_desc {
  * of up to 128, 64 of up to 256, else 32 (SHERRY_E_SHAPE). */
 int sherry_cache_evict(const sherry_cache_desc* cache, const sherry_evict_desc* args,
                        void* stream);
+
+/* New tokens of a ragged batch into a SHERRY_F8 cache: any number for each
+ * sequence, behind the rows that it has. */
+typedef struct sherry_extend_desc {
+  const void* q;         /* device, [tokens][heads][head_dim] of type, or     */
+                         /* NULL (heads is then ignored)                      */
+  const void* k;         /* device, [tokens][kv_heads][head_dim] of type      */
+  const void* v;         /* device, as k                                      */
+  void* q_out;           /* device, as q: q rotated, as sherry_append_desc    */
+  const int32_t* first;  /* device, int32 [batch + 1], ascending: tokens      */
+                         /* first[b] .. first[b + 1] - 1 are sequence b's     */
+  const int32_t* length; /* device, int32 [batch]: the rows that each has     */
+                         /* (below 0: none); its tokens go to the rows behind */
+  const int32_t* pos;    /* device, int32 [tokens]: rotary positions, or      */
+                         /* NULL: a token's row                               */
+  const float* cos;      /* device, fp32 [rope_rows][rot_dim / 2], or both    */
+  const float* sin;      /* NULL: no rotation                                 */
+  int64_t q_stride, k_stride, v_stride, q_out_stride; /* elements from token  */
+                         /* to token; 0: contiguous                           */
+  int32_t tokens;        /* 1 .. SHERRY_MAX_M                                 */
+  int32_t heads;         /* 1 .. 256 * 4096                                   */
+  int32_t type;          /* of q, k, v and q_out: SHERRY_F32, _F16 or _BF16   */
+  int32_t rope_rows;     /* positions in cos and sin                          */
+  int32_t rot_dim;       /* even, 2 .. head_dim; later values are not rotated */
+  int32_t pairing;       /* SHERRY_ROPE_HALVES or SHERRY_ROPE_PAIRS           */
+} sherry_extend_desc;
+
+/* Rotates q and k as sherry_cache_append does, writes q_out, and stores k and v
+ * as codes.  For each page and head that gets rows, need = 2^e with the smallest
+ * e >= -100 that has every finite new value within 448 * 2^e.  A page that begins
+ * at or behind a sequence's length holds nothing yet: its power becomes need.
+ * Otherwise it becomes the larger of need and what it was, and when it rises, the
+ * codes of the page's other rows become the nearest e4m3 values of code * old /
+ * new (so that a row rounded several times is off by at most the sum of steps that
+ * halve from one to the next).  A new code is the e4m3 value nearest to value /
+ * power, ties to even; infinities and NaN become NaN.  A token whose row (or, with
+ * cos, position) is out of range, or whose page does not exist, is left out
+ * entirely, tokens outside first[0] .. first[batch] - 1 too.  No page that gets rows
+ * may belong to another sequence (sherry_cache_fork sees to that); lengths are the
+ * caller's.  Calls of 2^32 threads and more are refused (SHERRY_E_SHAPE): about
+ * 256 for every 16 heads of a token's q and for every 2 heads of a page's k and v,
+ * tokens / page_size + 2 batch pages. */
+int sherry_cache_extend(const sherry_cache_desc* cache, const sherry_extend_desc* args,
+                        void* stream);
+
+/* Attention of any number of new tokens per sequence over a SHERRY_F8 cache that
+ * has their rows already: prompts, chunks of them, drafts. */
+typedef struct sherry_attend_tokens_desc {
+  const void* q;         /* device, [tokens][heads][head_dim] of type, 16-    */
+                         /* byte aligned; query head i reads key-value head   */
+                         /* i / (heads / kv_heads)                            */
+  void* out;             /* device, as q; may not overlap it                  */
+  const int32_t* first;  /* device, int32 [batch + 1], as sherry_extend_desc  */
+  const int32_t* length; /* device, int32 [batch]: the rows that each         */
+                         /* sequence had before these tokens                  */
+  const uint8_t* mask;   /* device, [batch][mask_stride], or NULL: rows with  */
+                         /* 0 are left out for every head and token           */
+  void* workspace;       /* device, 16-byte aligned, workspace_bytes >=       */
+  size_t workspace_bytes;/* sherry_cache_attend_tokens_workspace; its         */
+                         /* contents do not matter                            */
+  int64_t q_stride, out_stride; /* elements from token to token, a multiple   */
+                         /* of 8; 0: contiguous                               */
+  int64_t mask_stride;   /* >= table_width * page_size where used             */
+  int32_t tokens;        /* 1 .. SHERRY_MAX_M                                 */
+  int32_t heads;         /* a multiple of kv_heads, at most 256 times it      */
+  int32_t type;          /* of q and out: SHERRY_F32, _F16 or _BF16           */
+  int32_t window;        /* 0: all rows; else the last window rows            */
+  float scale;           /* of the scores, e.g. head_dim ^ -1/2               */
+  int32_t reserved;      /* set to 0                                          */
+} sherry_attend_tokens_desc;
+
+/* Bytes of workspace that sherry_cache_attend_tokens needs with these
+ * descriptors (host only; pointers in them are only compared with NULL); 0 if
+ * they are invalid. */
+size_t sherry_cache_attend_tokens_workspace(const sherry_cache_desc* cache,
+                                            const sherry_attend_tokens_desc* args);
+
+/* Token i of sequence b (i = 0 for token first[b]) attends to the rows r <=
+ * length[b] + i of the table, of these with window to r > length[b] + i - window.
+ * Rows and pages that are left out, outputs of nothing, NaN and infinities are as
+ * in sherry_cache_attend; tokens of no sequence are not written.  Scores,
+ * statistics and sums are in fp32; q is kept to 22 bits of its head's largest
+ * value.  The probabilities are rounded to 22 bits for fp32 outputs; for bf16 and
+ * f16 outputs to the 11 of f16, which moves an output by at most 2^-11 sum_r p_r
+ * |v_r| before its own rounding.  tokens * heads < 2^31 (SHERRY_E_SHAPE). */
+int sherry_cache_attend_tokens(const sherry_cache_desc* cache,
+                               const sherry_attend_tokens_desc* args, void* stream);
+
+/* ---------------------------------------------------------------------- */
+/* Pages that sequences share.  A page is in use when a sequence reaches   */
+/* it: when it stands in table[b][j] for a j < ceil(length[b] / page_size).*/
+/* Nothing else is kept about pages, so a sequence of length 0, or one cut */
+/* shorter, has given its pages back.                                      */
+/* The layers of a model whose pools follow each other at fixed strides    */
+/* share one table; cache has the first layer's pools.                     */
+/* ---------------------------------------------------------------------- */
+
+typedef struct sherry_fork_desc {
+  const int32_t* parent; /* device, int32 [batch]: the sequence that b goes   */
+                         /* on from, b itself included (outside [0, batch):   */
+                         /* b is empty), or NULL: each from itself            */
+  const int32_t* length; /* device, int32 [batch]: the sequences' rows before */
+                         /* the call (below 0: none; past the table: all)     */
+  const int32_t* add;    /* device, int32 [batch]: rows that b will get       */
+                         /* (below 0: none), or NULL: none                    */
+  const int32_t* from_row; /* device, int32 [batch]: the first row of b that  */
+                         /* will be written (below 0: 0; past its rows: the   */
+                         /* one behind them), or NULL: the one behind them    */
+  int32_t* table_out;    /* device, int32 [batch][table_width]; with parent   */
+                         /* NULL it may be cache->table, and may not overlap  */
+                         /* it otherwise                                      */
+  int32_t* length_out;   /* device, int32 [batch]: the rows of each sequence, */
+                         /* without add; may not be length                    */
+  int32_t* missing;      /* device, int32 [1]: 0, or by how many pages the    */
+                         /* free ones fall short: nothing else is written then*/
+  void* workspace;       /* device, 16-byte aligned, workspace_bytes >=       */
+  size_t workspace_bytes;/* sherry_cache_fork_workspace; its contents do not  */
+                         /* matter                                            */
+  int64_t layer_stride;  /* elements from a layer's k and v to the next's, a  */
+                         /* multiple of 8 (SHERRY_I8, _F8: 16), >= pages *    */
+                         /* page_stride where layers > 1                      */
+  int64_t scale_layer_stride; /* the same for k_scale and v_scale, >= their   */
+                         /* elements in a layer                               */
+  int32_t layers;        /* 1 .. 65535                                        */
+  int32_t reserved;      /* set to 0                                          */
+} sherry_fork_desc;
+
+size_t sherry_cache_fork_workspace(const sherry_cache_desc* cache, const sherry_fork_desc* args);
+
+/* Sequence b goes on from parent[b]: it takes that one's rows and pages, which
+ * the two then share, and gets pages of its own for the rows that will be written,
+ * from_row[b] .. length_out[b] + add[b] - 1 (as far as the table goes).  Of these
+ * rows' pages, those that do not exist yet are free ones; one that stands elsewhere
+ * in the new table too is copied to a free one, with its scales and in every layer,
+ * unless all the places where it stands are written: then the last of them (the
+ * highest b, then the highest place) keeps it.  Free pages are those that no new
+ * sequence reaches; they are given out from the lowest, to the places in order.
+ * Entries of table_out behind a sequence's last page, and of pages outside [0,
+ * pages), are -1.  Any sequence may be the parent of any number of others.
+ * batch * table_width < 2^31 (SHERRY_E_SHAPE). */
+int sherry_cache_fork(const sherry_cache_desc* cache, const sherry_fork_desc* args, void* stream);
+
+typedef struct sherry_compact_desc {
+  const int32_t* length; /* device, int32 [batch], as sherry_fork_desc        */
+  int32_t* table_out;    /* device, int32 [batch][table_width]; may be        */
+                         /* cache->table, and may not overlap it otherwise    */
+  int32_t* moved;        /* device, int32 [pages]: where each page is now, -1 */
+                         /* of pages that are free; or NULL                   */
+  int32_t* live;         /* device, int32 [1]: pages in use                   */
+  void* workspace;       /* as sherry_fork_desc, of                           */
+  size_t workspace_bytes;/* sherry_cache_compact_workspace bytes              */
+  int64_t layer_stride, scale_layer_stride; /* as sherry_fork_desc            */
+  int32_t layers;        /* 1 .. 65535                                        */
+  int32_t reserved;      /* set to 0                                          */
+} sherry_compact_desc;
+
+size_t sherry_cache_compact_workspace(const sherry_cache_desc* cache, const sherry_compact_desc* args);
+
+/* Moves the pages in use to the front of the pool, with the fewest moves: of `live`
+ * pages those in [0, live) stay, the others go, in ascending order, to the free
+ * places before live, with their scales and in every layer.  Pages from live on
+ * can then be given back.  Entries of table_out behind a sequence's last page, and
+ * of pages outside [0, pages), are -1.  batch * table_width < 2^31 (SHERRY_E_SHAPE). */
+int sherry_cache_compact(const sherry_cache_desc* cache, const sherry_compact_desc* args,
+                         void* stream);
 
 /* ---------------------------------------------------------------------- */
 /* Diagnostics.                                                            */

@@ -36,7 +36,7 @@ SHERRY_MAX_M = 1 << 24
 SHERRY_FUSED_MAX_K = 32768
 SHERRY_ACT_NONE, SHERRY_ACT_RELU, SHERRY_ACT_RELU2 = 0, 1, 2
 SHERRY_ACT_SILU, SHERRY_ACT_GELU, SHERRY_ACT_GELU_TANH = 3, 4, 5
-SHERRY_F32, SHERRY_F16, SHERRY_BF16, SHERRY_I8 = 0, 1, 2, 3
+SHERRY_F32, SHERRY_F16, SHERRY_BF16, SHERRY_I8, SHERRY_F8 = 0, 1, 2, 3, 4
 SHERRY_ROPE_HALVES, SHERRY_ROPE_PAIRS = 0, 1
 SHERRY_MAX_HEAD_DIM = 256
 SHERRY_MAX_CACHE_ROWS = 1 << 30
@@ -56,7 +56,9 @@ EXPORTS = [
     "sherry_gemv_f32_il_batched_prepare", "sherry_gemv_f32_il_batched",
     "sherry_gemm_il_batched_prepare", "sherry_gemm_il_batched", "sherry_interleave",
     "sherry_gemm_epilogue", "sherry_gemv_f32_epilogue", "sherry_cache_append",
-    "sherry_cache_attend_workspace", "sherry_cache_attend", "sherry_cache_evict",
+    "sherry_cache_attend_workspace", "sherry_cache_attend", "sherry_cache_evict", "sherry_cache_extend",
+    "sherry_cache_attend_tokens_workspace", "sherry_cache_attend_tokens", "sherry_cache_fork_workspace",
+    "sherry_cache_fork", "sherry_cache_compact_workspace", "sherry_cache_compact",
 ]
 
 
@@ -160,6 +162,50 @@ class sherry_evict_desc(ctypes.Structure):
     ]
 
 
+class sherry_extend_desc(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("q_out", ctypes.c_void_p), ("first", ctypes.c_void_p), ("length", ctypes.c_void_p),
+        ("pos", ctypes.c_void_p), ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64),
+        ("tokens", ctypes.c_int32), ("heads", ctypes.c_int32), ("type", ctypes.c_int32),
+        ("rope_rows", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("pairing", ctypes.c_int32),
+    ]
+
+
+class sherry_attend_tokens_desc(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("first", ctypes.c_void_p),
+        ("length", ctypes.c_void_p), ("mask", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t), ("q_stride", ctypes.c_int64),
+        ("out_stride", ctypes.c_int64), ("mask_stride", ctypes.c_int64),
+        ("tokens", ctypes.c_int32), ("heads", ctypes.c_int32), ("type", ctypes.c_int32),
+        ("window", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+    ]
+
+
+class sherry_fork_desc(ctypes.Structure):
+    _fields_ = [
+        ("parent", ctypes.c_void_p), ("length", ctypes.c_void_p), ("add", ctypes.c_void_p),
+        ("from_row", ctypes.c_void_p), ("table_out", ctypes.c_void_p),
+        ("length_out", ctypes.c_void_p), ("missing", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("layer_stride", ctypes.c_int64), ("scale_layer_stride", ctypes.c_int64),
+        ("layers", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class sherry_compact_desc(ctypes.Structure):
+    _fields_ = [
+        ("length", ctypes.c_void_p), ("table_out", ctypes.c_void_p), ("moved", ctypes.c_void_p),
+        ("live", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t), ("layer_stride", ctypes.c_int64),
+        ("scale_layer_stride", ctypes.c_int64), ("layers", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
 def _load():
     # torch ships its own HIP runtime (same SONAME as the system's).  Loading
     # torch first makes libsherry bind to that runtime instead of mapping a
@@ -243,6 +289,23 @@ def _load():
                                  ctypes.POINTER(sherry_attend_desc), vp], ctypes.c_int),
         "sherry_cache_evict": ([ctypes.POINTER(sherry_cache_desc),
                                 ctypes.POINTER(sherry_evict_desc), vp], ctypes.c_int),
+        "sherry_cache_extend": ([ctypes.POINTER(sherry_cache_desc),
+                                 ctypes.POINTER(sherry_extend_desc), vp], ctypes.c_int),
+        "sherry_cache_attend_tokens_workspace": ([ctypes.POINTER(sherry_cache_desc),
+                                                  ctypes.POINTER(sherry_attend_tokens_desc)],
+                                                 ctypes.c_size_t),
+        "sherry_cache_attend_tokens": ([ctypes.POINTER(sherry_cache_desc),
+                                        ctypes.POINTER(sherry_attend_tokens_desc), vp],
+                                       ctypes.c_int),
+        "sherry_cache_fork_workspace": ([ctypes.POINTER(sherry_cache_desc),
+                                         ctypes.POINTER(sherry_fork_desc)], ctypes.c_size_t),
+        "sherry_cache_fork": ([ctypes.POINTER(sherry_cache_desc),
+                               ctypes.POINTER(sherry_fork_desc), vp], ctypes.c_int),
+        "sherry_cache_compact_workspace": ([ctypes.POINTER(sherry_cache_desc),
+                                            ctypes.POINTER(sherry_compact_desc)],
+                                           ctypes.c_size_t),
+        "sherry_cache_compact": ([ctypes.POINTER(sherry_cache_desc),
+                                  ctypes.POINTER(sherry_compact_desc), vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -607,6 +670,41 @@ def sherry_cache_attend(cache, args, stream=None):
 def sherry_cache_evict(cache, args, stream=None):
     """Cuts the sequences of cache down by weight (sherry_evict_desc)."""
     _check(lib.sherry_cache_evict(cache, args, _stream(stream)), "sherry_cache_evict")
+
+
+def sherry_cache_extend(cache, args, stream=None):
+    """Rotates a ragged batch's new tokens (sherry_extend_desc) and stores them in an e4m3 cache."""
+    _check(lib.sherry_cache_extend(cache, args, _stream(stream)), "sherry_cache_extend")
+
+
+def sherry_cache_attend_tokens_workspace(cache, args) -> int:
+    """Bytes of args.workspace (0: the descriptors are invalid)."""
+    return int(lib.sherry_cache_attend_tokens_workspace(cache, args))
+
+
+def sherry_cache_attend_tokens(cache, args, stream=None):
+    """Attention of a ragged batch's new tokens over an e4m3 cache (sherry_attend_tokens_desc)."""
+    _check(lib.sherry_cache_attend_tokens(cache, args, _stream(stream)), "sherry_cache_attend_tokens")
+
+
+def sherry_cache_fork_workspace(cache, args) -> int:
+    """Bytes of args.workspace (0: the descriptors are invalid)."""
+    return int(lib.sherry_cache_fork_workspace(cache, args))
+
+
+def sherry_cache_fork(cache, args, stream=None):
+    """Sequences that go on from others, with pages for their new rows (sherry_fork_desc)."""
+    _check(lib.sherry_cache_fork(cache, args, _stream(stream)), "sherry_cache_fork")
+
+
+def sherry_cache_compact_workspace(cache, args) -> int:
+    """Bytes of args.workspace (0: the descriptors are invalid)."""
+    return int(lib.sherry_cache_compact_workspace(cache, args))
+
+
+def sherry_cache_compact(cache, args, stream=None):
+    """Moves the pages in use to the front of their pool (sherry_compact_desc)."""
+    _check(lib.sherry_cache_compact(cache, args, _stream(stream)), "sherry_cache_compact")
 
 
 def sherry_gemv2(w2, x, x_scale, w_scale: float, y, acc, n: int, k: int, stream=None):

@@ -137,7 +137,9 @@ __device__ __forceinline__ Span span_of(const Attend& a, int b) {
 //        128        1.70 / 1.14 / 1.00 / 1.03 / 1.06 / 1.15 / 1.23
 //        256        1.76 / 1.23 / 0.95 / 0.96 / 1.03 / 1.12 / 1.20
 // and f16 within 0.02 of bf16.
-constexpr int sequence_cost(int type, int dp) { return type == SHERRY_I8 ? 16 : dp == 256 ? 8 : 6; }
+constexpr int sequence_cost(int type, int dp) {
+  return type == SHERRY_I8 || type == SHERRY_F8 ? 16 : dp == 256 ? 8 : 6;
+}
 
 // Each workgroup column takes `run` of the sequences' costs, one after the
 // other; a sequence's first SEQ units (sequence_cost) are no tiles.
@@ -253,6 +255,17 @@ __device__ __forceinline__ uint32_t byte_pair_f16(uint32_t hi, uint32_t lo) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
+// e4m3 codes: bytes 2 i and 2 i + 1 of a word as f16 values (exact).
+template <int i>
+__device__ __forceinline__ uint32_t code_pair_f16(uint32_t x) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(x), 1.0f, i != 0));
+}
+// A page's power of two: the exponent of its scale alone, 2^-126 .. 2^127.
+__device__ __forceinline__ float power_of_page(float scale) {
+  const uint32_t e = __float_as_uint(scale) & 0x7F800000u;
+  return __uint_as_float(e < 0x00800000u ? 0x00800000u : e < 0x7F000000u ? e : 0x7F000000u);
+}
+
 // The largest of a value in the lanes n, n + 16, n + 32, n + 48.
 __device__ __forceinline__ float max_over_blocks(float v) {
   const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -291,8 +304,9 @@ template <int CT_, int QT_, int NT_, int DP_, bool ANY_, bool MORE_>
 struct Cfg {
   static constexpr int CT = CT_, QT = QT_, NT = NT_, DP = DP_;
   static constexpr int EU = waves_for(DP), SEQ = sequence_cost(CT, DP);
-  static constexpr bool ANY = ANY_, MORE = MORE_, F16 = CT != SHERRY_BF16, I8 = CT == SHERRY_I8;
-  static constexpr int E = I8 ? 1 : 2;         // bytes per value
+  static constexpr bool ANY = ANY_, MORE = MORE_, F16 = CT != SHERRY_BF16, I8 = CT == SHERRY_I8, F8 = CT == SHERRY_F8;
+  static constexpr bool BYTES = I8 || F8;
+  static constexpr int E = BYTES ? 1 : 2;      // bytes per value
   static constexpr int KS = DP / 32;           // MFMA steps of a score
   static constexpr int KL = DP * E / 64;       // 16-byte loads per lane and half tile of K
   static constexpr int CH = DP / 16;           // values per lane and row of V
@@ -302,13 +316,13 @@ struct Cfg {
   // Tiles in flight per wave: int8 rows are half as many bytes, and leave the
   // registers for two (64 sequences of 4000 rows 100 us against 110 with 128 values,
   // 59 against 64 with 64, 95 against 100 with 256; with a mask 102 against 111).
-  static constexpr int DEEP = I8 && !ANY ? 2 : 1;
+  static constexpr int DEEP = BYTES && !ANY ? 2 : 1;
 };
 
 // d of value j of MFMA step s in the lanes of block g.
 template <class G>
 __device__ __forceinline__ int k_dim(int s, int g) {
-  return G::I8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+  return G::BYTES ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
 }
 // d of value e of the V values of lane column n.
 template <class G>
@@ -363,9 +377,9 @@ struct Rows {
   uint32_t valid = 0;       // bit r: row r of the tile is attended to
   int rows[2] = {0, 0};     // !ANY: rows of each half that are read
   int64_t at[2] = {0, 0};   // !ANY: element offset of each half
-  int64_t srow[2] = {0, 0}; // !ANY, int8: offset of the half's scales
+  int64_t srow[2] = {0, 0}; // !ANY, bytes: offset of the half's scales
   int64_t row = 0;          // ANY: element offset of row lane % 32
-  int64_t sat = 0;          // ANY, int8: offset of its scale
+  int64_t sat = 0;          // ANY, bytes: offset of its scale
   // what a look-up has read of the tile after it
   int next_page[2] = {-1, -1}, next_pos = 0;
   uint32_t next_mask = 1;
@@ -424,7 +438,7 @@ struct Rows {
       const int pid = next_page[0], off = p - a.c.by_page.div(p) * a.c.page_size;
       ok = ok && pid >= 0 && pid < a.c.pages;
       row = ok ? a.c.at(pid, h) + int64_t(off) * a.c.dim : 0;
-      if constexpr (G::I8) sat = ok ? a.c.scale_at(pid, h) + off : 0;
+      if constexpr (G::BYTES) sat = ok ? a.c.scale_at(pid, h) + (G::I8 ? off : 0) : 0;
       valid = static_cast<uint32_t>(__ballot(ok));
     } else {
       // (scalar: the rows from begin to end, and of pages that exist)
@@ -441,7 +455,7 @@ struct Rows {
         const int off = ph - a.c.by_page.quotient(ph) * a.c.page_size;
         rows[t] = valid >> (16 * t) & 0xFFFFu ? (end - ph < 16 ? end - ph : 16) : 0;
         at[t] = a.c.at(pid, h) + int64_t(off) * a.c.dim;
-        if constexpr (G::I8) srow[t] = a.c.scale_at(pid, h) + off;
+        if constexpr (G::BYTES) srow[t] = a.c.scale_at(pid, h) + (G::I8 ? off : 0);
       }
     }
   }
@@ -461,14 +475,14 @@ struct Rows {
         const bool ok = (valid >> (16 * t + n)) & 1;
 #pragma unroll
         for (int s = 0; s < G::KL; ++s) {
-          const int d = (G::I8 ? 64 : 32) * s + (G::I8 ? 16 : 8) * g;
+          const int d = (G::BYTES ? 64 : 32) * s + (G::BYTES ? 16 : 8) * g;
           global_words<4>(&k[t][4 * s], a.c.k + (from + d) * G::E, ok && d < a.c.dim);
         }
       } else {
         const __amdgpu_buffer_rsrc_t r = half(a.c.k, t);
 #pragma unroll
         for (int s = 0; s < G::KL; ++s) {
-          const int d = (G::I8 ? 64 : 32) * s + (G::I8 ? 16 : 8) * g;
+          const int d = (G::BYTES ? 64 : 32) * s + (G::BYTES ? 16 : 8) * g;
           buffer_words<4>(&k[t][4 * s], r, d < a.c.dim ? (n * a.c.dim + d) * G::E : kOutside);
         }
       }
@@ -509,7 +523,13 @@ struct Rows {
           const int r = 16 * t + 4 * g + j;
           const int64_t from = __shfl(sat, r, 64);
           s[4 * t + j] = (valid >> r) & 1 ? as_global(pool)[from] : 0.0f;
+          if constexpr (G::F8) s[4 * t + j] = power_of_page(s[4 * t + j]);
         }
+      } else if constexpr (G::F8) {
+        // (one of the whole half, a scalar)
+        const float one = power_of_page(as_const(pool)[srow[t]]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[4 * t + j] = one;
       } else {
         // (whole 16-byte pieces: those of rows past the last one lie in the page too)
         const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
@@ -668,7 +688,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
 #pragma unroll
     for (int e = 0; e < G::CH; ++e) o[e] = v4f{0, 0, 0, 0};
     float m = kMinusInf, l = 0.0f;
-    // int8: V's scales are held over 2^ve, the largest of them so far
+    // bytes: V's scales are held over 2^ve, the largest of them so far
     int ve = kUp - 126;  // (2^(kUp - ve) is a finite factor)
 
     // Tile i's rows are read into slot i % D while those of the D tiles before it
@@ -690,12 +710,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
       hole[u] = !G::I8 && !G::ANY && rows.holes();
       start(i + kWaves);
       rows.load_k(kr[u]);
-      if constexpr (G::I8) rows.load_scales(a.c.ks, kscs[u]);
+      if constexpr (G::BYTES) rows.load_scales(a.c.ks, kscs[u]);
     };
     auto fetch_v = [&](auto slot) {
       constexpr int u = decltype(slot)::value;
       rows.load_v(vr[u]);
-      if constexpr (G::I8) rows.load_scales(a.c.vs, vscs[u]);
+      if constexpr (G::BYTES) rows.load_scales(a.c.vs, vscs[u]);
     };
     if (mine_first < t1) {
       rows.start(mine_first);
@@ -742,13 +762,21 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             u32x4 kf;
+            if constexpr (G::F8) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) kf[i] = k[t][4 * st + i];
+              for (int i = 0; i < 2; ++i) {
+                kf[2 * i] = code_pair_f16<0>(k[t][2 * st + i]);
+                kf[2 * i + 1] = code_pair_f16<1>(k[t][2 * st + i]);
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) kf[i] = k[t][4 * st + i];
+            }
 #pragma unroll
             for (int i = G::QT - 1; i >= 0; --i) s[t] = mfma<G::F16>(kf, qf[i][st], s[t]);
           }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3] * factor;
+        for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3] * (G::F8 ? factor * ksc[i] : factor);
       }
       if (more) fetch_k(slot, next);
       uint32_t mine = 0xFF;  // bit i: row of x[i] is attended to
@@ -763,7 +791,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
         for (int i = 0; i < 8; ++i) {
           x[i] = (mine >> i) & 1 ? x[i] : kMinusInf;
           if constexpr (G::MORE) kept[i] = (mine >> i) & 1 ? kept[i] : kMinusInf;
-          if constexpr (G::I8) vsc[i] = (mine >> i) & 1 ? vsc[i] : 0.0f;
+          if constexpr (G::BYTES) vsc[i] = (mine >> i) & 1 ? vsc[i] : 0.0f;
         }
       }
       if (G::MORE && a.weight && n < heads) {
@@ -779,7 +807,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
       top = fmaxf(m, max_over_blocks(top));
       const float base = top == kMinusInf ? 0.0f : top;
       int vt = ve;
-      if constexpr (G::I8) {
+      if constexpr (G::BYTES) {
         float big = 0.0f;  // of the tile's V scales
 #pragma unroll
         for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(vsc[i]));
@@ -790,7 +818,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
       if (__any(top > m || vt > ve)) {
         float down = __builtin_amdgcn_exp2f(m - base);
         l *= down;
-        if constexpr (G::I8) down = ldexpf(down, ve - vt);
+        if constexpr (G::BYTES) down = ldexpf(down, ve - vt);
 #pragma unroll
         for (int e = 0; e < G::CH; ++e)
 #pragma unroll
@@ -804,13 +832,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
 #pragma unroll
           for (int i = 0; i < G::VW; ++i) v[j][i] = (mine >> j) & 1 ? v[j][i] : 0;
       }
-      const float scale_p = G::I8 ? ldexpf(1.0f, kUp - ve) : ldexpf(1.0f, kUp);
+      const float scale_p = G::BYTES ? ldexpf(1.0f, kUp - ve) : ldexpf(1.0f, kUp);
       float p[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         p[i] = __builtin_amdgcn_exp2f(x[i] - base);
         l += p[i];
-        if constexpr (G::I8) p[i] *= vsc[i] * scale_p;
+        if constexpr (G::BYTES) p[i] *= vsc[i] * scale_p;
         else if constexpr (G::F16) p[i] *= scale_p;
       }
       u32x4 pf[NT];
@@ -828,6 +856,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
         for (int i = 0; i < 4; ++i) {
           if constexpr (G::I8)
             vf[i] = byte_pair_f16<e & 3>(v[2 * i + 1][e >> 2], v[2 * i][e >> 2]);
+          else if constexpr (G::F8)  // (the permuted word serves values e and e ^ 1)
+            vf[i] = code_pair_f16<e & 1>(
+                __builtin_amdgcn_perm(v[2 * i + 1][e >> 2], v[2 * i][e >> 2], e & 2 ? 0x07030602u : 0x05010400u));
           else
             vf[i] = e & 1 ? upper(v[2 * i + 1][e >> 1], v[2 * i][e >> 1])
                           : lower(v[2 * i + 1][e >> 1], v[2 * i][e >> 1]);
@@ -855,7 +886,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) top = fmaxf(top, stat[i][n].x);
     float down = m == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
-    if constexpr (G::I8) down = ldexpf(down, ve + kByteDown - kUp);
+    if constexpr (G::BYTES) down = ldexpf(down, ve + (G::I8 ? kByteDown : 0) - kUp);
     else if constexpr (G::F16) down = ldexpf(down, -kUp);
     if (n < heads) {
 #pragma unroll
@@ -1116,6 +1147,7 @@ int launch_attend(const sherry_cache_desc& c, const sherry_attend_desc& d, hipSt
                  d.window, sh.columns, sh.whole, d.scale};
   if (c.type == SHERRY_F16) return launch_dim<SHERRY_F16, 2, 2>(a, s);
   if (c.type == SHERRY_I8) return launch_dim<SHERRY_I8, 3, 2>(a, s);
+  if (c.type == SHERRY_F8) return d.type == SHERRY_F32 ? launch_dim<SHERRY_F8, 2, 2>(a, s) : launch_dim<SHERRY_F8, 1, 2>(a, s);
   switch (d.type) {
     case SHERRY_F32: return launch_dim<SHERRY_BF16, 3, 3>(a, s);
     case SHERRY_F16: return launch_dim<SHERRY_BF16, 2, 3>(a, s);

@@ -33,10 +33,11 @@ struct Cache {
   const int32_t* table;
   int64_t page_stride;  // elements
   int pages, kv, page_size, dim, batch, width, rows;  // rows = width * page_size
+  int scales;  // of a head in a page: page_size (SHERRY_I8) or 1 (SHERRY_F8)
   FastDiv by_page;
-  // First row of head h in page p, in rows (scales) and in elements.
+  // First row of head h in page p, in scales and in elements.
   __device__ __forceinline__ int64_t scale_at(int page, int h) const {
-    return (int64_t(page) * kv + h) * page_size;
+    return (int64_t(page) * kv + h) * scales;
   }
   __device__ __forceinline__ int64_t at(int page, int h) const {
     return int64_t(page) * page_stride + int64_t(h) * page_size * dim;
@@ -53,10 +54,11 @@ inline Cache cache_of(const sherry_cache_desc& d) {
   return Cache{static_cast<char*>(d.k), static_cast<char*>(d.v), d.k_scale, d.v_scale, d.table,
                d.page_stride ? d.page_stride : whole, d.pages, d.kv_heads, d.page_size,
                d.head_dim, d.batch, d.table_width, d.table_width * d.page_size,
+               d.type == SHERRY_F8 ? 1 : d.page_size,
                FastDiv::of(static_cast<uint32_t>(d.page_size))};
 }
 
-inline int type_bytes(int type) { return type == SHERRY_F32 ? 4 : type == SHERRY_I8 ? 1 : 2; }
+inline int type_bytes(int type) { return type == SHERRY_F32 ? 4 : type == SHERRY_I8 || type == SHERRY_F8 ? 1 : 2; }
 
 // fp32 -> 16 bits, to nearest even (NaN stays NaN).
 __device__ __forceinline__ uint16_t to_bf16(float x) {
@@ -98,11 +100,19 @@ __device__ __forceinline__ int wave_scan(int v) {
 int64_t append_threads(const sherry_cache_desc& c, const sherry_append_desc& a);
 int64_t attend_threads(const sherry_cache_desc& c, const sherry_attend_desc& a);
 int64_t evict_threads(const sherry_cache_desc& c, const sherry_evict_desc& a);
+int64_t extend_threads(const sherry_cache_desc& c, const sherry_extend_desc& a);
 inline bool fits_grid(int64_t threads) { return threads <= int64_t(UINT32_MAX); }
 
 size_t attend_workspace(const sherry_cache_desc& c, const sherry_attend_desc& a);
 int launch_attend(const sherry_cache_desc& c, const sherry_attend_desc& a, hipStream_t s);
 int launch_append(const sherry_cache_desc& c, const sherry_append_desc& a, hipStream_t s);
 int launch_evict(const sherry_cache_desc& c, const sherry_evict_desc& a, hipStream_t s);
+int launch_extend(const sherry_cache_desc& c, const sherry_extend_desc& a, hipStream_t s);
+size_t attend_tokens_workspace(const sherry_cache_desc& c, const sherry_attend_tokens_desc& a);
+int launch_attend_tokens(const sherry_cache_desc& c, const sherry_attend_tokens_desc& a, hipStream_t s);
+size_t fork_workspace(const sherry_cache_desc& c, const sherry_fork_desc& a);
+int launch_fork(const sherry_cache_desc& c, const sherry_fork_desc& a, hipStream_t s);
+size_t compact_workspace(const sherry_cache_desc& c, const sherry_compact_desc& a);
+int launch_compact(const sherry_cache_desc& c, const sherry_compact_desc& a, hipStream_t s);
 
 }  // namespace sherry

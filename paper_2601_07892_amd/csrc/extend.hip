@@ -1,0 +1,309 @@
+// New tokens of a ragged batch into a paged cache of e4m3 codes with a power of two
+// per page and head, and their rotary positions.
+//
+//   need = 2^e, the smallest e >= -100 with |y| <= 448 * 2^e for every finite new y
+//   power = need for a page that holds nothing yet, else max(need, old)
+//   code = e4m3(y / power); when power rises, the page's other codes = e4m3(code * old / power)
+//
+// A power of two keeps every step exact but the rounding to e4m3 itself: y / power
+// only moves the exponent, a code that is rounded again loses at most the lowest bits
+// of values near the subnormals, and a reader multiplies without rounding.
+//
+// What bounds it: the bytes of the tokens' q, k and v rows, read once, of q_out
+// and the codes, written once; a decode batch costs a launch and the chain of
+// dependent reads before its stores (lengths, table, rows and old power).
+//
+// Work mapping.  A page's power needs the largest new value of all of its rows, so
+// one owner takes all new rows of a page and head, of K or of V: a wave, or, where
+// that is more than its registers hold, the four waves of a workgroup.  The rows stay
+// in registers from the maximum to the stores (those past kKeep pieces a lane are read
+// again, out of the caches).  Which page is a matter of the lengths, which the device alone
+// knows: every workgroup finds its own by a scan over the sequences.  Further
+// workgroups rotate q, some heads of one token each.
+#include "rotary.h"
+
+namespace sherry {
+namespace {
+
+constexpr int kKeep = 8;       // pieces of four values a lane that stay in registers
+constexpr int kLeast = -100;   // the smallest exponent that extend gives
+
+struct Extend {
+  Cache c;
+  const void* q;
+  const void* k;
+  const void* v;
+  void* q_out;
+  const int32_t* first;
+  const int32_t* length;
+  const int32_t* pos;
+  Rotary rope;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+  int tokens, heads, units;   // units: most pages that the tokens reach
+  FastDiv by_parts, by_qparts;  // workgroups per page, and per token for q
+};
+
+// A sequence's tokens [t0, t0 + n) and its rows before them.
+struct Tokens {
+  int t0, n, len;
+};
+__device__ __forceinline__ Tokens tokens_of(const Extend& a, int b) {
+  const int f0 = as_global(a.first)[b], f1 = as_global(a.first)[b + 1];
+  const int t0 = f0 < 0 ? 0 : f0 < a.tokens ? f0 : a.tokens;
+  const int t1 = f1 < t0 ? t0 : f1 < a.tokens ? f1 : a.tokens;
+  const int len = a.c.length(a.length, b);
+  const int room = a.c.rows - len;
+  return Tokens{t0, t1 - t0 < room ? t1 - t0 : room, len};
+}
+__device__ __forceinline__ int pages_of(const Extend& a, const Tokens& t) {
+  return t.n > 0 ? static_cast<int>(a.c.by_page.div(t.len + t.n - 1) - a.c.by_page.div(t.len)) + 1 : 0;
+}
+
+// Sequence and page (of its table) that the u-th reached page is; b = -1: there are fewer.
+struct Unit {
+  int b, j;
+  Tokens t;
+};
+__device__ __forceinline__ Unit find_unit(const Extend& a, int u) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
+    const Tokens t = b0 + lane < a.c.batch ? tokens_of(a, b0 + lane) : Tokens{0, 0, 0};
+    const int n = pages_of(a, t), upto = wave_scan(n);
+    const uint64_t past = __ballot(before + upto > u);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      const int own = u - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(n, at));
+      const Tokens mine{__builtin_amdgcn_readlane(t.t0, at), __builtin_amdgcn_readlane(t.n, at),
+                        __builtin_amdgcn_readlane(t.len, at)};
+      return Unit{b0 + at, static_cast<int>(a.c.by_page.div(mine.len)) + own, mine};
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return Unit{-1, 0, {0, 0, 0}};
+}
+// The last sequence that begins at or before token t, by 64 probes a step (-1: none).
+__device__ __forceinline__ int find_sequence(const Extend& a, int t) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = a.c.batch;
+  for (;;) {
+    const int step = (n + 63) / 64, at = lane * step;
+    const int k = __builtin_popcountll(__ballot(at < n && as_global(a.first)[lo + (at < n ? at : 0)] <= t));
+    if (k == 0) return -1;
+    lo += (k - 1) * step;
+    n = step < n - (k - 1) * step ? step : n - (k - 1) * step;
+    if (step == 1) return lo;
+  }
+}
+
+// Exponent (biased by 127) of the smallest power of two >= 2^kLeast with top <= 448 of it.
+__device__ __forceinline__ int power_of(float top) {
+  const uint32_t u = __float_as_uint(top);  // 448 = 1.75 * 2^8
+  const int e = static_cast<int>(u >> 23) - 8 + ((u & 0x7FFFFFu) > 0x600000u);
+  return e > 127 + kLeast ? e : 127 + kLeast;
+}
+__device__ __forceinline__ float power(int biased) { return __uint_as_float(uint32_t(biased) << 23); }
+
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
+}
+__device__ __forceinline__ uint32_t requantized(uint32_t x, float ratio) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(x), false);
+  const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(x), true);
+  return codes4(lo[0] * ratio, lo[1] * ratio, hi[0] * ratio, hi[1] * ratio);
+}
+
+// WPP: waves per page, head and K or V.
+template <int LPR, int WPP, int TYPE, bool VEC>
+__device__ __forceinline__ void store_pages(const Extend& a, int blk) {
+  constexpr int RPW = 64 / LPR, STEP = RPW * WPP;  // rows per wave and iteration, and of all waves
+  __shared__ int most[4];
+  const int u = a.by_parts.div(blk), part = blk - u * a.by_parts.d;
+  const Unit unit = find_unit(a, u);
+  const int b = __builtin_amdgcn_readfirstlane(unit.b);
+  if (b < 0) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j = __builtin_amdgcn_readfirstlane(unit.j), p0 = j * a.c.page_size;
+  const int page = as_const(a.c.table)[int64_t(b) * a.c.width + j];
+  if (page < 0 || page >= a.c.pages) return;
+  const Tokens& t = unit.t;
+  const int r0 = t.len > p0 ? t.len : p0;
+  const int r1 = t.len + t.n - p0 < a.c.page_size ? t.len + t.n : p0 + a.c.page_size;
+  const int pair = part * (4 / WPP) + (WPP == 1 ? wave : 0);
+  if (pair >= 2 * a.c.kv) return;  // (with several waves a pair: the whole workgroup)
+  const bool is_k = pair < a.c.kv;
+  const int h = is_k ? pair : pair - a.c.kv;
+  const int mine = WPP == 1 ? 0 : wave;  // of the waves of a pair
+  const int d = 4 * (lane % LPR);
+  const bool in = d < a.c.dim;
+
+  auto value = [&](int row, float4& x) {
+    const int tok = t.t0 + row - t.len;
+    const int pos = a.pos ? as_global(a.pos)[tok] : row;
+    if (!in || !a.rope.has(pos)) return false;
+    x = is_k ? rotated<TYPE, VEC>(a.rope, a.k, int64_t(tok) * a.k_stride + h * a.c.dim, d, pos)
+             : load4<TYPE, VEC>(a.v, int64_t(tok) * a.v_stride + h * a.c.dim + d);
+    return true;
+  };
+  float top = 0.0f;
+  auto see = [&](const float4& x) {
+    auto one = [&](float v) { top = fmaxf(top, fabsf(v) < __builtin_huge_valf() ? fabsf(v) : 0.0f); };
+    one(x.x), one(x.y), one(x.z), one(x.w);
+  };
+  // (a page that holds rows already: the power that they have)
+  float* scale = (is_k ? a.c.ks : a.c.vs) + a.c.scale_at(page, h);
+  const bool fresh = p0 >= t.len;
+  int old = 0;
+  if (!fresh) {
+    old = static_cast<int>(__float_as_uint(as_global(scale)[0]) >> 23) & 0xFF;
+    old = old < 1 ? 1 : old < 254 ? old : 254;
+  }
+  float4 kept[kKeep];
+  uint32_t there = 0;
+  const int from = r0 + mine * RPW + lane / LPR;
+#pragma unroll
+  for (int i = 0; i < kKeep; ++i) {
+    kept[i] = make_float4(0, 0, 0, 0);
+    if (from + i * STEP < r1 && value(from + i * STEP, kept[i])) there |= 1u << i;
+  }
+#pragma unroll
+  for (int i = 0; i < kKeep; ++i) see(kept[i]);
+  for (int row = from + kKeep * STEP; row < r1; row += STEP) {
+    float4 x = make_float4(0, 0, 0, 0);
+    value(row, x);
+    see(x);
+  }
+  top = wave_max_f32(top);
+  int now = power_of(top);
+  now = now > old ? now : old;
+  if constexpr (WPP > 1) {
+    if (lane == 0) most[wave] = now;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) now = now > most[i] ? now : most[i];
+  }
+  now = __builtin_amdgcn_readfirstlane(now);
+
+  char* rows = (is_k ? a.c.k : a.c.v) + a.c.at(page, h);
+  auto store = [&](int row, const float4& x) {
+    auto one = [&](float v) {
+      return fabsf(v) < __builtin_huge_valf() ? v * power(254 - now) : __uint_as_float(0x7FC00000u);
+    };
+    *reinterpret_cast<SHERRY_GLOBAL uint32_t*>(as_global_mut(rows) + int64_t(row - p0) * a.c.dim + d) =
+        codes4(one(x.x), one(x.y), one(x.z), one(x.w));
+  };
+#pragma unroll
+  for (int i = 0; i < kKeep; ++i)
+    if ((there >> i) & 1) store(from + i * STEP, kept[i]);
+  for (int row = from + kKeep * STEP; row < r1; row += STEP) {
+    float4 x;
+    if (value(row, x)) store(row, x);
+  }
+  if (!fresh && now > old) {
+    // (a ratio below 2^-126 leaves nothing of any code)
+    const float ratio = power(127 - (now - old < 126 ? now - old : 126));
+    const int pieces = a.c.dim / 16;
+    const int64_t before = int64_t(r0 - p0) * pieces, gap = int64_t(r1 - r0) * pieces;
+    const int64_t all = int64_t(a.c.page_size) * pieces - gap;
+    for (int64_t i = mine * 64 + lane; i < all; i += 64 * WPP) {
+      SHERRY_GLOBAL u32x4* at = reinterpret_cast<SHERRY_GLOBAL u32x4*>(as_global_mut(rows)) + (i < before ? i : i + gap);
+      u32x4 x = *at;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) x[w] = requantized(x[w], ratio);
+      *at = x;
+    }
+  }
+  if (mine == 0 && lane == 0) as_global_mut(scale)[0] = power(now);
+}
+
+template <int LPR, int TYPE, bool VEC>
+__device__ __forceinline__ void turn_q(const Extend& a, int blk) {
+  const int t = a.by_qparts.div(blk), part = blk - t * a.by_qparts.d;
+  const int b = __builtin_amdgcn_readfirstlane(find_sequence(a, t));
+  if (b < 0) return;
+  const Tokens s = tokens_of(a, b);
+  const int row = s.len + (t - s.t0);
+  if (t < s.t0 || t - s.t0 >= s.n) return;
+  const int page = as_const(a.c.table)[int64_t(b) * a.c.width + a.c.by_page.div(row)];
+  const int pos = a.pos ? as_const(a.pos)[t] : row;
+  const int r = part * (256 / LPR) + threadIdx.x / LPR, d = 4 * (threadIdx.x % LPR);
+  if (page < 0 || page >= a.c.pages || !a.rope.has(pos) || r >= a.heads || d >= a.c.dim) return;
+  store4<TYPE, VEC>(a.q_out, int64_t(t) * a.q_out_stride + r * a.c.dim + d,
+                    rotated<TYPE, VEC>(a.rope, a.q, int64_t(t) * a.q_stride + r * a.c.dim, d, pos));
+}
+
+// Blocks [0, units * by_parts.d): pages; then [tokens][by_qparts.d]: q.
+template <int LPR, int WPP, int TYPE, bool VEC>
+__global__ __launch_bounds__(256) void extend_kernel(Extend a) {
+  const int pages = a.units * static_cast<int>(a.by_parts.d);
+  if (static_cast<int>(blockIdx.x) < pages) store_pages<LPR, WPP, TYPE, VEC>(a, blockIdx.x);
+  else turn_q<LPR, TYPE, VEC>(a, blockIdx.x - pages);
+}
+
+struct Grid {
+  int units;
+  int64_t parts, qparts;  // workgroups per page, and per token for q
+  bool wide;              // four waves per page, head and K or V
+  int64_t blocks(int64_t tokens) const { return units * parts + tokens * qparts; }
+};
+Grid grid_of(const sherry_cache_desc& c, const sherry_extend_desc& d) {
+  Grid g{};
+  const int lanes = lanes_per_row(c.head_dim);
+  const int64_t batch = c.batch < d.tokens ? c.batch : d.tokens;
+  const int64_t units = d.tokens / c.page_size + 2 * batch;  // n tokens reach n / page_size + 2 pages at most
+  g.units = static_cast<int>(units < d.tokens ? units : d.tokens);
+  // new rows of a page if the sequences have equally many
+  const int64_t rows = ceil_div(d.tokens, c.batch) < c.page_size ? ceil_div(d.tokens, c.batch) : c.page_size;
+  g.wide = rows * lanes > 64 * kKeep;
+  g.parts = g.wide ? 2 * c.kv_heads : ceil_div(2 * c.kv_heads, 4);
+  g.qparts = d.q ? ceil_div(d.heads, 256 / lanes) : 0;
+  return g;
+}
+
+template <int LPR, int TYPE, bool VEC>
+int launch_wide(const Extend& a, const Grid& g, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(g.blocks(a.tokens)));
+  return g.wide ? launch(extend_kernel<LPR, 4, TYPE, VEC>, grid, dim3(256), 0, s, a)
+                : launch(extend_kernel<LPR, 1, TYPE, VEC>, grid, dim3(256), 0, s, a);
+}
+template <int LPR>
+int launch_type(const Extend& a, int type, bool vec, const Grid& g, hipStream_t s) {
+  switch (type) {
+    case SHERRY_F32:
+      return vec ? launch_wide<LPR, SHERRY_F32, true>(a, g, s) : launch_wide<LPR, SHERRY_F32, false>(a, g, s);
+    case SHERRY_F16:
+      return vec ? launch_wide<LPR, SHERRY_F16, true>(a, g, s) : launch_wide<LPR, SHERRY_F16, false>(a, g, s);
+    default:
+      return vec ? launch_wide<LPR, SHERRY_BF16, true>(a, g, s) : launch_wide<LPR, SHERRY_BF16, false>(a, g, s);
+  }
+}
+
+}  // namespace
+
+int64_t extend_threads(const sherry_cache_desc& c, const sherry_extend_desc& d) {
+  return 256 * grid_of(c, d).blocks(d.tokens);
+}
+
+int launch_extend(const sherry_cache_desc& c, const sherry_extend_desc& d, hipStream_t s) {
+  const Grid g = grid_of(c, d);
+  const int heads = d.q ? d.heads : 0;
+  const int64_t qrow = int64_t(heads) * c.head_dim, row = int64_t(c.kv_heads) * c.head_dim;
+  const Extend a{cache_of(c), d.q, d.k, d.v, d.q_out, d.first, d.length, d.pos,
+                 Rotary{d.cos, d.sin, d.rope_rows, d.rot_dim, d.pairing == SHERRY_ROPE_PAIRS},
+                 d.q_stride ? d.q_stride : qrow, d.k_stride ? d.k_stride : row, d.v_stride ? d.v_stride : row,
+                 d.q_out_stride ? d.q_out_stride : qrow, d.tokens, heads, g.units,
+                 FastDiv::of(static_cast<uint32_t>(g.parts)),
+                 FastDiv::of(static_cast<uint32_t>(g.qparts ? g.qparts : 1))};
+  auto whole = [&](const void* p, int64_t stride) { return whole_pieces(p, stride, d.type); };
+  const bool vec = whole(a.k, a.k_stride) && whole(a.v, a.v_stride) &&
+                   (!heads || (whole(a.q, a.q_stride) && whole(a.q_out, a.q_out_stride))) &&
+                   reinterpret_cast<uintptr_t>(d.cos) % 16 == 0 && reinterpret_cast<uintptr_t>(d.sin) % 16 == 0;
+  switch (lanes_per_row(c.head_dim)) {
+    case 16: return launch_type<16>(a, d.type, vec, g, s);
+    case 32: return launch_type<32>(a, d.type, vec, g, s);
+    default: return launch_type<64>(a, d.type, vec, g, s);
+  }
+}
+
+}  // namespace sherry

@@ -1,0 +1,804 @@
+// Attention of many new tokens per sequence over a paged cache of e4m3 codes:
+//
+//   s_r = scale q . k_r,  p_r = exp(s_r - max) / sum exp(s - max),  out = sum_r p_r v_r
+//
+// over the rows up to the token's own, in one pass over them with a running maximum
+// and sum.
+//
+// What bounds it: 4 head_dim operations per token, query head and row, on the matrix
+// cores; and beside them, per score, an exponential, a maximum, a sum and a rounding
+// on the vector units, which is about as much for heads of 128 values and more for
+// heads of 64.  With few tokens, the cache's bytes.
+//
+// Work mapping.  A tile is 128 rows of q: as many tokens as fit, with all the query
+// heads that share one key-value head, so that K and V are read once for them.  What a tile
+// costs is the rows that it attends to; the tiles of all sequences and heads, one after
+// the other, are cut into equal runs over as many workgroups as fit the GPU,
+// between tiles or inside one.  The lengths are known to the device alone, so every
+// workgroup finds its place from them, by closed sums.  What a workgroup finds
+// for a tile, unless it has all of it, is joined by a second launch.  Consecutive
+// runs go to one XCD, whose L2 then serves the tiles of a head.
+//
+// In a workgroup every wave has 32 rows of q, and all share 64 rows of K and V at a
+// time, double buffered in LDS as f16.  Both products run on 32x32x16 MFMAs without
+// moving anything between lanes:
+//  * S^T = K Q^T: lane l holds the scores of q row l % 32 with rows 8 (i / 4) + 4 (l / 32)
+//    + i % 4 of each half of 32.
+//  * O^T = V^T P^T: eight probabilities of a lane are its P^T operand as they are; V is
+//    written to LDS transposed, and with its rows in the order that this asks for.
+//
+// Precision.  e4m3 codes are exact in f16, and so are their products with powers of
+// two down to 2^-15 of the largest in a tile of K, or so far of V, which take the pages'
+// scales (smaller ones are rounded at 2^-33 of that largest value).  q is scaled by the
+// power of two of its row's largest value: one f16 term holds all of bf16 and f16 values (but for
+// bits below 2^-25 of that largest), two 22 bits of fp32.  Probabilities, times
+// 2^10, are one term for 16-bit outputs (error 2^-11 of each at most, where the output's own
+// rounding is 2^-8 or 2^-11), two for fp32.  Scores, maxima, sums and outputs are
+// fp32; the maximum is taken anew only when a score passes it by 2^5.
+#include "cache_internal.h"
+
+namespace sherry {
+namespace {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kQRows = 32 * kWaves;  // of a tile
+constexpr int kRows = 64;            // of K and V at a time
+constexpr int kCus = 256, kXcds = 8;
+// What a tile costs besides its rows (its q, the first loads, the way out), in rows.
+constexpr int kTileCost = 128;
+constexpr int kMinRun = 384;         // the shortest run, in rows of cost
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kMinusInf = -__builtin_huge_valf();
+constexpr float kUp = 10.0f;         // p is held times 2^kUp
+constexpr float kLazy = 5.0f;        // scores may pass the maximum by this
+
+struct Tokens {
+  Cache c;
+  const void* q;
+  void* out;
+  const int32_t* first;
+  const int32_t* length;
+  const uint8_t* mask;
+  // what workgroup w found for the tile that its run begins in (part 2 w), and for the
+  // one that begins in its run and goes on behind it (2 w + 1)
+  float2* stat;  // [part][part_rows]: where p is 1, in units of ln 2, and the sum of p
+  float* sums;   // [part][part_rows][DP]: outputs of these rows
+  int64_t q_stride, out_stride, mask_stride;
+  int tokens, heads, group, gtiles, per_tile, hp, type, window, groups, part_rows;
+  float scale;
+};
+
+// ---- which tiles a workgroup takes -------------------------------------------
+
+// A sequence's tokens [t0, t0 + n), its rows before them, and its tiles per head.
+struct Seq {
+  int t0, n, len, tiles;
+};
+__device__ __forceinline__ Seq seq_of(const Tokens& a, int b) {
+  const int f0 = as_global(a.first)[b], f1 = as_global(a.first)[b + 1];
+  const int t0 = f0 < 0 ? 0 : f0 < a.tokens ? f0 : a.tokens;
+  const int t1 = f1 < t0 ? t0 : f1 < a.tokens ? f1 : a.tokens;
+  return Seq{t0, t1 - t0, a.c.length(a.length, b), (t1 - t0 + a.per_tile - 1) / a.per_tile};
+}
+// The rows that the first k tiles of a head attend to, and kTileCost each: tile t the
+// rows from max(0, len + 1 - window + t r) to len + min(n, (t + 1) r), r = tokens per tile.
+__device__ __forceinline__ int64_t cost_of(const Tokens& a, const Seq& s, int k) {
+  const int64_t r = a.per_tile, kk = k;
+  int64_t sum = kk * (s.len + kTileCost) + r * (kk * (kk + 1) / 2);
+  if (k == s.tiles) sum -= kk * r - s.n;
+  if (a.window) {
+    const int64_t low = int64_t(s.len) + 1 - a.window;
+    const int64_t from = low >= 0 ? 0 : (-low + r - 1) / r;  // the first tile that leaves rows out
+    if (from < kk) sum -= (kk - from) * low + r * ((kk * (kk - 1) - from * (from - 1)) / 2);
+  }
+  return sum;
+}
+
+struct Place {
+  int b;    // -1: nowhere
+  int head, t;    // key-value head and its tile of query heads; tile of tokens
+  int64_t at;     // unit of the tile's cost
+  Seq s;
+};
+__device__ __forceinline__ int64_t wave_scan64(int64_t v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t u = __shfl_up(v, o, 64);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
+__device__ __forceinline__ int64_t readlane64(int64_t v, int lane) {
+  return int64_t(uint64_t(uint32_t(__builtin_amdgcn_readlane(int(v >> 32), lane))) << 32 |
+                 uint32_t(__builtin_amdgcn_readlane(int(v), lane)));
+}
+__device__ __forceinline__ int64_t total_cost(const Tokens& a) {
+  const int lane = threadIdx.x & 63;
+  int64_t all = 0;
+  for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
+    int64_t n = 0;
+    if (b0 + lane < a.c.batch) {
+      const Seq s = seq_of(a, b0 + lane);
+      n = cost_of(a, s, s.tiles) * (int64_t(a.c.kv) * a.gtiles);
+    }
+    all += readlane64(wave_scan64(n), 63);
+  }
+  return all;
+}
+// Where unit u of all tiles' cost lies.
+__device__ __forceinline__ Place find_place(const Tokens& a, int64_t u) {
+  const int lane = threadIdx.x & 63;
+  const int64_t heads = int64_t(a.c.kv) * a.gtiles;
+  int64_t before = 0;
+  for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
+    Seq s{0, 0, 0, 0};
+    int64_t one = 0;
+    if (b0 + lane < a.c.batch) {
+      s = seq_of(a, b0 + lane);
+      one = cost_of(a, s, s.tiles);
+    }
+    const int64_t n = one * heads, upto = wave_scan64(n);
+    const uint64_t past = __ballot(before + upto > u);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      Place p;
+      p.b = b0 + at;
+      p.s = Seq{__builtin_amdgcn_readlane(s.t0, at), __builtin_amdgcn_readlane(s.n, at),
+                __builtin_amdgcn_readlane(s.len, at), __builtin_amdgcn_readlane(s.tiles, at)};
+      const int64_t head_cost = readlane64(one, at);
+      int64_t in = u - before - readlane64(upto - n, at);
+      const int64_t head = in / head_cost;
+      p.head = static_cast<int>(head < heads ? head : heads - 1);
+      in -= p.head * head_cost;
+      int lo = 0, hi = p.s.tiles;  // cost_of(lo) <= in < cost_of(hi)
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (cost_of(a, p.s, mid) <= in) lo = mid;
+        else hi = mid;
+      }
+      p.t = lo;
+      p.at = in - cost_of(a, p.s, lo);
+      return p;
+    }
+    before += readlane64(upto, 63);
+  }
+  return Place{-1, 0, 0, 0, {0, 0, 0, 0}};
+}
+__device__ __forceinline__ int64_t run_of(const Tokens& a, int64_t all) {
+  const int64_t run = (all + a.groups - 1) / a.groups;
+  return run < kMinRun ? kMinRun : run;
+}
+
+// The rows of K and V that a tile reads: blocks [k0, k1) of kRows, up to row end.
+struct Span {
+  int k0, k1, end;
+};
+__device__ __forceinline__ Span span_of(const Tokens& a, const Seq& s, int t) {
+  const int64_t tok0 = int64_t(t) * a.per_tile;
+  const int64_t tok1 = tok0 + a.per_tile < s.n ? tok0 + a.per_tile : s.n;
+  const int64_t end = s.len + tok1 < a.c.rows ? s.len + tok1 : a.c.rows;
+  int64_t low = a.window ? s.len + tok0 + 1 - a.window : 0;
+  low = low < 0 ? 0 : low < end ? low : end;
+  return Span{static_cast<int>(low / kRows), static_cast<int>((end + kRows - 1) / kRows), static_cast<int>(end)};
+}
+// The block of a tile's rows that unit `at` of its cost stands for.
+__device__ __forceinline__ int block_at(const Span& sp, int64_t at) {
+  const int64_t k = at > kTileCost ? sp.k0 + (at - kTileCost) / kRows : sp.k0;
+  return k < sp.k1 ? static_cast<int>(k) : sp.k1;
+}
+
+// ---- operands -----------------------------------------------------------------
+
+__device__ __forceinline__ v16f mfma(const u32x4& a, const u32x4& b, const v16f& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t pair_f16(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, v2h{static_cast<_Float16>(lo), static_cast<_Float16>(hi)});
+}
+// Two values as NT terms each: x = t[0] + t[1] up to the last one's rounding.
+template <int NT>
+__device__ __forceinline__ void split(float lo, float hi, uint32_t (&t)[NT]) {
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    t[n] = pair_f16(lo, hi);
+    if (n + 1 < NT) {
+      const v2h h = __builtin_bit_cast(v2h, t[n]);
+      lo -= static_cast<float>(h[0]);
+      hi -= static_cast<float>(h[1]);
+    }
+  }
+}
+template <bool HI>
+__device__ __forceinline__ uint32_t code_pair(uint32_t x, float times) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(x), times, HI));
+}
+__device__ __forceinline__ float power(int biased) { return __uint_as_float(uint32_t(biased) << 23); }
+// Biased exponent of a page's scale, 1 .. 254.
+__device__ __forceinline__ int exponent(float scale) {
+  const int e = static_cast<int>(__float_as_uint(scale) >> 23) & 0xFF;
+  return e < 1 ? 1 : e < 254 ? e : 254;
+}
+// The larger of a value in the lanes n and n + 32.
+__device__ __forceinline__ float max_of_halves(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ uint32_t max_of_halves(uint32_t v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return a[0] > a[1] ? a[0] : a[1];
+}
+__device__ __forceinline__ int wave_max(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const int u = __shfl_xor(v, o, 64);
+    v = v > u ? v : u;
+  }
+  return __builtin_amdgcn_readfirstlane(v);
+}
+
+// K in LDS: rows of DP f16 values, 16 bytes further apart than they are long.
+// V: DP rows of 64 f16 values, those of one step of 16 rows and lane half in a
+// piece of 16 bytes (rows 4 g + 0..3 and 8 + 4 g + 0..3 of the 16); the pieces of a row
+// are permuted so that reads (16 rows at once) and writes (VB rows apart) spread over
+// the banks.
+template <int DP>
+struct Lds {
+  static constexpr int KW = DP * 2 + 16, K = kRows * KW, V = DP * kRows * 2;
+  alignas(16) char k[2][K];
+  alignas(16) char v[2][V];
+  int64_t at[3][kRows];     // where a row begins in its pool; -1: left out
+  float kx[3][kRows], vx[3][kRows];  // what its codes are multiplied by
+  uint32_t valid[3][2];
+  int kref[3], vref[3];     // biased exponents that the products with kx and vx are over
+  int nan[3];               // some code of V is NaN
+};
+__device__ __forceinline__ int v_piece(int dim, int piece) { return piece ^ (dim >> 1 & 7) ^ (dim >> 4 & 7); }
+
+// Waves per SIMD that the registers allow.
+__host__ __device__ constexpr int waves_for(int dp, int terms) {
+  return dp == 256 ? 1 : dp == 128 ? 2 : terms == 1 ? 3 : 2;
+}
+
+// DP: head_dim rounded up to 64, 128 or 256; NT: terms of q and p.
+template <int DP, int NT>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_for(DP, NT)))) void tokens_kernel(
+    Tokens a) {
+  constexpr int KS = DP / 16;   // MFMA steps of a score
+  constexpr int DB = DP / 32;   // blocks of 32 values of V
+  constexpr int KP = DP / 64;   // 16-byte pieces of K per thread
+  constexpr int VB = DP / 16;   // bytes of V per thread and row
+  constexpr int VW = VB / 4;
+  __shared__ Lds<DP> lds;
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // consecutive runs on one XCD (workgroups go to them in turn)
+  const int w = blockIdx.x % kXcds * (a.groups / kXcds) + blockIdx.x / kXcds;
+  const int64_t all = total_cost(a), run = run_of(a, all);
+  int64_t u = int64_t(w) * run;
+  const int64_t u_end = u + run < all ? u + run : all;
+  if (u >= u_end) return;
+  Place pl = find_place(a, u);
+
+  for (;;) {
+    const Seq& s = pl.s;
+    const int64_t cost = cost_of(a, s, pl.t + 1) - cost_of(a, s, pl.t);
+    const int64_t upto = cost - pl.at < u_end - u ? cost : pl.at + (u_end - u);
+    if (upto <= pl.at) return;  // (first is not ascending, and the costs past 63 bits)
+    const Span sp = span_of(a, s, pl.t);
+    const int b = __builtin_amdgcn_readfirstlane(pl.b);
+    const bool whole = pl.at == 0 && upto == cost;
+    const int kb0 = __builtin_amdgcn_readfirstlane(pl.at == 0 ? sp.k0 : block_at(sp, pl.at));
+    const int kb1 = __builtin_amdgcn_readfirstlane(upto == cost ? sp.k1 : block_at(sp, upto));
+    const int end = __builtin_amdgcn_readfirstlane(sp.end);
+    const int kvh = __builtin_amdgcn_readfirstlane(pl.head / a.gtiles);
+    const int head0 = kvh * a.group + (pl.head - kvh * a.gtiles) * a.hp;
+    const int heads = (kvh + 1) * a.group - head0 < a.hp ? (kvh + 1) * a.group - head0 : a.hp;
+    // this lane's row of q
+    const int r = wave * 32 + n, tok = r / a.hp, hd = r - tok * a.hp;
+    const int64_t in_seq = int64_t(pl.t) * a.per_tile + tok;
+    const bool mine = tok < a.per_tile && in_seq < s.n && hd < heads;
+    const int token = s.t0 + static_cast<int>(mine ? in_seq : 0);
+    const int64_t own = s.len + in_seq + 1;  // rows up to its own
+    const int lim = mine ? static_cast<int>(own < a.c.rows ? own : a.c.rows) : 0;
+    const int64_t low64 = a.window ? own - a.window : 0;
+    const int low = mine && low64 > 0 ? static_cast<int>(low64 < a.c.rows ? low64 : a.c.rows) : 0;
+    // of the wave's rows: every one attends to all of [all_low, all_lim), none outside
+    // [some_low, some_lim)
+    const int some_lim = wave_max(lim), all_low = wave_max(low);
+    const int all_lim = -wave_max(mine ? -lim : -0x7FFFFFFF), some_low = -wave_max(mine ? -low : -0x7FFFFFFF);
+
+    // q, over the power of two of its largest value
+    u32x4 qf[NT][KS];
+    float factor = fabsf(a.scale) * kLog2e;
+    {
+      float x[KS][8];
+      uint32_t most = 0;
+      const int64_t at = int64_t(token) * a.q_stride + int64_t(head0 + (mine ? hd : 0)) * a.c.dim;
+#pragma unroll
+      for (int st = 0; st < KS; ++st) {
+        const int d = 16 * st + 8 * g;
+        const bool in = mine && d < a.c.dim;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[st][i] = 0.0f;
+        if (in) {
+          if (a.type == SHERRY_F32) {
+            const SHERRY_GLOBAL v4f* p =
+                reinterpret_cast<const SHERRY_GLOBAL v4f*>(as_global(static_cast<const float*>(a.q)) + at + d);
+            const v4f lo = p[0], hi = p[1];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              x[st][i] = lo[i];
+              x[st][4 + i] = hi[i];
+            }
+          } else {
+            const u32x4 h =
+                *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(static_cast<const uint16_t*>(a.q)) + at + d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const uint16_t v = static_cast<uint16_t>(h[i >> 1] >> (16 * (i & 1)));
+              x[st][i] = a.type == SHERRY_BF16 ? from_bf16(v) : from_f16(v);
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t bits = __float_as_uint(x[st][i]) & 0x7FFFFFFFu;
+          most = bits > most ? bits : most;
+        }
+      }
+      most = max_of_halves(most);
+      constexpr uint32_t kTiny = 0x00400000u;  // 2^-127
+      const uint32_t e = most >> 23 < 254 ? most >> 23 : 254;
+      const float down = __uint_as_float(e < 254 ? (254 - e) << 23 : kTiny) * (a.scale < 0 ? -1.0f : 1.0f);
+      factor *= __uint_as_float(e > 0 ? e << 23 : kTiny);
+#pragma unroll
+      for (int st = 0; st < KS; ++st)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t t[NT];
+          split<NT>(x[st][2 * i] * down, x[st][2 * i + 1] * down, t);
+#pragma unroll
+          for (int j = 0; j < NT; ++j) qf[j][st][i] = t[j];
+        }
+    }
+
+    v16f o[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) o[i] = v16f{};
+    float m = kMinusInf, base = 0.0f, l = 0.0f;
+    int vrun = 1;  // o is over this power of two
+
+    // ---- what the first wave finds out about a block of rows ----
+    int next_page = -1, next_mask = 1, seen_vref = 1;
+    int64_t next_at = -1;
+    float next_ks = 0, next_vs = 0;
+    auto look_page = [&](int kb) {  // reads its pages
+      const int row = kb * kRows + lane;
+      const bool in = kb < kb1 && row < end;
+      next_page = in ? as_global(a.c.table)[int64_t(b) * a.c.width + a.c.by_page.div(row)] : -1;
+      next_mask = in && a.mask ? as_global(a.mask)[int64_t(b) * a.mask_stride + row] : 1;
+    };
+    auto look_scale = [&](int kb) {  // and then their scales
+      const int row = kb * kRows + lane;
+      const bool ok = next_page >= 0 && next_page < a.c.pages && next_mask != 0;
+      next_at = -1;
+      if (ok) {
+        const int off = row - static_cast<int>(a.c.by_page.div(row)) * a.c.page_size;
+        next_at = a.c.at(next_page, kvh) + int64_t(off) * a.c.dim;
+        next_ks = as_global(a.c.ks)[a.c.scale_at(next_page, kvh)];
+        next_vs = as_global(a.c.vs)[a.c.scale_at(next_page, kvh)];
+      }
+    };
+    auto publish = [&](int slot) {
+      const bool ok = next_at >= 0;
+      const int ke = ok ? exponent(next_ks) : 1, ve = ok ? exponent(next_vs) : 1;
+      const int kref = wave_max(ke), vmax = wave_max(ve);
+      seen_vref = vmax > seen_vref ? vmax : seen_vref;
+      lds.at[slot][lane] = next_at;
+      lds.kx[slot][lane] = power(127 - (kref - ke < 126 ? kref - ke : 126));
+      lds.vx[slot][lane] = power(127 - (seen_vref - ve < 126 ? seen_vref - ve : 126));
+      const uint64_t valid = __ballot(ok);
+      if (lane == 0) {
+        lds.valid[slot][0] = static_cast<uint32_t>(valid);
+        lds.valid[slot][1] = static_cast<uint32_t>(valid >> 32);
+        lds.kref[slot] = kref;
+        lds.vref[slot] = seen_vref;
+        lds.nan[slot] = 0;
+      }
+    };
+    // ---- a block's rows, from the pools to LDS ----
+    uint32_t kr[KP][4], vr[4][VW];
+    auto load = [&](int slot) {
+#pragma unroll
+      for (int i = 0; i < KP; ++i) {
+        const int p = tid + kThreads * i, row = p / (DP / 16), d = 16 * (p % (DP / 16));
+        const int64_t at = lds.at[slot][row];
+        u32x4 x = {0, 0, 0, 0};
+        if (at >= 0 && d < a.c.dim) x = *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(a.c.k) + at + d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) kr[i][j] = x[j];
+      }
+      const int quad = tid / 16, d = VB * (tid % 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t at = lds.at[slot][4 * quad + j];
+        const bool in = at >= 0 && d < a.c.dim;
+        const SHERRY_GLOBAL char* from = as_global(a.c.v) + at + d;
+        if constexpr (VW == 4) {
+          u32x4 x = {0, 0, 0, 0};
+          if (in) x = *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(from);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) vr[j][i] = x[i];
+        } else if constexpr (VW == 2) {
+          u32x2 x = {0, 0};
+          if (in) x = *reinterpret_cast<const SHERRY_GLOBAL u32x2*>(from);
+          vr[j][0] = x[0];
+          vr[j][1] = x[1];
+        } else {
+          vr[j][0] = in ? *reinterpret_cast<const SHERRY_GLOBAL uint32_t*>(from) : 0u;
+        }
+      }
+    };
+    auto fill = [&](int buf, int slot) {
+#pragma unroll
+      for (int i = 0; i < KP; ++i) {
+        const int p = tid + kThreads * i, row = p / (DP / 16), d = 16 * (p % (DP / 16));
+        const float times = lds.kx[slot][row];
+        u32x4 x[2];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[j >> 1][2 * (j & 1)] = code_pair<false>(kr[i][j], times);
+          x[j >> 1][2 * (j & 1) + 1] = code_pair<true>(kr[i][j], times);
+        }
+        u32x4* to = reinterpret_cast<u32x4*>(lds.k[buf] + row * Lds<DP>::KW + 2 * d);
+        to[0] = x[0];
+        to[1] = x[1];
+      }
+      const int quad = tid / 16, d0 = VB * (tid % 16);
+      const int piece = 2 * (quad >> 2) + (quad & 1), half = 8 * (quad >> 1 & 1);
+      // (rows of a quad lie in one page or in several: their factors)
+      const float4 times = *reinterpret_cast<const float4*>(&lds.vx[slot][4 * quad]);
+      const bool same = times.x == times.y && times.x == times.z && times.x == times.w;
+      uint32_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < VW; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) odd |= ((vr[j][i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          u32x2 x;
+          if (same) {
+            const uint32_t sel = e & 2 ? 0x07030602u : 0x05010400u;  // (values e and e ^ 1 of two rows)
+            const uint32_t p01 = __builtin_amdgcn_perm(vr[1][i], vr[0][i], sel);
+            const uint32_t p23 = __builtin_amdgcn_perm(vr[3][i], vr[2][i], sel);
+            x[0] = e & 1 ? code_pair<true>(p01, times.x) : code_pair<false>(p01, times.x);
+            x[1] = e & 1 ? code_pair<true>(p23, times.x) : code_pair<false>(p23, times.x);
+          } else {
+            uint32_t y[4];
+            const float t[4] = {times.x, times.y, times.z, times.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t z = e & 2 ? code_pair<true>(vr[j][i], t[j]) : code_pair<false>(vr[j][i], t[j]);
+              y[j] = e & 1 ? z >> 16 : z & 0xFFFFu;
+            }
+            x[0] = y[0] | y[1] << 16;
+            x[1] = y[2] | y[3] << 16;
+          }
+          const int d = d0 + 4 * i + e;
+          *reinterpret_cast<u32x2*>(lds.v[buf] + d * (2 * kRows) + 16 * v_piece(d, piece) + half) = x;
+        }
+      }
+      if (odd) lds.nan[slot] = 1;
+    };
+
+    __syncthreads();  // (the tile before has been read from LDS)
+    if (kb0 < kb1) {
+      if (wave == 0) {
+        look_page(kb0);
+        look_scale(kb0);
+        look_page(kb0 + 1);
+        publish(0);
+        look_scale(kb0 + 1);
+        look_page(kb0 + 2);
+        publish(1);
+      }
+      __syncthreads();
+      load(0);
+      fill(0, 0);
+      __syncthreads();
+    }
+    int slot = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      const int buf = (kb - kb0) & 1, slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
+      // the rows of the next block, and what the one after it is
+      if (kb + 1 < kb1) load(slot1);
+      if (wave == 0 && kb + 2 < kb1) {
+        look_scale(kb + 2);
+        look_page(kb + 3);
+      }
+      const int row0 = kb * kRows;
+      if (row0 < some_lim && row0 + kRows > some_low) {
+        const int vref = __builtin_amdgcn_readfirstlane(lds.vref[slot]);
+        const float f = factor * power(__builtin_amdgcn_readfirstlane(lds.kref[slot]));
+        const uint32_t valid[2] = {static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(lds.valid[slot][0])),
+                                   static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(lds.valid[slot][1]))};
+        const bool full = (valid[0] & valid[1]) == ~0u && row0 + kRows <= all_lim && row0 >= all_low;
+        v16f sc[2] = {v16f{}, v16f{}};
+#pragma unroll
+        for (int st = 0; st < KS; ++st)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const u32x4 kf = *reinterpret_cast<const u32x4*>(lds.k[buf] + (32 * h + n) * Lds<DP>::KW + 32 * st + 16 * g);
+#pragma unroll
+            for (int j = NT - 1; j >= 0; --j) sc[h] = mfma(kf, qf[j][st], sc[h]);
+          }
+        uint32_t ok[2] = {~0u, ~0u};  // bit 8 (i / 4) + i % 4: score i is attended to
+        if (!full) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r0 = row0 + 32 * h;
+            const int most = lim - r0, least = low - r0;
+            uint32_t bits = most >= 32 ? ~0u : most > 0 ? (1u << most) - 1 : 0u;
+            bits &= least >= 32 ? 0u : least > 0 ? ~0u << least : ~0u;
+            ok[h] = (bits & valid[h]) >> (4 * g);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              sc[h][i] = (ok[h] >> (8 * (i / 4) + i % 4)) & 1 ? sc[h][i] : kMinusInf;
+          }
+        }
+        float top = sc[0][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i >> 4][i & 15]);
+        top = max_of_halves(top);
+        top = top == kMinusInf ? kMinusInf : top * f;
+        if (__any(top > m + kLazy) || vref > vrun) {
+          const bool up = top > m;
+          const float to = up ? top - kUp : base;
+          float down = m == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(base - to);
+          if (up) {
+            base = to;
+            m = top;
+          }
+          l *= down;
+          down *= power(vref - vrun < 126 ? 127 - (vref - vrun) : 1);
+          vrun = vref;
+#pragma unroll
+          for (int i = 0; i < DB; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[i][j] *= down;
+        }
+        u32x4 pf[NT][4];
+        float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            float p[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[h][i + j], f, -base));
+              if (!full) p[j] = (ok[h] >> (8 * ((i + j) / 4) + (i + j) % 4)) & 1 ? p[j] : 0.0f;
+              sum[j] += p[j];
+            }
+            uint32_t t[NT];
+            split<NT>(p[0], p[1], t);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) pf[j][2 * h + (i >> 3)][(i & 7) >> 1] = t[j];
+          }
+        l += sum[0] + sum[1];
+        const bool poison = !full && lds.nan[slot] != 0;
+        auto v_at = [&](int db, int st) {
+          const int d = 32 * db + n;
+          return *reinterpret_cast<const u32x4*>(lds.v[buf] + d * (2 * kRows) + 16 * v_piece(d, 2 * st + g));
+        };
+        if (!__builtin_amdgcn_readfirstlane(poison)) {
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int st = 0; st < 4; ++st) {
+              const u32x4 vf = v_at(db, st);
+#pragma unroll
+              for (int j = NT - 1; j >= 0; --j) o[db] = mfma(vf, pf[j][st], o[db]);
+            }
+        } else {
+          // NaN of rows that some do not attend to: counted by those that do, apart
+          u32x4 one[4];
+#pragma unroll
+          for (int st = 0; st < 4; ++st)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int k = 8 * (st & 1) + 2 * i, c0 = 8 * (k / 4) + k % 4;
+              const uint32_t bits = ok[st >> 1] >> c0;
+              one[st][i] = (bits & 1 ? 0x3C00u : 0u) | (bits & 2 ? 0x3C000000u : 0u);
+            }
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            v16f count = v16f{};
+#pragma unroll
+            for (int st = 0; st < 4; ++st) {
+              u32x4 vf = v_at(db, st), is;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const bool lo = (vf[i] & 0x7FFFu) > 0x7C00u, hi = (vf[i] >> 16 & 0x7FFFu) > 0x7C00u;
+                is[i] = (lo ? 0x3C00u : 0u) | (hi ? 0x3C000000u : 0u);
+                vf[i] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+              }
+#pragma unroll
+              for (int j = NT - 1; j >= 0; --j) o[db] = mfma(vf, pf[j][st], o[db]);
+              count = mfma(is, one[st], count);
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[db][j] = count[j] > 0.0f ? __uint_as_float(0x7FC00000u) : o[db][j];
+          }
+        }
+      }
+      if (kb + 1 < kb1) fill(buf ^ 1, slot1);
+      if (wave == 0 && kb + 2 < kb1) publish(slot2);
+      __syncthreads();
+      slot = slot1;
+    }
+
+    // ---- the way out: o over p's sum ----
+    l += __shfl_xor(l, 32, 64);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (mine) {
+      const float times = power(vrun);
+      if (whole) {
+        const int64_t at = int64_t(token) * a.out_stride + int64_t(head0 + hd) * a.c.dim;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int d = 32 * db + 8 * j + 4 * g;
+            if (d >= a.c.dim) continue;
+            v4f x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = o[db][4 * j + i] * inv * times;
+            if (a.type == SHERRY_F32) {
+              *reinterpret_cast<SHERRY_GLOBAL v4f*>(as_global_mut(static_cast<float*>(a.out)) + at + d) = x;
+            } else {
+              uint16_t h[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) h[i] = a.type == SHERRY_BF16 ? to_bf16(x[i]) : to_f16(x[i]);
+              *reinterpret_cast<SHERRY_GLOBAL u32x2*>(as_global_mut(static_cast<uint16_t*>(a.out)) + at + d) =
+                  u32x2{uint32_t(h[0]) | uint32_t(h[1]) << 16, uint32_t(h[2]) | uint32_t(h[3]) << 16};
+            }
+          }
+      } else {
+        const int64_t at = (int64_t(2 * w + (pl.at == 0)) * a.part_rows + r);
+        if (g == 0) as_global_mut(a.stat)[at] = make_float2(base, l);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            v4f x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = o[db][4 * j + i] * inv * times;
+            *reinterpret_cast<SHERRY_GLOBAL v4f*>(as_global_mut(a.sums) + at * DP + 32 * db + 8 * j + 4 * g) = x;
+          }
+      }
+    }
+
+    u += upto - pl.at;
+    if (u >= u_end) return;
+    pl.at = 0;
+    if (pl.t + 1 < s.tiles) {
+      ++pl.t;
+    } else if (pl.head + 1 < a.c.kv * a.gtiles) {
+      ++pl.head;
+      pl.t = 0;
+    } else {
+      pl = find_place(a, u);
+      if (pl.b < 0) return;
+    }
+  }
+}
+
+// Workgroup w joins the tile that begins in run w and goes on behind it; blockIdx.y: a
+// share of its rows.
+template <int DP>
+__global__ __launch_bounds__(256) void tokens_join_kernel(Tokens a) {
+  const int64_t all = total_cost(a), run = run_of(a, all);
+  const int w = blockIdx.x;
+  const int64_t e = (int64_t(w) + 1) * run;
+  if (e >= all) return;
+  const Place pl = find_place(a, e);
+  if (pl.b < 0 || pl.at == 0 || e - pl.at < int64_t(w) * run) return;
+  const int64_t cost = cost_of(a, pl.s, pl.t + 1) - cost_of(a, pl.s, pl.t);
+  const int last = static_cast<int>((e - pl.at + cost - 1) / run);  // the workgroup that ends it
+  const int kvh = pl.head / a.gtiles;
+  const int head0 = kvh * a.group + (pl.head - kvh * a.gtiles) * a.hp;
+  const int heads = (kvh + 1) * a.group - head0 < a.hp ? (kvh + 1) * a.group - head0 : a.hp;
+  constexpr int LANES = DP / 4, STEP = 256 / LANES;  // rows at a time
+  for (int r = blockIdx.y * STEP + threadIdx.x / LANES; r < a.part_rows; r += gridDim.y * STEP) {
+    const int tok = r / a.hp, hd = r - tok * a.hp, d = 4 * (threadIdx.x % LANES);
+    const int64_t in_seq = int64_t(pl.t) * a.per_tile + tok;
+    if (tok >= a.per_tile || in_seq >= pl.s.n || hd >= heads || d >= a.c.dim) continue;
+    float base = kMinusInf, l = 0.0f;
+    v4f sum = {0, 0, 0, 0};
+    for (int i = w; i <= last; ++i) {
+      const int64_t at = int64_t(2 * i + (i == w)) * a.part_rows + r;
+      const float2 st = as_global(a.stat)[at];
+      if (st.y == 0.0f) continue;  // (nothing attended to)
+      const v4f x = *reinterpret_cast<const SHERRY_GLOBAL v4f*>(as_global(a.sums) + at * DP + d);
+      const float to = fmaxf(base, st.x);
+      const float f0 = base == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(base - to);
+      const float f1 = st.y * __builtin_amdgcn_exp2f(st.x - to);
+      l = l * f0 + f1;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[j] = sum[j] * f0 + x[j] * f1;
+      base = to;
+    }
+    const int64_t at = int64_t(pl.s.t0 + in_seq) * a.out_stride + int64_t(head0 + hd) * a.c.dim + d;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) store_from_f32(a.out, at + j, a.type, l == 0.0f ? 0.0f : sum[j] / l);
+  }
+}
+
+int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+constexpr int kJoinShares = 4;
+
+struct Shape {
+  int group, gtiles, hp, per_tile, groups, part_rows;
+  size_t stat_bytes, sum_bytes;
+};
+Shape shape_of(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d) {
+  Shape s{};
+  s.group = d.heads / c.kv_heads;
+  s.hp = s.group < kQRows ? s.group : kQRows;
+  s.gtiles = static_cast<int>(ceil_div(s.group, s.hp));
+  s.per_tile = kQRows / s.hp;
+  const int dp = padded_dim(c.head_dim);
+  // as many workgroups as run at once, but no more than the shortest runs of the
+  // most tiles that the tokens make, each over the whole table
+  const int64_t fit = kCus * waves_for(dp, d.type == SHERRY_F32 ? 2 : 1);
+  const int64_t split = d.tokens / s.per_tile + c.batch;
+  const double tiles = double(split < d.tokens ? split : d.tokens) * c.kv_heads * s.gtiles;
+  const double rows = double(c.table_width) * c.page_size + s.per_tile + kTileCost;
+  const double most = tiles * rows / kMinRun / kXcds + 1;
+  s.groups = static_cast<int>(most < fit / kXcds ? static_cast<int64_t>(most) * kXcds : fit);
+  const int64_t part = int64_t(d.tokens) * s.hp;
+  s.part_rows = static_cast<int>(part < kQRows ? part : kQRows);
+  s.stat_bytes = (size_t(2) * s.groups * s.part_rows * 8 + 255) / 256 * 256;
+  s.sum_bytes = size_t(2) * s.groups * s.part_rows * dp * 4;
+  return s;
+}
+template <int DP>
+int launch_dim(const Tokens& a, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(a.groups));
+  const int rc = a.type == SHERRY_F32 ? launch(tokens_kernel<DP, 2>, grid, dim3(kThreads), 0, s, a)
+                                      : launch(tokens_kernel<DP, 1>, grid, dim3(kThreads), 0, s, a);
+  if (rc != SHERRY_OK) return rc;
+  return launch(tokens_join_kernel<DP>, dim3(static_cast<unsigned>(a.groups), kJoinShares), dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+size_t attend_tokens_workspace(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d) {
+  const Shape s = shape_of(c, d);
+  return s.stat_bytes + s.sum_bytes;
+}
+
+int launch_attend_tokens(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d, hipStream_t s) {
+  const Shape sh = shape_of(c, d);
+  char* ws = static_cast<char*>(d.workspace);
+  const int64_t row = int64_t(d.heads) * c.head_dim;
+  const Tokens a{cache_of(c), d.q, d.out, d.first, d.length, d.mask, reinterpret_cast<float2*>(ws),
+                 reinterpret_cast<float*>(ws + sh.stat_bytes), d.q_stride ? d.q_stride : row,
+                 d.out_stride ? d.out_stride : row, d.mask_stride, d.tokens, d.heads, sh.group, sh.gtiles,
+                 sh.per_tile, sh.hp, d.type, d.window, sh.groups, sh.part_rows, d.scale};
+  switch (padded_dim(c.head_dim)) {
+    case 64: return launch_dim<64>(a, s);
+    case 128: return launch_dim<128>(a, s);
+    default: return launch_dim<256>(a, s);
+  }
+}
+
+}  // namespace sherry
