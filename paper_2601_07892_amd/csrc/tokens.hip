@@ -215,9 +215,10 @@ __device__ __forceinline__ void split(float lo, float hi, uint32_t (&t)[NT]) {
     }
   }
 }
-template <bool HI>
-__device__ __forceinline__ uint32_t code_pair(uint32_t x, float times) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(x), times, HI));
+// Codes 0 and 1, or 2 and 3, of a word, times a power of two (hi: known when compiled).
+__device__ __forceinline__ uint32_t code_pair(uint32_t x, float times, bool hi) {
+  return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(x), times, true)
+                                         : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(x), times, false));
 }
 __device__ __forceinline__ float power(int biased) { return __uint_as_float(uint32_t(biased) << 23); }
 // Biased exponent of a page's scale, 1 .. 254.
@@ -245,36 +246,95 @@ __device__ __forceinline__ int wave_max(int v) {
 
 // K in LDS: rows of DP f16 values, 16 bytes further apart than they are long.
 // V: DP rows of 64 f16 values, those of one step of 16 rows and lane half in a
-// piece of 16 bytes (rows 4 g + 0..3 and 8 + 4 g + 0..3 of the 16); the pieces of a row
-// are permuted so that reads (16 rows at once) and writes (VB rows apart) spread over
-// the banks.
+// piece of 16 bytes (rows 4 g + 0..3 and 8 + 4 g + 0..3 of the 16); piece p of row d is
+// at place p ^ (d / 2 % 8) ^ (d / 16 % 8), so that reads (16 rows at once) and writes (VB
+// rows apart) spread over the banks.
 template <int DP>
 struct Lds {
   static constexpr int KW = DP * 2 + 16, K = kRows * KW, V = DP * kRows * 2;
   alignas(16) char k[2][K];
   alignas(16) char v[2][V];
-  int64_t at[3][kRows];     // where a row begins in its pool; -1: left out
+  int64_t at[3][kRows];     // where a row begins in its pool (left out: a place that can be read)
   float kx[3][kRows], vx[3][kRows];  // what its codes are multiplied by
   uint32_t valid[3][2];
   int kref[3], vref[3];     // biased exponents that the products with kx and vx are over
-  int nan[3];               // some code of V is NaN
+  int part[3];              // not every row of the tile attends to all of it
+  int nan[3];               // and some code of V is NaN:
+  alignas(16) uint8_t odd[2][DP][16];  // of a value and four rows, a bit each
 };
-__device__ __forceinline__ int v_piece(int dim, int piece) { return piece ^ (dim >> 1 & 7) ^ (dim >> 4 & 7); }
 
 // Waves per SIMD that the registers allow.
 __host__ __device__ constexpr int waves_for(int dp, int terms) {
   return dp == 256 ? 1 : dp == 128 ? 2 : terms == 1 ? 3 : 2;
 }
 
-// DP: head_dim rounded up to 64, 128 or 256; NT: terms of q and p.
+// This lane's row of q in terms, over the power of two of its largest value, which
+// goes into the factor of its scores; the sign of scale goes into q.
 template <int DP, int NT>
+__device__ __forceinline__ void load_q(const Tokens& a, int64_t at, bool mine, u32x4 (&qf)[NT][DP / 16], float& factor) {
+  constexpr int KS = DP / 16;
+  const int g = (threadIdx.x & 63) >> 5;
+  float x[KS][8];
+  uint32_t most = 0;
+#pragma unroll
+  for (int st = 0; st < KS; ++st) {
+    const int d = 16 * st + 8 * g;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[st][i] = 0.0f;
+    if (mine && d < a.c.dim) {
+      if (a.type == SHERRY_F32) {
+        const SHERRY_GLOBAL v4f* p =
+            reinterpret_cast<const SHERRY_GLOBAL v4f*>(as_global(static_cast<const float*>(a.q)) + at + d);
+        const v4f lo = p[0], hi = p[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[st][i] = lo[i];
+          x[st][4 + i] = hi[i];
+        }
+      } else {
+        const u32x4 h =
+            *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(static_cast<const uint16_t*>(a.q)) + at + d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint16_t v = static_cast<uint16_t>(h[i >> 1] >> (16 * (i & 1)));
+          x[st][i] = a.type == SHERRY_BF16 ? from_bf16(v) : from_f16(v);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t bits = __float_as_uint(x[st][i]) & 0x7FFFFFFFu;
+      most = bits > most ? bits : most;
+    }
+  }
+  most = max_of_halves(most);
+  constexpr uint32_t kTiny = 0x00400000u;  // 2^-127
+  const uint32_t e = most >> 23 < 254 ? most >> 23 : 254;
+  const float down = __uint_as_float(e < 254 ? (254 - e) << 23 : kTiny) * (a.scale < 0 ? -1.0f : a.scale > 0 ? 1.0f : 0.0f);
+  factor *= __uint_as_float(e > 0 ? e << 23 : kTiny);
+#pragma unroll
+  for (int st = 0; st < KS; ++st)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t t[NT];
+      split<NT>(x[st][2 * i] * down, x[st][2 * i + 1] * down, t);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) qf[j][st][i] = t[j];
+    }
+}
+
+// DP: head_dim rounded up to 64, 128 or 256; NT: terms of q and p; QUADS: page_size % 4
+// == 0, so that four rows of V together have one factor.
+template <int DP, int NT, bool QUADS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_for(DP, NT)))) void tokens_kernel(
     Tokens a) {
   constexpr int KS = DP / 16;   // MFMA steps of a score
   constexpr int DB = DP / 32;   // blocks of 32 values of V
   constexpr int KP = DP / 64;   // 16-byte pieces of K per thread
+  constexpr int KR = 4096 / DP; // rows from one to the next
   constexpr int VB = DP / 16;   // bytes of V per thread and row
   constexpr int VW = VB / 4;
+  constexpr int KW = Lds<DP>::KW, VROW = 2 * kRows;
   __shared__ Lds<DP> lds;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -285,6 +345,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
   const int64_t u_end = u + run < all ? u + run : all;
   if (u >= u_end) return;
   Place pl = find_place(a, u);
+
+  // this thread's places: of K a piece of 16 codes, of V some codes of four rows.
+  // (Values past head_dim are those at 0: q has zeros there, and outputs are not written.)
+  const int k_row = tid / (DP / 16), k_dim = 16 * (tid % (DP / 16));
+  const int k_d = k_dim < a.c.dim ? k_dim : 0, k_to = k_row * KW + 2 * k_dim;
+  const int quad = tid / 16, col = tid % 16, v_d = VB * col < a.c.dim ? VB * col : 0;
+  const int v_to = VB * col * VROW + 8 * (quad >> 1 & 1);
+  const int v_piece = 16 * ((2 * (quad >> 2) + (quad & 1)) ^ (VB * col >> 1 & 7) ^ (VB * col >> 4 & 7));
+  // and of the operands
+  const int k_from = n * KW + 16 * g, v_from = n * VROW, v_swap = (n >> 1 & 7) ^ (n >> 4) ^ g;
 
   for (;;) {
     const Seq& s = pl.s;
@@ -309,65 +379,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
     const int lim = mine ? static_cast<int>(own < a.c.rows ? own : a.c.rows) : 0;
     const int64_t low64 = a.window ? own - a.window : 0;
     const int low = mine && low64 > 0 ? static_cast<int>(low64 < a.c.rows ? low64 : a.c.rows) : 0;
-    // of the wave's rows: every one attends to all of [all_low, all_lim), none outside
-    // [some_low, some_lim)
-    const int some_lim = wave_max(lim), all_low = wave_max(low);
-    const int all_lim = -wave_max(mine ? -lim : -0x7FFFFFFF), some_low = -wave_max(mine ? -low : -0x7FFFFFFF);
+    // some of the wave's rows attend to some of [some_low, some_lim); the first token of
+    // the tile to rows before all_lim, the last one to those from all_low
+    const int some_lim = wave_max(lim), some_low = -wave_max(mine ? -low : -0x7FFFFFFF);
+    const int64_t own0 = s.len + int64_t(pl.t) * a.per_tile + 1;
+    const int all_lim = __builtin_amdgcn_readfirstlane(static_cast<int>(own0 < end ? own0 : end));
+    const int64_t low1 = a.window ? own0 + a.per_tile - a.window : 0;
+    const int all_low = __builtin_amdgcn_readfirstlane(static_cast<int>(low1 < 0 ? 0 : low1 < end ? low1 : end));
 
     // q, over the power of two of its largest value
     u32x4 qf[NT][KS];
     float factor = fabsf(a.scale) * kLog2e;
-    {
-      float x[KS][8];
-      uint32_t most = 0;
-      const int64_t at = int64_t(token) * a.q_stride + int64_t(head0 + (mine ? hd : 0)) * a.c.dim;
-#pragma unroll
-      for (int st = 0; st < KS; ++st) {
-        const int d = 16 * st + 8 * g;
-        const bool in = mine && d < a.c.dim;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[st][i] = 0.0f;
-        if (in) {
-          if (a.type == SHERRY_F32) {
-            const SHERRY_GLOBAL v4f* p =
-                reinterpret_cast<const SHERRY_GLOBAL v4f*>(as_global(static_cast<const float*>(a.q)) + at + d);
-            const v4f lo = p[0], hi = p[1];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              x[st][i] = lo[i];
-              x[st][4 + i] = hi[i];
-            }
-          } else {
-            const u32x4 h =
-                *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(static_cast<const uint16_t*>(a.q)) + at + d);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint16_t v = static_cast<uint16_t>(h[i >> 1] >> (16 * (i & 1)));
-              x[st][i] = a.type == SHERRY_BF16 ? from_bf16(v) : from_f16(v);
-            }
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t bits = __float_as_uint(x[st][i]) & 0x7FFFFFFFu;
-          most = bits > most ? bits : most;
-        }
-      }
-      most = max_of_halves(most);
-      constexpr uint32_t kTiny = 0x00400000u;  // 2^-127
-      const uint32_t e = most >> 23 < 254 ? most >> 23 : 254;
-      const float down = __uint_as_float(e < 254 ? (254 - e) << 23 : kTiny) * (a.scale < 0 ? -1.0f : 1.0f);
-      factor *= __uint_as_float(e > 0 ? e << 23 : kTiny);
-#pragma unroll
-      for (int st = 0; st < KS; ++st)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t t[NT];
-          split<NT>(x[st][2 * i] * down, x[st][2 * i + 1] * down, t);
-#pragma unroll
-          for (int j = 0; j < NT; ++j) qf[j][st][i] = t[j];
-        }
-    }
+    load_q<DP, NT>(a, int64_t(token) * a.q_stride + int64_t(head0 + (mine ? hd : 0)) * a.c.dim, mine, qf, factor);
 
     v16f o[DB];
 #pragma unroll
@@ -377,125 +400,222 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 
     // ---- what the first wave finds out about a block of rows ----
     int next_page = -1, next_mask = 1, seen_vref = 1;
-    int64_t next_at = -1;
+    int64_t next_at = 0;
     float next_ks = 0, next_vs = 0;
+    bool next_ok = false;
     auto look_page = [&](int kb) {  // reads its pages
       const int row = kb * kRows + lane;
       const bool in = kb < kb1 && row < end;
       next_page = in ? as_global(a.c.table)[int64_t(b) * a.c.width + a.c.by_page.div(row)] : -1;
       next_mask = in && a.mask ? as_global(a.mask)[int64_t(b) * a.mask_stride + row] : 1;
     };
-    auto look_scale = [&](int kb) {  // and then their scales
+    auto look_scale = [&](int kb) {  // and then their scales (rows of no page: any place that can be read)
       const int row = kb * kRows + lane;
-      const bool ok = next_page >= 0 && next_page < a.c.pages && next_mask != 0;
-      next_at = -1;
-      if (ok) {
-        const int off = row - static_cast<int>(a.c.by_page.div(row)) * a.c.page_size;
-        next_at = a.c.at(next_page, kvh) + int64_t(off) * a.c.dim;
-        next_ks = as_global(a.c.ks)[a.c.scale_at(next_page, kvh)];
-        next_vs = as_global(a.c.vs)[a.c.scale_at(next_page, kvh)];
-      }
+      const bool there = next_page >= 0 && next_page < a.c.pages;
+      next_ok = there && next_mask != 0;
+      const int page = there ? next_page : 0;
+      const int off = there ? row - static_cast<int>(a.c.by_page.div(row)) * a.c.page_size : 0;
+      next_at = a.c.at(page, kvh) + int64_t(off) * a.c.dim;
+      next_ks = as_global(a.c.ks)[a.c.scale_at(page, kvh)];
+      next_vs = as_global(a.c.vs)[a.c.scale_at(page, kvh)];
     };
-    auto publish = [&](int slot) {
-      const bool ok = next_at >= 0;
-      const int ke = ok ? exponent(next_ks) : 1, ve = ok ? exponent(next_vs) : 1;
-      const int kref = wave_max(ke), vmax = wave_max(ve);
+    auto publish = [&](int kb, int slot) {
+      // (a row that is masked shares its factor with others of its page)
+      const int ke = exponent(next_ks), ve = exponent(next_vs);
+      const int kref = wave_max(next_ok ? ke : 1), vmax = wave_max(next_ok ? ve : 1);
       seen_vref = vmax > seen_vref ? vmax : seen_vref;
+      auto over = [](int ref, int e) { return power(ref - e < 0 ? 127 : ref - e < 126 ? 127 - (ref - e) : 1); };
       lds.at[slot][lane] = next_at;
-      lds.kx[slot][lane] = power(127 - (kref - ke < 126 ? kref - ke : 126));
-      lds.vx[slot][lane] = power(127 - (seen_vref - ve < 126 ? seen_vref - ve : 126));
-      const uint64_t valid = __ballot(ok);
+      lds.kx[slot][lane] = over(kref, ke);
+      lds.vx[slot][lane] = over(seen_vref, ve);
+      const uint64_t valid = __ballot(next_ok);
+      const int row0 = kb * kRows;
       if (lane == 0) {
         lds.valid[slot][0] = static_cast<uint32_t>(valid);
         lds.valid[slot][1] = static_cast<uint32_t>(valid >> 32);
+        lds.part[slot] = ~valid != 0 || row0 + kRows > all_lim || row0 < all_low;
         lds.kref[slot] = kref;
         lds.vref[slot] = seen_vref;
         lds.nan[slot] = 0;
       }
     };
     // ---- a block's rows, from the pools to LDS ----
-    uint32_t kr[KP][4], vr[4][VW];
+    u32x4 kr[KP];
+    uint32_t vr[4][VW];
     auto load = [&](int slot) {
 #pragma unroll
-      for (int i = 0; i < KP; ++i) {
-        const int p = tid + kThreads * i, row = p / (DP / 16), d = 16 * (p % (DP / 16));
-        const int64_t at = lds.at[slot][row];
-        u32x4 x = {0, 0, 0, 0};
-        if (at >= 0 && d < a.c.dim) x = *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(a.c.k) + at + d);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) kr[i][j] = x[j];
-      }
-      const int quad = tid / 16, d = VB * (tid % 16);
+      for (int i = 0; i < KP; ++i)
+        kr[i] = *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(a.c.k) + lds.at[slot][k_row + KR * i] + k_d);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int64_t at = lds.at[slot][4 * quad + j];
-        const bool in = at >= 0 && d < a.c.dim;
-        const SHERRY_GLOBAL char* from = as_global(a.c.v) + at + d;
+        const SHERRY_GLOBAL char* from = as_global(a.c.v) + lds.at[slot][4 * quad + j] + v_d;
         if constexpr (VW == 4) {
-          u32x4 x = {0, 0, 0, 0};
-          if (in) x = *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(from);
+          const u32x4 x = *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(from);
 #pragma unroll
           for (int i = 0; i < 4; ++i) vr[j][i] = x[i];
         } else if constexpr (VW == 2) {
-          u32x2 x = {0, 0};
-          if (in) x = *reinterpret_cast<const SHERRY_GLOBAL u32x2*>(from);
+          const u32x2 x = *reinterpret_cast<const SHERRY_GLOBAL u32x2*>(from);
           vr[j][0] = x[0];
           vr[j][1] = x[1];
         } else {
-          vr[j][0] = in ? *reinterpret_cast<const SHERRY_GLOBAL uint32_t*>(from) : 0u;
+          vr[j][0] = *reinterpret_cast<const SHERRY_GLOBAL uint32_t*>(from);
         }
       }
     };
     auto fill = [&](int buf, int slot) {
+      if (__builtin_amdgcn_readfirstlane(lds.part[slot])) {
+        // NaN must not reach rows of q that do not attend to it: it is 0 here, and noted
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+          uint32_t bits = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t t = ((vr[j][i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+            bits |= t >> (7 - j);
+            vr[j][i] &= ~(t | (t - (t >> 7)));
+          }
+          any |= bits;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) lds.odd[buf][VB * col + 4 * i + e][quad] = static_cast<uint8_t>(bits >> (8 * e));
+        }
+        if (any) lds.nan[slot] = 1;
+      }
 #pragma unroll
       for (int i = 0; i < KP; ++i) {
-        const int p = tid + kThreads * i, row = p / (DP / 16), d = 16 * (p % (DP / 16));
-        const float times = lds.kx[slot][row];
+        const float times = lds.kx[slot][k_row + KR * i];
         u32x4 x[2];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          x[j >> 1][2 * (j & 1)] = code_pair<false>(kr[i][j], times);
-          x[j >> 1][2 * (j & 1) + 1] = code_pair<true>(kr[i][j], times);
+          x[j >> 1][2 * (j & 1)] = code_pair(kr[i][j], times, false);
+          x[j >> 1][2 * (j & 1) + 1] = code_pair(kr[i][j], times, true);
         }
-        u32x4* to = reinterpret_cast<u32x4*>(lds.k[buf] + row * Lds<DP>::KW + 2 * d);
+        u32x4* to = reinterpret_cast<u32x4*>(lds.k[buf] + k_to + KR * i * KW);
         to[0] = x[0];
         to[1] = x[1];
       }
-      const int quad = tid / 16, d0 = VB * (tid % 16);
-      const int piece = 2 * (quad >> 2) + (quad & 1), half = 8 * (quad >> 1 & 1);
-      // (rows of a quad lie in one page or in several: their factors)
-      const float4 times = *reinterpret_cast<const float4*>(&lds.vx[slot][4 * quad]);
-      const bool same = times.x == times.y && times.x == times.z && times.x == times.w;
-      uint32_t odd = 0;
+      float times[4] = {lds.vx[slot][4 * quad], 0, 0, 0};
+      if constexpr (!QUADS)
 #pragma unroll
-      for (int i = 0; i < VW; ++i) {
+        for (int j = 1; j < 4; ++j) times[j] = lds.vx[slot][4 * quad + j];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) odd |= ((vr[j][i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+      for (int i = 0; i < VW; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           u32x2 x;
-          if (same) {
+          if constexpr (QUADS) {
             const uint32_t sel = e & 2 ? 0x07030602u : 0x05010400u;  // (values e and e ^ 1 of two rows)
-            const uint32_t p01 = __builtin_amdgcn_perm(vr[1][i], vr[0][i], sel);
-            const uint32_t p23 = __builtin_amdgcn_perm(vr[3][i], vr[2][i], sel);
-            x[0] = e & 1 ? code_pair<true>(p01, times.x) : code_pair<false>(p01, times.x);
-            x[1] = e & 1 ? code_pair<true>(p23, times.x) : code_pair<false>(p23, times.x);
+            x[0] = code_pair(__builtin_amdgcn_perm(vr[1][i], vr[0][i], sel), times[0], e & 1);
+            x[1] = code_pair(__builtin_amdgcn_perm(vr[3][i], vr[2][i], sel), times[0], e & 1);
           } else {
             uint32_t y[4];
-            const float t[4] = {times.x, times.y, times.z, times.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const uint32_t z = e & 2 ? code_pair<true>(vr[j][i], t[j]) : code_pair<false>(vr[j][i], t[j]);
+              const uint32_t z = code_pair(vr[j][i], times[j], e & 2);
               y[j] = e & 1 ? z >> 16 : z & 0xFFFFu;
             }
             x[0] = y[0] | y[1] << 16;
             x[1] = y[2] | y[3] << 16;
           }
-          const int d = d0 + 4 * i + e;
-          *reinterpret_cast<u32x2*>(lds.v[buf] + d * (2 * kRows) + 16 * v_piece(d, piece) + half) = x;
+          constexpr int kSwap = VB / 2 < 8 ? VB / 2 : 8;
+          const int d = 4 * i + e;
+          *reinterpret_cast<u32x2*>(lds.v[buf] + v_to + (v_piece ^ 16 * (d / 2 % kSwap)) + d * VROW) = x;
+        }
+    };
+
+    // ---- a block's scores, probabilities and outputs ----
+    auto attend = [&](int kb, int buf, int slot) {
+      const int row0 = kb * kRows;
+      const bool part = __builtin_amdgcn_readfirstlane(lds.part[slot]) != 0;
+      const int vref = __builtin_amdgcn_readfirstlane(lds.vref[slot]);
+      // (above 0, so that -infinity stays what it is)
+      const float f = fmaxf(factor * power(__builtin_amdgcn_readfirstlane(lds.kref[slot])), 0x1p-126f);
+      const char* kp = lds.k[buf] + k_from;
+      const char* vp = lds.v[buf] + v_from;
+      v16f sc[2] = {v16f{}, v16f{}};
+#pragma unroll
+      for (int st = 0; st < KS; ++st)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const u32x4 kf = *reinterpret_cast<const u32x4*>(kp + 32 * h * KW + 32 * st);
+#pragma unroll
+          for (int j = NT - 1; j >= 0; --j) sc[h] = mfma(kf, qf[j][st], sc[h]);
+        }
+      // the rows that this row of q attends to
+      auto attended = [&](int h) {
+        const int most = lim - row0 - 32 * h, least = low - row0 - 32 * h;
+        const uint32_t bits = most >= 32 ? ~0u : most > 0 ? (1u << most) - 1 : 0u;
+        return bits & (least >= 32 ? 0u : least > 0 ? ~0u << least : ~0u) & lds.valid[slot][h];
+      };
+      if (part) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t ok = attended(h) >> (4 * g);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[h][i] = (ok >> (8 * (i / 4) + i % 4)) & 1 ? sc[h][i] : kMinusInf;
         }
       }
-      if (odd) lds.nan[slot] = 1;
+      float top = sc[0][0];
+#pragma unroll
+      for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i >> 4][i & 15]);
+      top = max_of_halves(top) * f;
+      if (__any(top > m + kLazy) || vref > vrun) {
+        const bool up = top > m;
+        const float to = up ? top - kUp : base;
+        float down = m == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(base - to);
+        if (up) {
+          base = to;
+          m = top;
+        }
+        l *= down;
+        down *= power(vref - vrun < 126 ? 127 - (vref - vrun) : 1);
+        vrun = vref;
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o[i][j] *= down;
+      }
+      float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int st = 0; st < 4; ++st) {
+        u32x4 pf[NT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float p[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[st >> 1][8 * (st & 1) + 2 * i + j], f, -base));
+            sum[j] += p[j];
+          }
+          uint32_t t[NT];
+          split<NT>(p[0], p[1], t);
+#pragma unroll
+          for (int j = 0; j < NT; ++j) pf[j][i] = t[j];
+        }
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const u32x4 vf =
+              *reinterpret_cast<const u32x4*>(vp + 16 * (2 * (st ^ (db & 3)) ^ v_swap) + 32 * db * VROW);
+#pragma unroll
+          for (int j = NT - 1; j >= 0; --j) o[db] = mfma(vf, pf[j], o[db]);
+        }
+      }
+      l += sum[0] + sum[1];
+      if (part && __builtin_amdgcn_readfirstlane(lds.nan[slot])) {
+        u32x4 mine_of;  // the attended rows, four a byte
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          const uint32_t x = attended(h >> 1) >> (16 * (h & 1));
+          mine_of[h] = (x & 0xF) | (x & 0xF0) << 4 | (x & 0xF00) << 8 | (x & 0xF000) << 12;
+        }
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(lds.odd[buf][32 * db + 8 * (j / 4) + 4 * g + j % 4]) & mine_of;
+            o[db][j] = (x[0] | x[1] | x[2] | x[3]) ? __uint_as_float(0x7FC00000u) : o[db][j];
+          }
+      }
     };
 
     __syncthreads();  // (the tile before has been read from LDS)
@@ -504,10 +624,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         look_page(kb0);
         look_scale(kb0);
         look_page(kb0 + 1);
-        publish(0);
+        publish(kb0, 0);
         look_scale(kb0 + 1);
         look_page(kb0 + 2);
-        publish(1);
+        publish(kb0 + 1, 1);
       }
       __syncthreads();
       load(0);
@@ -519,128 +639,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       const int buf = (kb - kb0) & 1, slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
       // the rows of the next block, and what the one after it is
       if (kb + 1 < kb1) load(slot1);
-      if (wave == 0 && kb + 2 < kb1) {
+      if (wave == 0) {
         look_scale(kb + 2);
         look_page(kb + 3);
       }
-      const int row0 = kb * kRows;
-      if (row0 < some_lim && row0 + kRows > some_low) {
-        const int vref = __builtin_amdgcn_readfirstlane(lds.vref[slot]);
-        const float f = factor * power(__builtin_amdgcn_readfirstlane(lds.kref[slot]));
-        const uint32_t valid[2] = {static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(lds.valid[slot][0])),
-                                   static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(lds.valid[slot][1]))};
-        const bool full = (valid[0] & valid[1]) == ~0u && row0 + kRows <= all_lim && row0 >= all_low;
-        v16f sc[2] = {v16f{}, v16f{}};
-#pragma unroll
-        for (int st = 0; st < KS; ++st)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const u32x4 kf = *reinterpret_cast<const u32x4*>(lds.k[buf] + (32 * h + n) * Lds<DP>::KW + 32 * st + 16 * g);
-#pragma unroll
-            for (int j = NT - 1; j >= 0; --j) sc[h] = mfma(kf, qf[j][st], sc[h]);
-          }
-        uint32_t ok[2] = {~0u, ~0u};  // bit 8 (i / 4) + i % 4: score i is attended to
-        if (!full) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int r0 = row0 + 32 * h;
-            const int most = lim - r0, least = low - r0;
-            uint32_t bits = most >= 32 ? ~0u : most > 0 ? (1u << most) - 1 : 0u;
-            bits &= least >= 32 ? 0u : least > 0 ? ~0u << least : ~0u;
-            ok[h] = (bits & valid[h]) >> (4 * g);
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              sc[h][i] = (ok[h] >> (8 * (i / 4) + i % 4)) & 1 ? sc[h][i] : kMinusInf;
-          }
-        }
-        float top = sc[0][0];
-#pragma unroll
-        for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i >> 4][i & 15]);
-        top = max_of_halves(top);
-        top = top == kMinusInf ? kMinusInf : top * f;
-        if (__any(top > m + kLazy) || vref > vrun) {
-          const bool up = top > m;
-          const float to = up ? top - kUp : base;
-          float down = m == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(base - to);
-          if (up) {
-            base = to;
-            m = top;
-          }
-          l *= down;
-          down *= power(vref - vrun < 126 ? 127 - (vref - vrun) : 1);
-          vrun = vref;
-#pragma unroll
-          for (int i = 0; i < DB; ++i)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) o[i][j] *= down;
-        }
-        u32x4 pf[NT][4];
-        float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            float p[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[h][i + j], f, -base));
-              if (!full) p[j] = (ok[h] >> (8 * ((i + j) / 4) + (i + j) % 4)) & 1 ? p[j] : 0.0f;
-              sum[j] += p[j];
-            }
-            uint32_t t[NT];
-            split<NT>(p[0], p[1], t);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) pf[j][2 * h + (i >> 3)][(i & 7) >> 1] = t[j];
-          }
-        l += sum[0] + sum[1];
-        const bool poison = !full && lds.nan[slot] != 0;
-        auto v_at = [&](int db, int st) {
-          const int d = 32 * db + n;
-          return *reinterpret_cast<const u32x4*>(lds.v[buf] + d * (2 * kRows) + 16 * v_piece(d, 2 * st + g));
-        };
-        if (!__builtin_amdgcn_readfirstlane(poison)) {
-#pragma unroll
-          for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int st = 0; st < 4; ++st) {
-              const u32x4 vf = v_at(db, st);
-#pragma unroll
-              for (int j = NT - 1; j >= 0; --j) o[db] = mfma(vf, pf[j][st], o[db]);
-            }
-        } else {
-          // NaN of rows that some do not attend to: counted by those that do, apart
-          u32x4 one[4];
-#pragma unroll
-          for (int st = 0; st < 4; ++st)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int k = 8 * (st & 1) + 2 * i, c0 = 8 * (k / 4) + k % 4;
-              const uint32_t bits = ok[st >> 1] >> c0;
-              one[st][i] = (bits & 1 ? 0x3C00u : 0u) | (bits & 2 ? 0x3C000000u : 0u);
-            }
-#pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            v16f count = v16f{};
-#pragma unroll
-            for (int st = 0; st < 4; ++st) {
-              u32x4 vf = v_at(db, st), is;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const bool lo = (vf[i] & 0x7FFFu) > 0x7C00u, hi = (vf[i] >> 16 & 0x7FFFu) > 0x7C00u;
-                is[i] = (lo ? 0x3C00u : 0u) | (hi ? 0x3C000000u : 0u);
-                vf[i] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
-              }
-#pragma unroll
-              for (int j = NT - 1; j >= 0; --j) o[db] = mfma(vf, pf[j][st], o[db]);
-              count = mfma(is, one[st], count);
-            }
-#pragma unroll
-            for (int j = 0; j < 16; ++j) o[db][j] = count[j] > 0.0f ? __uint_as_float(0x7FC00000u) : o[db][j];
-          }
-        }
-      }
+      if (kb * kRows < some_lim && (kb + 1) * kRows > some_low) attend(kb, buf, slot);
       if (kb + 1 < kb1) fill(buf ^ 1, slot1);
-      if (wave == 0 && kb + 2 < kb1) publish(slot2);
+      if (wave == 0) publish(kb + 2, slot2);
       __syncthreads();
       slot = slot1;
     }
@@ -770,11 +775,15 @@ Shape shape_of(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d) {
   s.sum_bytes = size_t(2) * s.groups * s.part_rows * dp * 4;
   return s;
 }
+template <int DP, bool QUADS>
+int launch_terms(const Tokens& a, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(a.groups));
+  return a.type == SHERRY_F32 ? launch(tokens_kernel<DP, 2, QUADS>, grid, dim3(kThreads), 0, s, a)
+                              : launch(tokens_kernel<DP, 1, QUADS>, grid, dim3(kThreads), 0, s, a);
+}
 template <int DP>
 int launch_dim(const Tokens& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(a.groups));
-  const int rc = a.type == SHERRY_F32 ? launch(tokens_kernel<DP, 2>, grid, dim3(kThreads), 0, s, a)
-                                      : launch(tokens_kernel<DP, 1>, grid, dim3(kThreads), 0, s, a);
+  const int rc = a.c.page_size % 4 == 0 ? launch_terms<DP, true>(a, s) : launch_terms<DP, false>(a, s);
   if (rc != SHERRY_OK) return rc;
   return launch(tokens_join_kernel<DP>, dim3(static_cast<unsigned>(a.groups), kJoinShares), dim3(256), 0, s, a);
 }
