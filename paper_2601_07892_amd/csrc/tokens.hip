@@ -235,13 +235,16 @@ __device__ __forceinline__ uint32_t max_of_halves(uint32_t v) {
   const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
   return a[0] > a[1] ? a[0] : a[1];
 }
+// The largest of a value over the wave (steps inside 16 lanes, then across them).
 __device__ __forceinline__ int wave_max(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const int u = __shfl_xor(v, o, 64);
-    v = v > u ? v : u;
-  }
-  return __builtin_amdgcn_readfirstlane(v);
+  auto with = [&](int u) { v = v > u ? v : u; };
+  with(__builtin_amdgcn_update_dpp(v, v, 0x111, 0xF, 0xF, false));
+  with(__builtin_amdgcn_update_dpp(v, v, 0x112, 0xF, 0xF, false));
+  with(__builtin_amdgcn_update_dpp(v, v, 0x114, 0xF, 0xF, false));
+  with(__builtin_amdgcn_update_dpp(v, v, 0x118, 0xF, 0xF, false));
+  with(__builtin_amdgcn_update_dpp(v, v, 0x142, 0xA, 0xF, false));
+  with(__builtin_amdgcn_update_dpp(v, v, 0x143, 0xC, 0xF, false));
+  return __builtin_amdgcn_readlane(v, 63);
 }
 
 // K in LDS: rows of DP f16 values, 16 bytes further apart than they are long.
@@ -256,9 +259,10 @@ struct Lds {
   alignas(16) char v[2][V];
   int64_t at[3][kRows];     // where a row begins in its pool (left out: a place that can be read)
   float kx[3][kRows], vx[3][kRows];  // what its codes are multiplied by
-  uint32_t valid[3][2];
-  int kref[3], vref[3];     // biased exponents that the products with kx and vx are over
-  int part[3];              // not every row of the tile attends to all of it
+  // of a block: its rows that there are (64 bits); kref | vref << 8 | part << 16, the biased
+  // exponents that the products with kx and vx are over, and whether not every row of the
+  // tile attends to all of it
+  u32x4 about[3];
   int nan[3];               // and some code of V is NaN:
   alignas(16) uint8_t odd[2][DP][16];  // of a value and four rows, a bit each
 };
@@ -321,6 +325,19 @@ __device__ __forceinline__ void load_q(const Tokens& a, int64_t at, bool mine, u
 #pragma unroll
       for (int j = 0; j < NT; ++j) qf[j][st][i] = t[j];
     }
+}
+
+// Nothing is moved over this when compiled: operands are read from LDS a group ahead of
+// their use.  (Left to itself the compiler read each right before its use, and waited for it.)
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+// N times an MFMA and VALU other instructions.
+template <int N, int VALU>
+__device__ __forceinline__ void take_turns() {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x402, VALU, 0);
+  }
 }
 
 // DP: head_dim rounded up to 64, 128 or 256; NT: terms of q and p; QUADS: page_size % 4
@@ -431,11 +448,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       const uint64_t valid = __ballot(next_ok);
       const int row0 = kb * kRows;
       if (lane == 0) {
-        lds.valid[slot][0] = static_cast<uint32_t>(valid);
-        lds.valid[slot][1] = static_cast<uint32_t>(valid >> 32);
-        lds.part[slot] = ~valid != 0 || row0 + kRows > all_lim || row0 < all_low;
-        lds.kref[slot] = kref;
-        lds.vref[slot] = seen_vref;
+        const bool part = ~valid != 0 || row0 + kRows > all_lim || row0 < all_low;
+        lds.about[slot] = u32x4{static_cast<uint32_t>(valid), static_cast<uint32_t>(valid >> 32),
+                                static_cast<uint32_t>(kref | seen_vref << 8 | int(part) << 16), 0};
         lds.nan[slot] = 0;
       }
     };
@@ -463,7 +478,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       }
     };
     auto fill = [&](int buf, int slot) {
-      if (__builtin_amdgcn_readfirstlane(lds.part[slot])) {
+      if (__builtin_amdgcn_readfirstlane(lds.about[slot][2]) >> 16) {
         // NaN must not reach rows of q that do not attend to it: it is 0 here, and noted
         uint32_t any = 0;
 #pragma unroll
@@ -526,26 +541,45 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
     // ---- a block's scores, probabilities and outputs ----
     auto attend = [&](int kb, int buf, int slot) {
       const int row0 = kb * kRows;
-      const bool part = __builtin_amdgcn_readfirstlane(lds.part[slot]) != 0;
-      const int vref = __builtin_amdgcn_readfirstlane(lds.vref[slot]);
-      // (above 0, so that -infinity stays what it is)
-      const float f = fmaxf(factor * power(__builtin_amdgcn_readfirstlane(lds.kref[slot])), 0x1p-126f);
       const char* kp = lds.k[buf] + k_from;
       const char* vp = lds.v[buf] + v_from;
+      constexpr int GROUP = 4, GROUPS = 2 * KS / GROUP;
+      u32x4 kf[2][GROUP], vf[2][DB];
+      auto read_k = [&](int grp) {  // of 16 values after 16, both halves of the rows
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i)
+          kf[grp & 1][i] = *reinterpret_cast<const u32x4*>(kp + 32 * (i & 1) * KW + 32 * (grp * GROUP / 2 + i / 2));
+      };
+      auto read_v = [&](int st) {  // of 16 rows after 16
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          vf[st & 1][db] = *reinterpret_cast<const u32x4*>(vp + 16 * (2 * (st ^ (db & 3)) ^ v_swap) + 32 * db * VROW);
+      };
+      const u32x4 about = lds.about[slot];
+      read_k(0);
       v16f sc[2] = {v16f{}, v16f{}};
 #pragma unroll
-      for (int st = 0; st < KS; ++st)
+      for (int grp = 0; grp < GROUPS; ++grp) {
+        if (grp + 1 < GROUPS) read_k(grp + 1);
+        else read_v(0);
+        fence();
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const u32x4 kf = *reinterpret_cast<const u32x4*>(kp + 32 * h * KW + 32 * st);
+        for (int i = 0; i < GROUP; ++i)
 #pragma unroll
-          for (int j = NT - 1; j >= 0; --j) sc[h] = mfma(kf, qf[j][st], sc[h]);
-        }
+          for (int j = NT - 1; j >= 0; --j)
+            sc[i & 1] = mfma(kf[grp & 1][i], qf[j][grp * GROUP / 2 + i / 2], sc[i & 1]);
+        fence();
+      }
+      const uint32_t refs = __builtin_amdgcn_readfirstlane(about[2]);
+      const bool part = refs >> 16;
+      const int vref = refs >> 8 & 0xFF;
+      // (above 0, so that -infinity stays what it is)
+      const float f = fmaxf(factor * power(refs & 0xFF), 0x1p-126f);
       // the rows that this row of q attends to
       auto attended = [&](int h) {
         const int most = lim - row0 - 32 * h, least = low - row0 - 32 * h;
         const uint32_t bits = most >= 32 ? ~0u : most > 0 ? (1u << most) - 1 : 0u;
-        return bits & (least >= 32 ? 0u : least > 0 ? ~0u << least : ~0u) & lds.valid[slot][h];
+        return bits & (least >= 32 ? 0u : least > 0 ? ~0u << least : ~0u) & about[h];
       };
       if (part) {
 #pragma unroll
@@ -576,9 +610,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
           for (int j = 0; j < 16; ++j) o[i][j] *= down;
       }
       float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-      for (int st = 0; st < 4; ++st) {
-        u32x4 pf[NT];
+      u32x4 pf[2][NT];
+      auto probabilities = [&](int st) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float p[2];
@@ -590,15 +623,21 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
           uint32_t t[NT];
           split<NT>(p[0], p[1], t);
 #pragma unroll
-          for (int j = 0; j < NT; ++j) pf[j][i] = t[j];
+          for (int j = 0; j < NT; ++j) pf[st & 1][j][i] = t[j];
         }
+      };
+      probabilities(0);
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const u32x4 vf =
-              *reinterpret_cast<const u32x4*>(vp + 16 * (2 * (st ^ (db & 3)) ^ v_swap) + 32 * db * VROW);
+      for (int st = 0; st < 4; ++st) {
+        if (st < 3) read_v(st + 1);
+        fence();
+        if (st < 3) probabilities(st + 1);
 #pragma unroll
-          for (int j = NT - 1; j >= 0; --j) o[db] = mfma(vf, pf[j], o[db]);
-        }
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int j = NT - 1; j >= 0; --j) o[db] = mfma(vf[st & 1][db], pf[st & 1][j], o[db]);
+        if (st < 3) take_turns<DB * NT, (28 + 24 * (NT - 1)) / (DB * NT)>();
+        fence();
       }
       l += sum[0] + sum[1];
       if (part && __builtin_amdgcn_readfirstlane(lds.nan[slot])) {
@@ -637,12 +676,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
     int slot = 0;
     for (int kb = kb0; kb < kb1; ++kb) {
       const int buf = (kb - kb0) & 1, slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
-      // the rows of the next block, and what the one after it is
-      if (kb + 1 < kb1) load(slot1);
+      // what the blocks after the next one are (first: its answers come in order), and the
+      // rows of the next one
       if (wave == 0) {
         look_scale(kb + 2);
         look_page(kb + 3);
       }
+      if (kb + 1 < kb1) load(slot1);
       if (kb * kRows < some_lim && (kb + 1) * kRows > some_low) attend(kb, buf, slot);
       if (kb + 1 < kb1) fill(buf ^ 1, slot1);
       if (wave == 0) publish(kb + 2, slot2);
