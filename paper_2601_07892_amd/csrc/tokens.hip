@@ -35,7 +35,11 @@
 // 2^10, are one term for 16-bit outputs (error 2^-11 of each at most, where the output's own
 // rounding is 2^-8 or 2^-11), two for fp32.  Scores, maxima, sums and outputs are
 // fp32; the maximum is taken anew only when a score passes it by 2^5.
+#include <type_traits>
+
 #include "cache_internal.h"
+
+#define SHERRY_INLINE __attribute__((always_inline))
 
 namespace sherry {
 namespace {
@@ -51,12 +55,18 @@ constexpr int kQRows = 32 * kWaves;  // of a tile
 constexpr int kRows = 64;            // of K and V at a time
 constexpr int kCus = 256, kXcds = 8;
 // What a tile costs besides its rows (its q, the first loads, the way out), in rows.
-constexpr int kTileCost = 128;
-constexpr int kMinRun = 384;         // the shortest run, in rows of cost
+constexpr int kTileCost = 256;
+constexpr int kMinRun = 512;         // the shortest run, in rows of cost
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kMinusInf = -__builtin_huge_valf();
 constexpr float kUp = 10.0f;         // p is held times 2^kUp
 constexpr float kLazy = 5.0f;        // scores may pass the maximum by this
+
+// A tile that workgroup w has the beginning of, and `last` the end: its tokens [first, first
+// + tokens) and query heads.  tokens = 0: there is none.
+struct Split {
+  int first, tokens, head0, heads, last;
+};
 
 struct Tokens {
   Cache c;
@@ -69,9 +79,11 @@ struct Tokens {
   // one that begins in its run and goes on behind it (2 w + 1)
   float2* stat;  // [part][part_rows]: where p is 1, in units of ln 2, and the sum of p
   float* sums;   // [part][part_rows][DP]: outputs of these rows
+  Split* split;  // [workgroup]
   int64_t q_stride, out_stride, mask_stride;
   int tokens, heads, group, gtiles, per_tile, hp, type, window, groups, part_rows;
   float scale;
+  FastDiv by_hp, by_tile;
 };
 
 // ---- which tiles a workgroup takes -------------------------------------------
@@ -84,7 +96,7 @@ __device__ __forceinline__ Seq seq_of(const Tokens& a, int b) {
   const int f0 = as_global(a.first)[b], f1 = as_global(a.first)[b + 1];
   const int t0 = f0 < 0 ? 0 : f0 < a.tokens ? f0 : a.tokens;
   const int t1 = f1 < t0 ? t0 : f1 < a.tokens ? f1 : a.tokens;
-  return Seq{t0, t1 - t0, a.c.length(a.length, b), (t1 - t0 + a.per_tile - 1) / a.per_tile};
+  return Seq{t0, t1 - t0, a.c.length(a.length, b), static_cast<int>(a.by_tile.div(t1 - t0 + a.per_tile - 1))};
 }
 // The rows that the first k tiles of a head attend to, and kTileCost each: tile t the
 // rows from max(0, len + 1 - window + t r) to len + min(n, (t + 1) r), r = tokens per tile.
@@ -94,10 +106,24 @@ __device__ __forceinline__ int64_t cost_of(const Tokens& a, const Seq& s, int k)
   if (k == s.tiles) sum -= kk * r - s.n;
   if (a.window) {
     const int64_t low = int64_t(s.len) + 1 - a.window;
-    const int64_t from = low >= 0 ? 0 : (-low + r - 1) / r;  // the first tile that leaves rows out
+    // (the first tile that leaves rows out)
+    const int64_t from = low >= 0 ? 0 : int64_t(a.by_tile.div(static_cast<uint32_t>(-low - 1))) + 1;
     if (from < kk) sum -= (kk - from) * low + r * ((kk * (kk - 1) - from * (from - 1)) / 2);
   }
   return sum;
+}
+
+// What tile t alone costs.
+__device__ __forceinline__ int64_t tile_cost(const Tokens& a, const Seq& s, int t) {
+  const int64_t tok0 = int64_t(t) * a.per_tile, low = a.window ? s.len + 1 - a.window + tok0 : 0;
+  return s.len + kTileCost + (t + 1 < s.tiles ? tok0 + a.per_tile : s.n) - (low > 0 ? low : 0);
+}
+// n / d for quotients below 2^50.  (A division of 64-bit integers is some 200 instructions,
+// which every workgroup would have to fetch first.)
+__device__ __forceinline__ int64_t divide(int64_t n, int64_t d) {
+  int64_t q = static_cast<int64_t>(double(n) / double(d));
+  if (q * d > n) --q;
+  return (q + 1) * d <= n ? q + 1 : q;
 }
 
 struct Place {
@@ -119,60 +145,66 @@ __device__ __forceinline__ int64_t readlane64(int64_t v, int lane) {
   return int64_t(uint64_t(uint32_t(__builtin_amdgcn_readlane(int(v >> 32), lane))) << 32 |
                  uint32_t(__builtin_amdgcn_readlane(int(v), lane)));
 }
-__device__ __forceinline__ int64_t total_cost(const Tokens& a) {
-  const int lane = threadIdx.x & 63;
-  int64_t all = 0;
-  for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
-    int64_t n = 0;
-    if (b0 + lane < a.c.batch) {
-      const Seq s = seq_of(a, b0 + lane);
-      n = cost_of(a, s, s.tiles) * (int64_t(a.c.kv) * a.gtiles);
-    }
-    all += readlane64(wave_scan64(n), 63);
+// The first 64 sequences as the lanes have them, and what all sequences cost.
+struct Costs {
+  Seq s;
+  int64_t head, upto, all;  // the lane's sequence: a head's tiles; the sequences' up to it
+};
+__device__ __forceinline__ Costs costs_from(const Tokens& a, int b0) {
+  const int b = b0 + (threadIdx.x & 63);
+  Costs c{{0, 0, 0, 0}, 0, 0, 0};
+  if (b < a.c.batch) {
+    c.s = seq_of(a, b);
+    c.head = cost_of(a, c.s, c.s.tiles);
   }
-  return all;
+  c.upto = wave_scan64(c.head * (int64_t(a.c.kv) * a.gtiles));
+  c.all = readlane64(c.upto, 63);
+  return c;
+}
+__device__ __forceinline__ Costs costs_of(const Tokens& a) {
+  Costs c = costs_from(a, 0);
+  for (int b0 = 64; b0 < a.c.batch; b0 += 64) c.all += costs_from(a, b0).all;
+  return c;
 }
 // Where unit u of all tiles' cost lies.
-__device__ __forceinline__ Place find_place(const Tokens& a, int64_t u) {
+__device__ __forceinline__ Place find_place(const Tokens& a, const Costs& first, int64_t u) {
   const int lane = threadIdx.x & 63;
   const int64_t heads = int64_t(a.c.kv) * a.gtiles;
   int64_t before = 0;
   for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
-    Seq s{0, 0, 0, 0};
-    int64_t one = 0;
-    if (b0 + lane < a.c.batch) {
-      s = seq_of(a, b0 + lane);
-      one = cost_of(a, s, s.tiles);
+    const Costs c = b0 == 0 ? first : costs_from(a, b0);
+    const uint64_t past = __ballot(before + c.upto > u);
+    if (!past) {
+      before += readlane64(c.upto, 63);
+      continue;
     }
-    const int64_t n = one * heads, upto = wave_scan64(n);
-    const uint64_t past = __ballot(before + upto > u);
-    if (past) {
-      const int at = __builtin_ctzll(past);
-      Place p;
-      p.b = b0 + at;
-      p.s = Seq{__builtin_amdgcn_readlane(s.t0, at), __builtin_amdgcn_readlane(s.n, at),
-                __builtin_amdgcn_readlane(s.len, at), __builtin_amdgcn_readlane(s.tiles, at)};
-      const int64_t head_cost = readlane64(one, at);
-      int64_t in = u - before - readlane64(upto - n, at);
-      const int64_t head = in / head_cost;
-      p.head = static_cast<int>(head < heads ? head : heads - 1);
-      in -= p.head * head_cost;
-      int lo = 0, hi = p.s.tiles;  // cost_of(lo) <= in < cost_of(hi)
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (cost_of(a, p.s, mid) <= in) lo = mid;
-        else hi = mid;
-      }
-      p.t = lo;
-      p.at = in - cost_of(a, p.s, lo);
-      return p;
+    const int at = __builtin_ctzll(past);
+    Place p;
+    p.b = b0 + at;
+    p.s = Seq{__builtin_amdgcn_readlane(c.s.t0, at), __builtin_amdgcn_readlane(c.s.n, at),
+              __builtin_amdgcn_readlane(c.s.len, at), __builtin_amdgcn_readlane(c.s.tiles, at)};
+    const int64_t head_cost = readlane64(c.head, at);
+    int64_t in = u - before - (readlane64(c.upto, at) - head_cost * heads);
+    const int64_t head = divide(in, head_cost);
+    p.head = static_cast<int>(head);
+    in -= head * head_cost;
+    int lo = 0, n = p.s.tiles;  // the last tile that begins at or before `in`, by 64 probes a step
+    for (;;) {
+      const int step = (n + 63) / 64, probe = lane * step;
+      const uint64_t not_past = __ballot(probe < n && cost_of(a, p.s, lo + (probe < n ? probe : 0)) <= in);
+      const int k = __builtin_popcountll(not_past) - 1;  // (at least one: a tile begins at 0)
+      lo += (k > 0 ? k : 0) * step;
+      n = step < n - (k > 0 ? k : 0) * step ? step : n - (k > 0 ? k : 0) * step;
+      if (step == 1) break;
     }
-    before += readlane64(upto, 63);
+    p.t = lo;
+    p.at = in - cost_of(a, p.s, lo);
+    return p;
   }
   return Place{-1, 0, 0, 0, {0, 0, 0, 0}};
 }
 __device__ __forceinline__ int64_t run_of(const Tokens& a, int64_t all) {
-  const int64_t run = (all + a.groups - 1) / a.groups;
+  const int64_t run = divide(all + a.groups - 1, a.groups);
   return run < kMinRun ? kMinRun : run;
 }
 
@@ -188,9 +220,13 @@ __device__ __forceinline__ Span span_of(const Tokens& a, const Seq& s, int t) {
   low = low < 0 ? 0 : low < end ? low : end;
   return Span{static_cast<int>(low / kRows), static_cast<int>((end + kRows - 1) / kRows), static_cast<int>(end)};
 }
-// The block of a tile's rows that unit `at` of its cost stands for.
-__device__ __forceinline__ int block_at(const Span& sp, int64_t at) {
-  const int64_t k = at > kTileCost ? sp.k0 + (at - kTileCost) / kRows : sp.k0;
+// A run's end inside a tile, at unit `at` of its cost: the block of its rows that it stands
+// for.  Near the tile's begin or end it is that (k0 or k1), so that no workgroup takes up a
+// tile for a few rows of it.
+__device__ __forceinline__ int block_at(const Span& sp, int64_t at, int64_t cost) {
+  if (at < kTileCost) return sp.k0;
+  if (cost - at < kTileCost) return sp.k1;
+  const int64_t k = sp.k0 + (at - kTileCost / 2) / kRows;
   return k < sp.k1 ? static_cast<int>(k) : sp.k1;
 }
 
@@ -201,6 +237,10 @@ __device__ __forceinline__ v16f mfma(const u32x4& a, const u32x4& b, const v16f&
 }
 __device__ __forceinline__ uint32_t pair_f16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, v2h{static_cast<_Float16>(lo), static_cast<_Float16>(hi)});
+}
+__device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
+  typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, v2bf{static_cast<__bf16>(lo), static_cast<__bf16>(hi)});
 }
 // Two values as NT terms each: x = t[0] + t[1] up to the last one's rounding.
 template <int NT>
@@ -235,9 +275,12 @@ __device__ __forceinline__ uint32_t max_of_halves(uint32_t v) {
   const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
   return a[0] > a[1] ? a[0] : a[1];
 }
-// The largest of a value over the wave (steps inside 16 lanes, then across them).
-__device__ __forceinline__ int wave_max(int v) {
-  auto with = [&](int u) { v = v > u ? v : u; };
+// The largest of two 16-bit values over the wave (steps inside 16 lanes, then across them).
+__device__ __forceinline__ uint32_t wave_max_pairs(uint32_t v) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  auto with = [&](uint32_t u) {
+    v = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, v), __builtin_bit_cast(u16x2, u)));
+  };
   with(__builtin_amdgcn_update_dpp(v, v, 0x111, 0xF, 0xF, false));
   with(__builtin_amdgcn_update_dpp(v, v, 0x112, 0xF, 0xF, false));
   with(__builtin_amdgcn_update_dpp(v, v, 0x114, 0xF, 0xF, false));
@@ -257,13 +300,14 @@ struct Lds {
   static constexpr int KW = DP * 2 + 16, K = kRows * KW, V = DP * kRows * 2;
   alignas(16) char k[2][K];
   alignas(16) char v[2][V];
-  int64_t at[3][kRows];     // where a row begins in its pool (left out: a place that can be read)
-  float kx[3][kRows], vx[3][kRows];  // what its codes are multiplied by
-  // of a block: its rows that there are (64 bits); kref | vref << 8 | part << 16, the biased
-  // exponents that the products with kx and vx are over, and whether not every row of the
-  // tile attends to all of it
-  u32x4 about[3];
-  int nan[3];               // and some code of V is NaN:
+  // of eight blocks:
+  int64_t at[8][kRows];     // where a row begins in its pool (of no page: a place that can be read)
+  float kx[8][kRows], vx[8][kRows];  // what its codes are multiplied by
+  // which rows there are (64 bits); kref | vref << 8 | part << 16, the biased exponents that
+  // the products with kx and vx are over, and whether not every row of the tile attends to all
+  u32x4 about[8];
+  int vmax[8];              // the largest biased exponent of V's scales
+  int nan[16];               // and some code of V is NaN:
   alignas(16) uint8_t odd[2][DP][16];  // of a value and four rows, a bit each
 };
 
@@ -272,64 +316,74 @@ __host__ __device__ constexpr int waves_for(int dp, int terms) {
   return dp == 256 ? 1 : dp == 128 ? 2 : terms == 1 ? 3 : 2;
 }
 
-// This lane's row of q in terms, over the power of two of its largest value, which
-// goes into the factor of its scores; the sign of scale goes into q.
+// Nothing is moved over this when compiled: operands are read from LDS a group ahead of
+// their use.  (Left to itself the compiler read each right before its use, and waited for it.)
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+
+// A row of q as it lies (fp32 with two terms, else 16 bits), values 16 st + 8 g ...  (One
+// address and fixed steps: with a condition and an address for each, the eight reads waited
+// for each other's, 8 us.)
 template <int DP, int NT>
-__device__ __forceinline__ void load_q(const Tokens& a, int64_t at, bool mine, u32x4 (&qf)[NT][DP / 16], float& factor) {
-  constexpr int KS = DP / 16;
+__device__ __forceinline__ void load_q(const Tokens& a, int64_t at, u32x4 (&raw)[DP / 16][NT]) {
   const int g = (threadIdx.x & 63) >> 5;
-  float x[KS][8];
+  const SHERRY_GLOBAL u32x4* p =
+      reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(static_cast<const char*>(a.q)) + (at + 8 * g) * (2 * NT));
+#pragma unroll
+  for (int st = 0; st < DP / 16; ++st)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      raw[st][j] = u32x4{0, 0, 0, 0};
+      if (16 * st < a.c.dim) raw[st][j] = p[2 * NT * st + j];
+    }
+}
+// The same in terms, over the power of two of its largest value; returns the factor of its
+// scores in units of ln 2 (the sign of scale goes into q).
+template <int DP, int NT>
+__device__ __forceinline__ float split_q(const Tokens& a, const u32x4 (&raw)[DP / 16][NT], u32x4 (&qf)[NT][DP / 16]) {
+  constexpr int KS = DP / 16;
+  const bool bf16 = a.type == SHERRY_BF16;
+  auto pair = [&](int st, int i, float& lo, float& hi) {  // values 2 i, 2 i + 1 of a step
+    if constexpr (NT == 2) {
+      lo = __uint_as_float(raw[st][i >> 1][2 * (i & 1)]);
+      hi = __uint_as_float(raw[st][i >> 1][2 * (i & 1) + 1]);
+    } else {
+      const uint32_t x = raw[st][0][i];
+      const v2h h = __builtin_bit_cast(v2h, x);
+      lo = bf16 ? __uint_as_float(x << 16) : static_cast<float>(h[0]);
+      hi = bf16 ? __uint_as_float(x & 0xFFFF0000u) : static_cast<float>(h[1]);
+    }
+  };
   uint32_t most = 0;
-#pragma unroll
-  for (int st = 0; st < KS; ++st) {
-    const int d = 16 * st + 8 * g;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[st][i] = 0.0f;
-    if (mine && d < a.c.dim) {
-      if (a.type == SHERRY_F32) {
-        const SHERRY_GLOBAL v4f* p =
-            reinterpret_cast<const SHERRY_GLOBAL v4f*>(as_global(static_cast<const float*>(a.q)) + at + d);
-        const v4f lo = p[0], hi = p[1];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[st][i] = lo[i];
-          x[st][4 + i] = hi[i];
-        }
-      } else {
-        const u32x4 h =
-            *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(static_cast<const uint16_t*>(a.q)) + at + d);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint16_t v = static_cast<uint16_t>(h[i >> 1] >> (16 * (i & 1)));
-          x[st][i] = a.type == SHERRY_BF16 ? from_bf16(v) : from_f16(v);
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t bits = __float_as_uint(x[st][i]) & 0x7FFFFFFFu;
-      most = bits > most ? bits : most;
-    }
-  }
-  most = max_of_halves(most);
-  constexpr uint32_t kTiny = 0x00400000u;  // 2^-127
-  const uint32_t e = most >> 23 < 254 ? most >> 23 : 254;
-  const float down = __uint_as_float(e < 254 ? (254 - e) << 23 : kTiny) * (a.scale < 0 ? -1.0f : a.scale > 0 ? 1.0f : 0.0f);
-  factor *= __uint_as_float(e > 0 ? e << 23 : kTiny);
 #pragma unroll
   for (int st = 0; st < KS; ++st)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      float lo, hi;
+      pair(st, i, lo, hi);
+      const uint32_t l = __float_as_uint(lo) & 0x7FFFFFFFu, h = __float_as_uint(hi) & 0x7FFFFFFFu;
+      most = l > most ? l : most;
+      most = h > most ? h : most;
+    }
+  most = max_of_halves(most);
+  constexpr uint32_t kTiny = 0x00400000u;  // 2^-127
+  const uint32_t e = most >> 23 < 254 ? most >> 23 : 254;
+  const float down = __uint_as_float(e < 254 ? (254 - e) << 23 : kTiny) * (a.scale < 0 ? -1.0f : a.scale > 0 ? 1.0f : 0.0f);
+#pragma unroll
+  for (int st = 0; st < KS; ++st) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float lo, hi;
+      pair(st, i, lo, hi);
       uint32_t t[NT];
-      split<NT>(x[st][2 * i] * down, x[st][2 * i + 1] * down, t);
+      split<NT>(lo * down, hi * down, t);
 #pragma unroll
       for (int j = 0; j < NT; ++j) qf[j][st][i] = t[j];
     }
+    fence();
+  }
+  return fabsf(a.scale) * kLog2e * __uint_as_float(e > 0 ? e << 23 : kTiny);
 }
 
-// Nothing is moved over this when compiled: operands are read from LDS a group ahead of
-// their use.  (Left to itself the compiler read each right before its use, and waited for it.)
-__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 // N times an MFMA and VALU other instructions.
 template <int N, int VALU>
 __device__ __forceinline__ void take_turns() {
@@ -357,11 +411,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // consecutive runs on one XCD (workgroups go to them in turn)
   const int w = blockIdx.x % kXcds * (a.groups / kXcds) + blockIdx.x / kXcds;
-  const int64_t all = total_cost(a), run = run_of(a, all);
+  const Costs costs = costs_of(a);
+  const int64_t run = run_of(a, costs.all);
   int64_t u = int64_t(w) * run;
-  const int64_t u_end = u + run < all ? u + run : all;
+  const int64_t u_end = u + run < costs.all ? u + run : costs.all;
+  if (tid == 0) as_global_mut(a.split)[w] = Split{0, 0, 0, 0, 0};
   if (u >= u_end) return;
-  Place pl = find_place(a, u);
+  Place pl = find_place(a, costs, u);
 
   // this thread's places: of K a piece of 16 codes, of V some codes of four rows.
   // (Values past head_dim are those at 0: q has zeros there, and outputs are not written.)
@@ -375,59 +431,64 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 
   for (;;) {
     const Seq& s = pl.s;
-    const int64_t cost = cost_of(a, s, pl.t + 1) - cost_of(a, s, pl.t);
+    const int64_t cost = tile_cost(a, s, pl.t);
     const int64_t upto = cost - pl.at < u_end - u ? cost : pl.at + (u_end - u);
     if (upto <= pl.at) return;  // (first is not ascending, and the costs past 63 bits)
     const Span sp = span_of(a, s, pl.t);
     const int b = __builtin_amdgcn_readfirstlane(pl.b);
-    const bool whole = pl.at == 0 && upto == cost;
-    const int kb0 = __builtin_amdgcn_readfirstlane(pl.at == 0 ? sp.k0 : block_at(sp, pl.at));
-    const int kb1 = __builtin_amdgcn_readfirstlane(upto == cost ? sp.k1 : block_at(sp, upto));
+    const int kb0 = __builtin_amdgcn_readfirstlane(block_at(sp, pl.at, cost));
+    const int kb1 = __builtin_amdgcn_readfirstlane(block_at(sp, upto, cost));
+    const bool begins = kb0 == sp.k0, whole = begins && kb1 == sp.k1;
     const int end = __builtin_amdgcn_readfirstlane(sp.end);
-    const int kvh = __builtin_amdgcn_readfirstlane(pl.head / a.gtiles);
+    const int kvh = __builtin_amdgcn_readfirstlane(a.gtiles == 1 ? pl.head : pl.head / a.gtiles);
     const int head0 = kvh * a.group + (pl.head - kvh * a.gtiles) * a.hp;
     const int heads = (kvh + 1) * a.group - head0 < a.hp ? (kvh + 1) * a.group - head0 : a.hp;
-    // this lane's row of q
-    const int r = wave * 32 + n, tok = r / a.hp, hd = r - tok * a.hp;
-    const int64_t in_seq = int64_t(pl.t) * a.per_tile + tok;
-    const bool mine = tok < a.per_tile && in_seq < s.n && hd < heads;
-    const int token = s.t0 + static_cast<int>(mine ? in_seq : 0);
-    const int64_t own = s.len + in_seq + 1;  // rows up to its own
+    // a lane's row of q (where the tile has none for it: the first one, of which nothing comes)
+    struct Row {
+      int r, tok, token, head;
+      bool mine;
+    };
+    auto row_of = [&](int lane_row) SHERRY_INLINE {
+      const int r = wave * 32 + lane_row, tok = a.by_hp.div(r), hd = r - tok * a.hp;
+      const int64_t in_seq = int64_t(pl.t) * a.per_tile + tok;
+      const bool mine = tok < a.per_tile && in_seq < s.n && hd < heads;
+      return Row{r, static_cast<int>(mine ? in_seq : 0), s.t0 + static_cast<int>(mine ? in_seq : 0),
+                 head0 + (mine ? hd : 0), mine};
+    };
+    const Row row = row_of(n);
+    const bool mine = row.mine;
+    const int64_t own = int64_t(s.len) + row.tok + 1;  // rows up to its own
     const int lim = mine ? static_cast<int>(own < a.c.rows ? own : a.c.rows) : 0;
     const int64_t low64 = a.window ? own - a.window : 0;
     const int low = mine && low64 > 0 ? static_cast<int>(low64 < a.c.rows ? low64 : a.c.rows) : 0;
-    // some of the wave's rows attend to some of [some_low, some_lim); the first token of
-    // the tile to rows before all_lim, the last one to those from all_low
-    const int some_lim = wave_max(lim), some_low = -wave_max(mine ? -low : -0x7FFFFFFF);
+    const bool active = __any(mine);  // (the tile may have fewer rows than the workgroup)
+    // the first token of the tile attends to rows before all_lim, the last to those from all_low
     const int64_t own0 = s.len + int64_t(pl.t) * a.per_tile + 1;
     const int all_lim = __builtin_amdgcn_readfirstlane(static_cast<int>(own0 < end ? own0 : end));
     const int64_t low1 = a.window ? own0 + a.per_tile - a.window : 0;
     const int all_low = __builtin_amdgcn_readfirstlane(static_cast<int>(low1 < 0 ? 0 : low1 < end ? low1 : end));
 
-    // q, over the power of two of its largest value
-    u32x4 qf[NT][KS];
-    float factor = fabsf(a.scale) * kLog2e;
-    load_q<DP, NT>(a, int64_t(token) * a.q_stride + int64_t(head0 + (mine ? hd : 0)) * a.c.dim, mine, qf, factor);
+    u32x4 qraw[KS][NT], qf[NT][KS];
+    float factor = 0.0f;
 
     v16f o[DB];
-#pragma unroll
-    for (int i = 0; i < DB; ++i) o[i] = v16f{};
     float m = kMinusInf, base = 0.0f, l = 0.0f;
     int vrun = 1;  // o is over this power of two
 
-    // ---- what the first wave finds out about a block of rows ----
-    int next_page = -1, next_mask = 1, seen_vref = 1;
+    // ---- what the waves find out about blocks of rows, each about every fourth block:
+    // its pages, their scales, the largest of these, and what follows for its rows ----
+    int next_page = -1, next_mask = 1, seen_vref = 1, next_kref = 1;
     int64_t next_at = 0;
     float next_ks = 0, next_vs = 0;
     bool next_ok = false;
-    auto look_page = [&](int kb) {  // reads its pages
-      const int row = kb * kRows + lane;
-      const bool in = kb < kb1 && row < end;
+    auto look_page = [&](int kb) SHERRY_INLINE {
+      const int row = (kb + wave) * kRows + lane;
+      const bool in = kb + wave < kb1 && row < end;
       next_page = in ? as_global(a.c.table)[int64_t(b) * a.c.width + a.c.by_page.div(row)] : -1;
       next_mask = in && a.mask ? as_global(a.mask)[int64_t(b) * a.mask_stride + row] : 1;
     };
-    auto look_scale = [&](int kb) {  // and then their scales (rows of no page: any place that can be read)
-      const int row = kb * kRows + lane;
+    auto look_scale = [&](int kb) SHERRY_INLINE {  // (rows of no page: any place that can be read)
+      const int row = (kb + wave) * kRows + lane;
       const bool there = next_page >= 0 && next_page < a.c.pages;
       next_ok = there && next_mask != 0;
       const int page = there ? next_page : 0;
@@ -436,28 +497,38 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       next_ks = as_global(a.c.ks)[a.c.scale_at(page, kvh)];
       next_vs = as_global(a.c.vs)[a.c.scale_at(page, kvh)];
     };
-    auto publish = [&](int kb, int slot) {
-      // (a row that is masked shares its factor with others of its page)
-      const int ke = exponent(next_ks), ve = exponent(next_vs);
-      const int kref = wave_max(next_ok ? ke : 1), vmax = wave_max(next_ok ? ve : 1);
-      seen_vref = vmax > seen_vref ? vmax : seen_vref;
+    auto look_refs = [&](int kb) SHERRY_INLINE {
+      // (largest of both at once; a row that is masked shares its factor with others of its page)
+      const uint32_t both = next_ok ? exponent(next_ks) | exponent(next_vs) << 16 : 0x10001u;
+      const uint32_t top = wave_max_pairs(both);
+      next_kref = top & 0xFFFF;
+      if (lane == 0) lds.vmax[(kb - kb0 + wave) & 7] = top >> 16;
+    };
+    auto publish = [&](int kb) SHERRY_INLINE {
+      const int slot = (kb - kb0 + wave) & 7;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        const int v = __builtin_amdgcn_readfirstlane(lds.vmax[(kb - kb0 + i) & 7]);
+        seen_vref = v > seen_vref ? v : seen_vref;
+      }
       auto over = [](int ref, int e) { return power(ref - e < 0 ? 127 : ref - e < 126 ? 127 - (ref - e) : 1); };
       lds.at[slot][lane] = next_at;
-      lds.kx[slot][lane] = over(kref, ke);
-      lds.vx[slot][lane] = over(seen_vref, ve);
+      lds.kx[slot][lane] = over(next_kref, exponent(next_ks));
+      lds.vx[slot][lane] = over(seen_vref, exponent(next_vs));
       const uint64_t valid = __ballot(next_ok);
-      const int row0 = kb * kRows;
+      const int row0 = (kb + wave) * kRows;
       if (lane == 0) {
         const bool part = ~valid != 0 || row0 + kRows > all_lim || row0 < all_low;
         lds.about[slot] = u32x4{static_cast<uint32_t>(valid), static_cast<uint32_t>(valid >> 32),
-                                static_cast<uint32_t>(kref | seen_vref << 8 | int(part) << 16), 0};
-        lds.nan[slot] = 0;
+                                static_cast<uint32_t>(next_kref | seen_vref << 8 | int(part) << 16), 0};
+        lds.nan[(kb - kb0 + wave) & 15] = 0;
       }
     };
+
     // ---- a block's rows, from the pools to LDS ----
     u32x4 kr[KP];
     uint32_t vr[4][VW];
-    auto load = [&](int slot) {
+    auto load = [&](int slot) SHERRY_INLINE {
 #pragma unroll
       for (int i = 0; i < KP; ++i)
         kr[i] = *reinterpret_cast<const SHERRY_GLOBAL u32x4*>(as_global(a.c.k) + lds.at[slot][k_row + KR * i] + k_d);
@@ -477,7 +548,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         }
       }
     };
-    auto fill = [&](int buf, int slot) {
+    auto fill = [&](int buf, int rel) SHERRY_INLINE {
+      const int slot = rel & 7;
       if (__builtin_amdgcn_readfirstlane(lds.about[slot][2]) >> 16) {
         // NaN must not reach rows of q that do not attend to it: it is 0 here, and noted
         uint32_t any = 0;
@@ -494,7 +566,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 #pragma unroll
           for (int e = 0; e < 4; ++e) lds.odd[buf][VB * col + 4 * i + e][quad] = static_cast<uint8_t>(bits >> (8 * e));
         }
-        if (any) lds.nan[slot] = 1;
+        if (any) lds.nan[rel & 15] = 1;
       }
 #pragma unroll
       for (int i = 0; i < KP; ++i) {
@@ -539,7 +611,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
     };
 
     // ---- a block's scores, probabilities and outputs ----
-    auto attend = [&](int kb, int buf, int slot) {
+    auto attend = [&](int kb, int buf) SHERRY_INLINE {
       const int row0 = kb * kRows;
       const char* kp = lds.k[buf] + k_from;
       const char* vp = lds.v[buf] + v_from;
@@ -555,7 +627,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         for (int db = 0; db < DB; ++db)
           vf[st & 1][db] = *reinterpret_cast<const u32x4*>(vp + 16 * (2 * (st ^ (db & 3)) ^ v_swap) + 32 * db * VROW);
       };
-      const u32x4 about = lds.about[slot];
+      const u32x4 about = lds.about[(kb - kb0) & 7];
       read_k(0);
       v16f sc[2] = {v16f{}, v16f{}};
 #pragma unroll
@@ -640,7 +712,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         fence();
       }
       l += sum[0] + sum[1];
-      if (part && __builtin_amdgcn_readfirstlane(lds.nan[slot])) {
+      if (part && __builtin_amdgcn_readfirstlane(lds.nan[(kb - kb0) & 15])) {
         u32x4 mine_of;  // the attended rows, four a byte
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
@@ -657,80 +729,93 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       }
     };
 
-    __syncthreads();  // (the tile before has been read from LDS)
+    // A block's rows are read two blocks before their turn, and put into LDS one before it; what
+    // the blocks are is known from two to five blocks before they are read.
+    // (first reads first: pages and q, then what the pages lead to)
     if (kb0 < kb1) {
-      if (wave == 0) {
-        look_page(kb0);
-        look_scale(kb0);
-        look_page(kb0 + 1);
-        publish(kb0, 0);
-        look_scale(kb0 + 1);
-        look_page(kb0 + 2);
-        publish(kb0 + 1, 1);
-      }
+      look_page(kb0);
+      load_q<DP, NT>(a, int64_t(row.token) * a.q_stride + int64_t(row.head) * a.c.dim, qraw);
+      look_scale(kb0);
+      __syncthreads();  // (the tile before has been read from LDS)
+      lds.at[wave][lane] = next_at;
+      look_refs(kb0);
       __syncthreads();
       load(0);
+      publish(kb0);
+      look_page(kb0 + kWaves);
+      factor = split_q<DP, NT>(a, qraw, qf);
+      look_scale(kb0 + kWaves);
+      __syncthreads();
       fill(0, 0);
+      load(1);
       __syncthreads();
     }
-    int slot = 0;
-    for (int kb = kb0; kb < kb1; ++kb) {
-      const int buf = (kb - kb0) & 1, slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
-      // what the blocks after the next one are (first: its answers come in order), and the
-      // rows of the next one
-      if (wave == 0) {
-        look_scale(kb + 2);
-        look_page(kb + 3);
-      }
-      if (kb + 1 < kb1) load(slot1);
-      if (kb * kRows < some_lim && (kb + 1) * kRows > some_low) attend(kb, buf, slot);
-      if (kb + 1 < kb1) fill(buf ^ 1, slot1);
-      if (wave == 0) publish(kb + 2, slot2);
+#pragma unroll
+    for (int i = 0; i < DB; ++i) o[i] = v16f{};
+    // (four turns written out: what one has asked memory for, a later one takes, and no
+    // answer has to be there where turns would join)
+    auto turn = [&](auto turn_c, int kb) SHERRY_INLINE {
+      constexpr int t = decltype(turn_c)::value;
+      const int rel = kb - kb0;
+      if (active) attend(kb, t & 1);
+      // (behind the last block: rows of no page, of which nothing comes)
+      fill((t & 1) ^ 1, rel + 1);
+      if constexpr (t == 0) look_refs(kb + kWaves);
+      if constexpr (t == 1) publish(kb - 1 + kWaves);
+      if constexpr (t == 2) look_page(kb - 2 + 2 * kWaves);
+      if constexpr (t == 3) look_scale(kb - 3 + 2 * kWaves);
+      load((rel + 2) & 7);
       __syncthreads();
-      slot = slot1;
+    };
+    for (int kb = kb0; kb < kb1; kb += 4) {
+      turn(std::integral_constant<int, 0>{}, kb);
+      if (kb + 1 >= kb1) break;
+      turn(std::integral_constant<int, 1>{}, kb + 1);
+      if (kb + 2 >= kb1) break;
+      turn(std::integral_constant<int, 2>{}, kb + 2);
+      if (kb + 3 >= kb1) break;
+      turn(std::integral_constant<int, 3>{}, kb + 3);
     }
 
     // ---- the way out: o over p's sum ----
     l += __shfl_xor(l, 32, 64);
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    if (mine) {
+    int again = n;  // (found anew: it would take registers all the way)
+    asm volatile("" : "+v"(again));
+    const Row out = row_of(again);
+    if (out.mine && (kb0 < kb1 || whole)) {
       const float times = power(vrun);
-      if (whole) {
-        const int64_t at = int64_t(token) * a.out_stride + int64_t(head0 + hd) * a.c.dim;
+      const int64_t part = int64_t(2 * w + begins) * a.part_rows + out.r;
+      const int64_t at = whole ? int64_t(out.token) * a.out_stride + int64_t(out.head) * a.c.dim : part * DP;
+      if (!whole && g == 0) as_global_mut(a.stat)[part] = make_float2(base, l);
+      SHERRY_GLOBAL char* to = as_global_mut(static_cast<char*>(whole ? a.out : a.sums)) +
+                               (at + 4 * g) * (whole && NT == 1 ? 2 : 4);
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
+      for (int db = 0; db < DB; ++db)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int d = 32 * db + 8 * j + 4 * g;
-            if (d >= a.c.dim) continue;
-            v4f x;
+        for (int j = 0; j < 4; ++j) {
+          const int d = 32 * db + 8 * j;  // (and 4 g)
+          if (16 * (d / 16) >= a.c.dim) continue;
+          v4f x;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = o[db][4 * j + i] * inv * times;
-            if (a.type == SHERRY_F32) {
-              *reinterpret_cast<SHERRY_GLOBAL v4f*>(as_global_mut(static_cast<float*>(a.out)) + at + d) = x;
-            } else {
-              uint16_t h[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) h[i] = a.type == SHERRY_BF16 ? to_bf16(x[i]) : to_f16(x[i]);
-              *reinterpret_cast<SHERRY_GLOBAL u32x2*>(as_global_mut(static_cast<uint16_t*>(a.out)) + at + d) =
-                  u32x2{uint32_t(h[0]) | uint32_t(h[1]) << 16, uint32_t(h[2]) | uint32_t(h[3]) << 16};
-            }
-          }
-      } else {
-        const int64_t at = (int64_t(2 * w + (pl.at == 0)) * a.part_rows + r);
-        if (g == 0) as_global_mut(a.stat)[at] = make_float2(base, l);
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            v4f x;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = o[db][4 * j + i] * inv * times;
-            *reinterpret_cast<SHERRY_GLOBAL v4f*>(as_global_mut(a.sums) + at * DP + 32 * db + 8 * j + 4 * g) = x;
-          }
-      }
+          for (int i = 0; i < 4; ++i) x[i] = o[db][4 * j + i] * inv * times;
+          if (NT == 2 || !whole)
+            *reinterpret_cast<SHERRY_GLOBAL v4f*>(to + 4 * d) = x;
+          else
+            *reinterpret_cast<SHERRY_GLOBAL u32x2*>(to + 2 * d) =
+                a.type == SHERRY_BF16 ? u32x2{pair_bf16(x[0], x[1]), pair_bf16(x[2], x[3])}
+                                      : u32x2{pair_f16(x[0], x[1]), pair_f16(x[2], x[3])};
+        }
     }
 
+    if (tid == 0 && begins && kb0 < kb1 && !whole) {  // (another workgroup ends it)
+      const int tok0 = pl.t * a.per_tile;
+      const int64_t from = u - pl.at;
+      int64_t last = divide(from + cost - 1, run);
+      if (block_at(sp, last * run - from, cost) == sp.k1) --last;
+      as_global_mut(a.split)[w] = Split{s.t0 + tok0, s.n - tok0 < a.per_tile ? s.n - tok0 : a.per_tile, head0, heads,
+                                        static_cast<int>(last)};
+    }
     u += upto - pl.at;
     if (u >= u_end) return;
     pl.at = 0;
@@ -740,7 +825,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       ++pl.head;
       pl.t = 0;
     } else {
-      pl = find_place(a, u);
+      pl = find_place(a, costs, u);
       if (pl.b < 0) return;
     }
   }
@@ -748,51 +833,51 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 
 // Workgroup w joins the tile that begins in run w and goes on behind it; blockIdx.y: a
 // share of its rows.
+constexpr int kJoinThreads = 1024;
 template <int DP>
-__global__ __launch_bounds__(256) void tokens_join_kernel(Tokens a) {
-  const int64_t all = total_cost(a), run = run_of(a, all);
+__global__ __launch_bounds__(kJoinThreads) void tokens_join_kernel(Tokens a) {
   const int w = blockIdx.x;
-  const int64_t e = (int64_t(w) + 1) * run;
-  if (e >= all) return;
-  const Place pl = find_place(a, e);
-  if (pl.b < 0 || pl.at == 0 || e - pl.at < int64_t(w) * run) return;
-  const int64_t cost = cost_of(a, pl.s, pl.t + 1) - cost_of(a, pl.s, pl.t);
-  const int last = static_cast<int>((e - pl.at + cost - 1) / run);  // the workgroup that ends it
-  const int kvh = pl.head / a.gtiles;
-  const int head0 = kvh * a.group + (pl.head - kvh * a.gtiles) * a.hp;
-  const int heads = (kvh + 1) * a.group - head0 < a.hp ? (kvh + 1) * a.group - head0 : a.hp;
-  constexpr int LANES = DP / 4, STEP = 256 / LANES;  // rows at a time
-  for (int r = blockIdx.y * STEP + threadIdx.x / LANES; r < a.part_rows; r += gridDim.y * STEP) {
-    const int tok = r / a.hp, hd = r - tok * a.hp, d = 4 * (threadIdx.x % LANES);
-    const int64_t in_seq = int64_t(pl.t) * a.per_tile + tok;
-    if (tok >= a.per_tile || in_seq >= pl.s.n || hd >= heads || d >= a.c.dim) continue;
-    float base = kMinusInf, l = 0.0f;
-    v4f sum = {0, 0, 0, 0};
-    for (int i = w; i <= last; ++i) {
+  const SHERRY_CONST Split& sp = as_const(a.split)[w];
+  const int tokens = sp.tokens, heads = sp.heads, last = sp.last;
+  constexpr int LANES = DP / 4, AT = 4;  // parts in flight
+  const int d = 4 * (threadIdx.x % LANES), r = (blockIdx.y * kJoinThreads + threadIdx.x) / LANES;
+  const int tok = a.by_hp.div(r), hd = r - tok * a.hp;
+  if (tok >= tokens || hd >= heads || d >= a.c.dim) return;
+  float base = kMinusInf, l = 0.0f;
+  v4f sum = {0, 0, 0, 0};
+  for (int i0 = w; i0 <= last; i0 += AT) {
+    float2 st[AT];
+    v4f x[AT];
+#pragma unroll
+    for (int j = 0; j < AT; ++j) {
+      const int i = i0 + j <= last ? i0 + j : i0;
       const int64_t at = int64_t(2 * i + (i == w)) * a.part_rows + r;
-      const float2 st = as_global(a.stat)[at];
-      if (st.y == 0.0f) continue;  // (nothing attended to)
-      const v4f x = *reinterpret_cast<const SHERRY_GLOBAL v4f*>(as_global(a.sums) + at * DP + d);
-      const float to = fmaxf(base, st.x);
+      st[j] = as_global(a.stat)[at];
+      x[j] = *reinterpret_cast<const SHERRY_GLOBAL v4f*>(as_global(a.sums) + at * DP + d);
+      if (i0 + j > last) st[j].y = 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < AT; ++j) {
+      if (st[j].y == 0.0f) continue;  // (nothing attended to)
+      const float to = fmaxf(base, st[j].x);
       const float f0 = base == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(base - to);
-      const float f1 = st.y * __builtin_amdgcn_exp2f(st.x - to);
+      const float f1 = st[j].y * __builtin_amdgcn_exp2f(st[j].x - to);
       l = l * f0 + f1;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum[j] = sum[j] * f0 + x[j] * f1;
+      for (int e = 0; e < 4; ++e) sum[e] = sum[e] * f0 + x[j][e] * f1;
       base = to;
     }
-    const int64_t at = int64_t(pl.s.t0 + in_seq) * a.out_stride + int64_t(head0 + hd) * a.c.dim + d;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) store_from_f32(a.out, at + j, a.type, l == 0.0f ? 0.0f : sum[j] / l);
   }
+  const int64_t at = int64_t(sp.first + tok) * a.out_stride + int64_t(sp.head0 + hd) * a.c.dim + d;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) store_from_f32(a.out, at + e, a.type, l == 0.0f ? 0.0f : sum[e] / l);
 }
 
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
-constexpr int kJoinShares = 4;
 
 struct Shape {
   int group, gtiles, hp, per_tile, groups, part_rows;
-  size_t stat_bytes, sum_bytes;
+  size_t split_bytes, stat_bytes, sum_bytes;
 };
 Shape shape_of(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d) {
   Shape s{};
@@ -811,6 +896,7 @@ Shape shape_of(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d) {
   s.groups = static_cast<int>(most < fit / kXcds ? static_cast<int64_t>(most) * kXcds : fit);
   const int64_t part = int64_t(d.tokens) * s.hp;
   s.part_rows = static_cast<int>(part < kQRows ? part : kQRows);
+  s.split_bytes = (s.groups * sizeof(Split) + 255) / 256 * 256;
   s.stat_bytes = (size_t(2) * s.groups * s.part_rows * 8 + 255) / 256 * 256;
   s.sum_bytes = size_t(2) * s.groups * s.part_rows * dp * 4;
   return s;
@@ -825,24 +911,26 @@ template <int DP>
 int launch_dim(const Tokens& a, hipStream_t s) {
   const int rc = a.c.page_size % 4 == 0 ? launch_terms<DP, true>(a, s) : launch_terms<DP, false>(a, s);
   if (rc != SHERRY_OK) return rc;
-  return launch(tokens_join_kernel<DP>, dim3(static_cast<unsigned>(a.groups), kJoinShares), dim3(256), 0, s, a);
+  const dim3 join(static_cast<unsigned>(a.groups), static_cast<unsigned>(ceil_div(int64_t(a.part_rows) * (DP / 4), kJoinThreads)));
+  return launch(tokens_join_kernel<DP>, join, dim3(kJoinThreads), 0, s, a);
 }
 
 }  // namespace
 
 size_t attend_tokens_workspace(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d) {
   const Shape s = shape_of(c, d);
-  return s.stat_bytes + s.sum_bytes;
+  return s.split_bytes + s.stat_bytes + s.sum_bytes;
 }
 
 int launch_attend_tokens(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d, hipStream_t s) {
   const Shape sh = shape_of(c, d);
   char* ws = static_cast<char*>(d.workspace);
   const int64_t row = int64_t(d.heads) * c.head_dim;
-  const Tokens a{cache_of(c), d.q, d.out, d.first, d.length, d.mask, reinterpret_cast<float2*>(ws),
-                 reinterpret_cast<float*>(ws + sh.stat_bytes), d.q_stride ? d.q_stride : row,
+  const Tokens a{cache_of(c), d.q, d.out, d.first, d.length, d.mask, reinterpret_cast<float2*>(ws + sh.split_bytes),
+                 reinterpret_cast<float*>(ws + sh.split_bytes + sh.stat_bytes), reinterpret_cast<Split*>(ws), d.q_stride ? d.q_stride : row,
                  d.out_stride ? d.out_stride : row, d.mask_stride, d.tokens, d.heads, sh.group, sh.gtiles,
-                 sh.per_tile, sh.hp, d.type, d.window, sh.groups, sh.part_rows, d.scale};
+                 sh.per_tile, sh.hp, d.type, d.window, sh.groups, sh.part_rows, d.scale,
+                 FastDiv::of(static_cast<uint32_t>(sh.hp)), FastDiv::of(static_cast<uint32_t>(sh.per_tile))};
   switch (padded_dim(c.head_dim)) {
     case 64: return launch_dim<64>(a, s);
     case 128: return launch_dim<128>(a, s);
