@@ -26,6 +26,7 @@ namespace sherry {
 namespace {
 
 constexpr int kKeep = 8;       // pieces of four values a lane that stay in registers
+constexpr int kQGroups = 1024, kMostQ = 16;  // workgroups for q before they take several tokens; the most
 constexpr int kLeast = -100;   // the smallest exponent that extend gives
 
 struct Extend {
@@ -40,7 +41,8 @@ struct Extend {
   Rotary rope;
   int64_t q_stride, k_stride, v_stride, q_out_stride;
   int tokens, heads, units;   // units: most pages that the tokens reach
-  FastDiv by_parts, by_qparts;  // workgroups per page, and per token for q
+  int per_q;                  // tokens of a workgroup that turns q
+  FastDiv by_parts, by_qparts;  // workgroups per page, and per per_q tokens for q
 };
 
 // A sequence's tokens [t0, t0 + n) and its rows before them.
@@ -217,23 +219,30 @@ __device__ __forceinline__ void store_pages(const Extend& a, int blk) {
   if (mine == 0 && lane == 0) as_global_mut(scale)[0] = power(now);
 }
 
+// per_q tokens one after the other, 256 / LPR of their heads.
 template <int LPR, int TYPE, bool VEC>
 __device__ __forceinline__ void turn_q(const Extend& a, int blk) {
-  const int t = a.by_qparts.div(blk), part = blk - t * a.by_qparts.d;
-  const int b = __builtin_amdgcn_readfirstlane(find_sequence(a, t));
-  if (b < 0) return;
-  const Tokens s = tokens_of(a, b);
-  const int row = s.len + (t - s.t0);
-  if (t < s.t0 || t - s.t0 >= s.n) return;
-  const int page = as_const(a.c.table)[int64_t(b) * a.c.width + a.c.by_page.div(row)];
-  const int pos = a.pos ? as_const(a.pos)[t] : row;
+  const int group = a.by_qparts.div(blk), part = blk - group * a.by_qparts.d;
+  const int t0 = group * a.per_q, t1 = t0 + a.per_q < a.tokens ? t0 + a.per_q : a.tokens;
   const int r = part * (256 / LPR) + threadIdx.x / LPR, d = 4 * (threadIdx.x % LPR);
-  if (page < 0 || page >= a.c.pages || !a.rope.has(pos) || r >= a.heads || d >= a.c.dim) return;
-  store4<TYPE, VEC>(a.q_out, int64_t(t) * a.q_out_stride + r * a.c.dim + d,
-                    rotated<TYPE, VEC>(a.rope, a.q, int64_t(t) * a.q_stride + r * a.c.dim, d, pos));
+  const bool in = r < a.heads && d < a.c.dim;
+  int b = __builtin_amdgcn_readfirstlane(find_sequence(a, t0));
+  b = b < 0 ? 0 : b;
+  Tokens s = tokens_of(a, b);
+#pragma unroll 4
+  for (int t = t0; t < t1; ++t) {
+    while (b + 1 < a.c.batch && as_const(a.first)[b + 1] <= t) s = tokens_of(a, ++b);
+    const int row = s.len + (t - s.t0);
+    if (t < s.t0 || t - s.t0 >= s.n) continue;
+    const int page = as_const(a.c.table)[int64_t(b) * a.c.width + a.c.by_page.div(row)];
+    const int pos = a.pos ? as_const(a.pos)[t] : row;
+    if (page < 0 || page >= a.c.pages || !a.rope.has(pos) || !in) continue;
+    store4<TYPE, VEC>(a.q_out, int64_t(t) * a.q_out_stride + r * a.c.dim + d,
+                      rotated<TYPE, VEC>(a.rope, a.q, int64_t(t) * a.q_stride + r * a.c.dim, d, pos));
+  }
 }
 
-// Blocks [0, units * by_parts.d): pages; then [tokens][by_qparts.d]: q.
+// Blocks [0, units * by_parts.d): pages; then [tokens / per_q][by_qparts.d]: q.
 template <int LPR, int WPP, int TYPE, bool VEC>
 __global__ __launch_bounds__(256) void extend_kernel(Extend a) {
   const int pages = a.units * static_cast<int>(a.by_parts.d);
@@ -243,9 +252,10 @@ __global__ __launch_bounds__(256) void extend_kernel(Extend a) {
 
 struct Grid {
   int units;
-  int64_t parts, qparts;  // workgroups per page, and per token for q
+  int per_q;              // tokens of a workgroup that turns q
+  int64_t parts, qparts;  // workgroups per page, and per per_q tokens for q
   bool wide;              // four waves per page, head and K or V
-  int64_t blocks(int64_t tokens) const { return units * parts + tokens * qparts; }
+  int64_t blocks(int64_t tokens) const { return units * parts + ceil_div(tokens, per_q) * qparts; }
 };
 Grid grid_of(const sherry_cache_desc& c, const sherry_extend_desc& d) {
   Grid g{};
@@ -258,6 +268,10 @@ Grid grid_of(const sherry_cache_desc& c, const sherry_extend_desc& d) {
   g.wide = rows * lanes > 64 * kKeep;
   g.parts = g.wide ? 2 * c.kv_heads : ceil_div(2 * c.kv_heads, 4);
   g.qparts = d.q ? ceil_div(d.heads, 256 / lanes) : 0;
+  // A workgroup finds its token's place by reads that wait for each other; past what runs at
+  // once it takes several tokens, whose places follow from the first one's.
+  const int64_t per = d.tokens * g.qparts / kQGroups;
+  g.per_q = static_cast<int>(per < 1 ? 1 : per < kMostQ ? per : kMostQ);
   return g;
 }
 
@@ -292,7 +306,7 @@ int launch_extend(const sherry_cache_desc& c, const sherry_extend_desc& d, hipSt
   const Extend a{cache_of(c), d.q, d.k, d.v, d.q_out, d.first, d.length, d.pos,
                  Rotary{d.cos, d.sin, d.rope_rows, d.rot_dim, d.pairing == SHERRY_ROPE_PAIRS},
                  d.q_stride ? d.q_stride : qrow, d.k_stride ? d.k_stride : row, d.v_stride ? d.v_stride : row,
-                 d.q_out_stride ? d.q_out_stride : qrow, d.tokens, heads, g.units,
+                 d.q_out_stride ? d.q_out_stride : qrow, d.tokens, heads, g.units, g.per_q,
                  FastDiv::of(static_cast<uint32_t>(g.parts)),
                  FastDiv::of(static_cast<uint32_t>(g.qparts ? g.qparts : 1))};
   auto whole = [&](const void* p, int64_t stride) { return whole_pieces(p, stride, d.type); };

@@ -19,6 +19,7 @@ namespace {
 constexpr int kThreads = 1024, kPlanWaves = kThreads / 64;
 constexpr int kSeqs = 1024;          // sequences whose place is kept in LDS
 constexpr int kLdsWords = 10 * 1024;  // words of bits that are
+constexpr int kLdsSmall = 24 * 1024;  // bytes of bits and last places that are in LDS beside the free pages
 constexpr int kDeep = 4;             // strips of 64 entries in flight per wave
 constexpr int kChunk = 16384;        // bytes that a workgroup copies at once
 constexpr int kCopyGroups = 256 * 8;
@@ -98,6 +99,24 @@ struct Bits {
   __device__ __forceinline__ bool operator[](int page) const { return (word(page >> 5) >> (page & 31)) & 1; }
 };
 
+// The last place of a page, + 1, in LDS or in the workspace (as Bits).
+template <bool LDS>
+struct Last {
+  int32_t* p;
+  __device__ __forceinline__ void clear(int page) const {
+    if constexpr (LDS) p[page] = 0;
+    else __hip_atomic_store(p + page, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __device__ __forceinline__ void raise(int page, int v) const {
+    if constexpr (LDS) atomicMax(p + page, v);
+    else __hip_atomic_fetch_max(p + page, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __device__ __forceinline__ int operator[](int page) const {
+    if constexpr (LDS) return p[page];
+    else return __hip_atomic_load(p + page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+};
+
 // Sums of v over the threads before this one, and over all.
 struct Scan {
   int before, all;
@@ -125,33 +144,56 @@ struct Entry {
   bool mine;
 };
 
-// f(entries) for this wave's share of the table, kDeep strips of 64 entries at a time.
-template <class Info, class F>
-__device__ __forceinline__ void for_entries(const Pages& a, const Info& info, F&& f) {
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t strips = (a.entries + 63) / 64, share = (strips + kPlanWaves - 1) / kPlanWaves;
-  const uint32_t s0 = wave * share, s1 = s0 + share < strips ? s0 + share : strips;
-  for (uint32_t s = s0; s < s1; s += kDeep) {
-    Entry e[kDeep];
+// The entries that this wave has: its share of the table, kDeep strips of 64 at a time.
+// Once: they are no more than kDeep strips a wave, and stay in registers from one pass to
+// the next (a fork of 32 sequences of 96 places took 10.8 us with five passes over memory).
+template <bool ONCE, class Info>
+struct Entries {
+  const Pages& a;
+  const Info& info;
+  uint32_t s0, s1;
+  Entry kept[kDeep];
+  __device__ __forceinline__ Entries(const Pages& args, const Info& i) : a(args), info(i) {
+    const uint32_t wave = threadIdx.x >> 6, strips = (a.entries + 63) / 64;
+    const uint32_t share = (strips + kPlanWaves - 1) / kPlanWaves;
+    s0 = wave * share;
+    s1 = s0 + share < strips ? s0 + share : strips;
+  }
+  __device__ __forceinline__ void read(uint32_t s) {
 #pragma unroll
     for (int i = 0; i < kDeep; ++i) {
-      e[i] = Entry{(s + i) * 64 + lane, -1, false};
-      if (s + i >= s1 || e[i].flat >= a.entries) {
-        e[i].flat = ~0u;
+      kept[i] = Entry{(s + i) * 64 + (threadIdx.x & 63), -1, false};
+      if (s + i >= s1 || kept[i].flat >= a.entries) {
+        kept[i].flat = ~0u;
         continue;
       }
-      const int b = static_cast<int>(a.by_width.div(e[i].flat)), j = static_cast<int>(e[i].flat - uint32_t(b) * a.c.width);
+      const int b = static_cast<int>(a.by_width.div(kept[i].flat));
+      const int j = static_cast<int>(kept[i].flat - uint32_t(b) * a.c.width);
       const Seq q = info(b);
-      e[i].mine = j >= q.lo && j < q.hi;
-      if (j < q.pages) e[i].page = as_global(a.c.table)[int64_t(q.parent) * a.c.width + j];
+      kept[i].mine = j >= q.lo && j < q.hi;
+      if (j < q.pages) kept[i].page = as_global(a.c.table)[int64_t(q.parent) * a.c.width + j];
     }
 #pragma unroll
-    for (int i = 0; i < kDeep; ++i) {
-      if (static_cast<uint32_t>(e[i].page) >= static_cast<uint32_t>(a.c.pages)) e[i].page = -1;
-      f(e[i]);
+    for (int i = 0; i < kDeep; ++i)
+      if (static_cast<uint32_t>(kept[i].page) >= static_cast<uint32_t>(a.c.pages)) kept[i].page = -1;
+  }
+  template <class F>
+  __device__ __forceinline__ void each(F&& f) {
+    if constexpr (ONCE) {
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) f(kept[i]);
+    } else {
+      for (uint32_t s = s0; s < s1; s += kDeep) {
+        read(s);
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) f(kept[i]);
+      }
     }
   }
-}
+  __device__ __forceinline__ void begin() {  // (after info is there)
+    if constexpr (ONCE) read(s0);
+  }
+};
 
 struct InfoOf {
   const Pages& a;
@@ -164,19 +206,25 @@ __device__ __forceinline__ void keep_info(const Pages& a, Seq* kept) {
 
 extern __shared__ uint32_t lds_bits[];
 
-template <bool LDS>
+// ONCE: the entries stay in registers, and with LDS free pages and the places of shared ones
+// in LDS too.
+template <bool LDS, bool ONCE>
 __global__ __launch_bounds__(kThreads) void fork_plan_kernel(Pages a) {
   __shared__ Seq kept[kSeqs];
   __shared__ int sums[kPlanWaves], needs[kPlanWaves], copies[kPlanWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ int32_t free_lds[ONCE ? kThreads * kDeep : 1];
   uint32_t* base = LDS ? lds_bits : a.bits;
   // pages that the new table has, has more than once, and has where it is not written
   const Bits<LDS> used{base}, more{base + a.words}, other{base + 2 * a.words};
+  const Last<LDS && ONCE> last{LDS && ONCE ? reinterpret_cast<int32_t*>(base + 3 * a.words) : a.last};
   for (int i = threadIdx.x; i < 3 * a.words; i += kThreads) Bits<LDS>{base}.clear(i);
   keep_info(a, kept);
   const InfoOf info{a, kept};
   __syncthreads();
-  for_entries(a, info, [&](const Entry& e) {
+  Entries<ONCE, InfoOf> entries(a, info);
+  entries.begin();
+  entries.each([&](const Entry& e) {
     if (e.page < 0) return;
     if (used.set(e.page)) more.set(e.page);
     if (!e.mine) other.set(e.page);
@@ -185,15 +233,14 @@ __global__ __launch_bounds__(kThreads) void fork_plan_kernel(Pages a) {
   // where all places of a shared page are written, the last of them keeps it
   auto contended = [&](const Entry& e) { return e.page >= 0 && e.mine && more[e.page] && !other[e.page]; };
   bool any = false;
-  for_entries(a, info, [&](const Entry& e) {
+  entries.each([&](const Entry& e) {
     if (!contended(e)) return;
     any = true;
-    __hip_atomic_store(a.last + e.page, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    last.clear(e.page);
   });
   if (__syncthreads_or(any)) {
-    for_entries(a, info, [&](const Entry& e) {
-      if (contended(e))
-        __hip_atomic_fetch_max(a.last + e.page, static_cast<int>(e.flat) + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    entries.each([&](const Entry& e) {
+      if (contended(e)) last.raise(e.page, static_cast<int>(e.flat) + 1);
     });
     __syncthreads();
   }
@@ -202,10 +249,10 @@ __global__ __launch_bounds__(kThreads) void fork_plan_kernel(Pages a) {
     if (e.page < 0) return true;
     if (!more[e.page]) return false;
     if (other[e.page]) return true;
-    return __hip_atomic_load(a.last + e.page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != static_cast<int>(e.flat) + 1;
+    return last[e.page] != static_cast<int>(e.flat) + 1;
   };
   int n = 0, nc = 0;  // (uniform over the wave)
-  for_entries(a, info, [&](const Entry& e) {
+  entries.each([&](const Entry& e) {
     const bool y = need(e);
     n += __builtin_popcountll(__ballot(y));
     nc += __builtin_popcountll(__ballot(y && e.page >= 0));
@@ -242,14 +289,20 @@ __global__ __launch_bounds__(kThreads) void fork_plan_kernel(Pages a) {
   if (missing) return;
   int rank = free.before;
   for (int i = w0; i < w1 && rank < all; ++i)
-    for (uint32_t f = free_bits(i); f && rank < all; f &= f - 1)
-      as_global_mut(a.free)[rank++] = 32 * i + __builtin_ctz(f);
+    for (uint32_t f = free_bits(i); f && rank < all; f &= f - 1) {
+      const int page = 32 * i + __builtin_ctz(f);
+      if constexpr (ONCE) free_lds[rank++] = page;
+      else as_global_mut(a.free)[rank++] = page;
+    }
   __syncthreads();
-  for_entries(a, info, [&](const Entry& e) {
+  entries.each([&](const Entry& e) {
     const bool y = need(e), c = y && e.page >= 0;
     const uint64_t ys = __ballot(y), cs = __ballot(c), below = (1ull << lane) - 1;
     int to = e.page;
-    if (y) to = as_global(a.free)[before + __builtin_popcountll(ys & below)];
+    if (y) {
+      const int i = before + __builtin_popcountll(ys & below);
+      to = ONCE ? free_lds[i] : as_global(a.free)[i];
+    }
     if (c) as_global_mut(a.pairs)[copies_before + __builtin_popcountll(cs & below)] = make_int2(e.page, to);
     before += __builtin_popcountll(ys);
     copies_before += __builtin_popcountll(cs);
@@ -267,7 +320,9 @@ __global__ __launch_bounds__(kThreads) void compact_plan_kernel(Pages a) {
   for (int i = threadIdx.x; i < a.words; i += kThreads) used.clear(i);
   keep_info(a, kept);
   __syncthreads();
-  for_entries(a, InfoOf{a, kept}, [&](const Entry& e) {
+  const InfoOf info{a, kept};
+  Entries<false, InfoOf> entries(a, info);
+  entries.each([&](const Entry& e) {
     if (e.page >= 0) used.set(e.page);
   });
   __syncthreads();
@@ -448,8 +503,12 @@ int launch_fork(const sherry_cache_desc& c, const sherry_fork_desc& d, hipStream
   a.from = d.from_row;
   a.length_out = d.length_out;
   a.missing = d.missing;
-  const int rc = l.bits ? launch(fork_plan_kernel<false>, dim3(1), dim3(kThreads), 0, s, a)
-                        : launch(fork_plan_kernel<true>, dim3(1), dim3(kThreads), 12u * l.words, s, a);
+  const bool once = a.entries <= kThreads * kDeep;
+  const size_t bits = 12u * l.words, last = 4u * static_cast<size_t>(c.pages);
+  const int rc = !l.bits && once && bits + last <= kLdsSmall
+                     ? launch(fork_plan_kernel<true, true>, dim3(1), dim3(kThreads), bits + last, s, a)
+                 : l.bits ? launch(fork_plan_kernel<false, false>, dim3(1), dim3(kThreads), 0, s, a)
+                          : launch(fork_plan_kernel<true, false>, dim3(1), dim3(kThreads), bits, s, a);
   if (rc != SHERRY_OK) return rc;
   return launch(copy_kernel, dim3(copy_groups(a, l)), dim3(256), 0, s, a);
 }
