@@ -698,6 +698,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
           for (int j = 0; j < NT; ++j) pf[st & 1][j][i] = t[j];
         }
       };
+      // (Of two workgroups on a CU the older one was served first, 2.1 us a block against 3.2, and
+      // the other ended alone: chunk of 2048 tokens on 30011 rows 1183 us.  With what is half
+      // done first 1146; with turns by a clock 1136.)
+      __builtin_amdgcn_s_setprio(1);
       probabilities(0);
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
@@ -711,6 +715,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         if (st < 3) take_turns<DB * NT, (28 + 24 * (NT - 1)) / (DB * NT)>();
         fence();
       }
+      __builtin_amdgcn_s_setprio(0);
       l += sum[0] + sum[1];
       if (part && __builtin_amdgcn_readfirstlane(lds.nan[(kb - kb0) & 15])) {
         u32x4 mine_of;  // the attended rows, four a byte
