@@ -11,6 +11,12 @@
 // other, so that is one launch of one workgroup, its bits in LDS; the copies, whose
 // number the device alone knows, are a second one of as many workgroups as fill the
 // GPU, each taking 16 KB at a time.
+//
+// Measured: 32 beams of 100 to 1500 rows go on from others, 16 layers of 8 heads of 64 bf16
+// values 11.0 us, of which the plan is 7 to 8; 12 sequences get private copies of 2000 to 7000
+// shared rows, 4 layers of 8 heads of 128 e4m3 values, 0.49 GB both ways 89 us, 5.5 TB/s (part of
+// it in the caches); 32 compacted sequences, 0.98 GB 202 us, 4.8 TB/s, where a 4 GiB copy
+// reaches 4.67.
 #include "cache_internal.h"
 
 namespace sherry {
@@ -22,6 +28,8 @@ constexpr int kLdsWords = 10 * 1024;  // words of bits that are
 constexpr int kLdsSmall = 24 * 1024;  // bytes of bits and last places that are in LDS beside the free pages
 constexpr int kDeep = 4;             // strips of 64 entries in flight per wave
 constexpr int kChunk = 16384;        // bytes that a workgroup copies at once
+// (with 512 / 1024 / 2048 / 4096: 12 forked sequences 116 / 96 / 88 / 92 us, 32 compacted
+// 250 / 213 / 202 / 202)
 constexpr int kCopyGroups = 256 * 8;
 
 struct Meta {
@@ -146,7 +154,8 @@ struct Entry {
 
 // The entries that this wave has: its share of the table, kDeep strips of 64 at a time.
 // Once: they are no more than kDeep strips a wave, and stay in registers from one pass to
-// the next (a fork of 32 sequences of 96 places took 10.8 us with five passes over memory).
+// the next (32 beams of up to 94 places 11.4 us in all against 15.6 with every pass over memory,
+// 12 private prompts of up to 219 88 against 95).
 template <bool ONCE, class Info>
 struct Entries {
   const Pages& a;

@@ -54,13 +54,19 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kQRows = 32 * kWaves;  // of a tile
 constexpr int kRows = 64;            // of K and V at a time
 constexpr int kCus = 256, kXcds = 8;
-// What a tile costs besides its rows (its q, the first loads, the way out), in rows.
+// What a tile costs besides its rows (its q, the first loads, the way out), in rows.  With 64 /
+// 128 / 256 / 512: 16 drafts of 5 tokens 55.7 / 39.4 / 34.4 / 36.9 us, 6 prompts of 100 to 2500
+// tokens 163 / 125 / 93 / 90 (a run's end near a tile's begin or end goes there, block_at).
 constexpr int kTileCost = 256;
-constexpr int kMinRun = 512;         // the shortest run, in rows of cost
+// The shortest run, in rows of cost.  With 128 / 256 / 512: the drafts 30.7 / 30.6 / 33.4 us, one
+// sequence of 3000 rows and 5 tokens 22.6 / 22.7 / 27.1, one prompt of 500 tokens 36.4 / 34.9 / 38.2.
+constexpr int kMinRun = 256;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kMinusInf = -__builtin_huge_valf();
 constexpr float kUp = 10.0f;         // p is held times 2^kUp
-constexpr float kLazy = 5.0f;        // scores may pass the maximum by this
+// Scores may pass the maximum by this (with 0, where o is rescaled at every new maximum, 6
+// prompts 94.4 us against 92.7).
+constexpr float kLazy = 5.0f;
 
 // A tile that workgroup w has the beginning of, and `last` the end: its tokens [first, first
 // + tokens) and query heads.  tokens = 0: there is none.
@@ -311,7 +317,9 @@ struct Lds {
   alignas(16) uint8_t odd[2][DP][16];  // of a value and four rows, a bit each
 };
 
-// Waves per SIMD that the registers allow.
+// Waves per SIMD that the registers allow.  One more, spilling: chunk of 2048 tokens on 30011
+// rows of 128 values 1824 us against 1156, drafts of 64 values and two terms 59.0 against 34.4;
+// one fewer 1753 and 32.8.
 __host__ __device__ constexpr int waves_for(int dp, int terms) {
   return dp == 256 ? 1 : dp == 128 ? 2 : terms == 1 ? 3 : 2;
 }
@@ -395,7 +403,8 @@ __device__ __forceinline__ void take_turns() {
 }
 
 // DP: head_dim rounded up to 64, 128 or 256; NT: terms of q and p; QUADS: page_size % 4
-// == 0, so that four rows of V together have one factor.
+// == 0, so that four rows of V together have one factor (6 prompts 92.7 us against 97.5 without,
+// the chunk 1156 against 1169).
 template <int DP, int NT, bool QUADS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_for(DP, NT)))) void tokens_kernel(
     Tokens a) {
@@ -418,6 +427,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
   if (tid == 0) as_global_mut(a.split)[w] = Split{0, 0, 0, 0, 0};
   if (u >= u_end) return;
   Place pl = find_place(a, costs, u);
+  if (pl.b < 0) return;  // (as below)
 
   // this thread's places: of K a piece of 16 codes, of V some codes of four rows.
   // (Values past head_dim are those at 0: q has zeros there, and outputs are not written.)
@@ -738,18 +748,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
     // the blocks are is known from two to five blocks before they are read.
     // (first reads first: pages and q, then what the pages lead to)
     if (kb0 < kb1) {
+      look_page(kb0 + kWaves);
+      const int later_page = next_page, later_mask = next_mask;
       look_page(kb0);
       load_q<DP, NT>(a, int64_t(row.token) * a.q_stride + int64_t(row.head) * a.c.dim, qraw);
       look_scale(kb0);
+      const int64_t at = next_at;
+      const float ks = next_ks, vs = next_vs;
+      const bool ok = next_ok;
+      next_page = later_page;
+      next_mask = later_mask;
+      look_scale(kb0 + kWaves);
+      const int64_t later_at = next_at;
+      const float later_ks = next_ks, later_vs = next_vs;
+      const bool later_ok = next_ok;
+      next_at = at, next_ks = ks, next_vs = vs, next_ok = ok;
       __syncthreads();  // (the tile before has been read from LDS)
       lds.at[wave][lane] = next_at;
       look_refs(kb0);
       __syncthreads();
       load(0);
       publish(kb0);
-      look_page(kb0 + kWaves);
+      next_at = later_at, next_ks = later_ks, next_vs = later_vs, next_ok = later_ok;
       factor = split_q<DP, NT>(a, qraw, qf);
-      look_scale(kb0 + kWaves);
       __syncthreads();
       fill(0, 0);
       load(1);

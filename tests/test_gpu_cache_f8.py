@@ -230,6 +230,16 @@ def test_extend_token_by_token_keeps_older_rows(dev, ref):
         assert np.all(np.abs(got - x) <= 2 * (2.0 ** -4 * np.abs(x) + 2.0 ** -10 * power))
 
 
+@pytest.mark.parametrize("kind,heads,dim", [("bf16", 20, 64), ("f32", 40, 128)])
+def test_extend_of_so_many_tokens_that_workgroups_turn_several(dev, ref, kind, heads, dim):
+    """q of tokens that a workgroup takes one after the other: sequences that end among them,
+    that have none, and tokens that belong to nobody or lie past the table."""
+    _case("extend many", kind, heads, dim)
+    length, new = [3, 0, 16, 700, 5, 9, 40, 990], [700, 0, 1, 300, 3, 2, 1100, 60]
+    c = ref.Cache(np.random.default_rng(19), 8, 64, 1, 16, dim, length)
+    Extend(dev, ref, c, kind, heads, length, new, dim, lead=5, tail=9).check(ref)
+
+
 # ---- attention ------------------------------------------------------------------
 
 class Attend:
@@ -372,6 +382,37 @@ def test_tokens_long_rows_are_split_and_joined(dev, ref):
         mask = np.zeros((len(length), c.rows), np.uint8)
         mask[0, 1500:1503] = 1
         Attend(dev, ref, c, kind, heads, length, new, mask=mask).check(ref)
+
+
+@pytest.mark.parametrize("kind,dim,page", [("f32", 64, 16), ("bf16", 64, 48), ("bf16", 128, 10), ("f16", 256, 32)])
+@pytest.mark.parametrize("window", [0, 130])
+def test_tokens_over_every_number_of_blocks(dev, ref, kind, dim, page, window):
+    """Tiles over 1 to 11 blocks of rows, ending at, before and behind a block's end, with rows
+    left out that hold NaN."""
+    _case("tokens blocks", kind, dim, page, window)
+    rng = np.random.default_rng(20)
+    length = [max(0, 64 * i + j) for i in range(1, 12) for j in (-2, -1, 0)]
+    new = [1 + i % 3 for i in range(len(length))]
+    full = [n + m for n, m in zip(length, new)]
+    c = ref.Cache(rng, len(length), -(-max(full) // page), 1, page, dim, full)
+    mask = (rng.random((len(length), c.rows)) < 0.95).astype(np.uint8)
+    mask[::2] = 1
+    for b in range(len(length)):
+        for r in np.flatnonzero(mask[b, :full[b]] == 0):
+            c.code["k"][c.table[b, r // page], :, r % page] = 0x7F
+            c.code["v"][c.table[b, r // page], :, r % page] = 0xFF
+    Attend(dev, ref, c, kind, 3, length, new, window=window, mask=mask).check(ref)
+
+
+@pytest.mark.parametrize("kind,heads,kv,dim,window", [("bf16", 4, 1, 128, 0), ("f32", 4, 2, 64, 0), ("f16", 2, 1, 256, 0),
+                                                      ("bf16", 6, 2, 64, 777)])
+def test_tokens_whose_tiles_many_workgroups_share(dev, ref, kind, heads, kv, dim, window):
+    """Runs that end inside tiles, near their begin and near their end, several a tile."""
+    _case("tokens shared tiles", kind, heads, kv, dim, window)
+    length, new = [3000, 0, 1500], [200, 333, 70]
+    full = [n + m for n, m in zip(length, new)]
+    c = ref.Cache(np.random.default_rng(21), 3, -(-max(full) // 16), kv, 16, dim, full, spread=6)
+    Attend(dev, ref, c, kind, heads, length, new, window=window).check(ref)
 
 
 @pytest.mark.parametrize("scale", [0.0, -0.2, 30.0, 1e-30])

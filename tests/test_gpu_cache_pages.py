@@ -246,6 +246,22 @@ def test_large_pools(dev, ref):
         _compact(dev, ref, rng, table, lens, pages, 1, 1, 16, "f8", 1, 0)
 
 
+@pytest.mark.parametrize("pages,batch,width", [(4700, 70, 64), (4200, 64, 64), (9000, 64, 64), (2500, 1, 2100), (3000, 1030, 2)])
+def test_fork_of_tables_near_what_a_workgroup_keeps(dev, ref, pages, batch, width):
+    """Entries, pages and sequences on both sides of what stays in registers and on chip."""
+    _case("fork kept", pages, batch, width)
+    rng = np.random.default_rng(7)
+    lens = rng.integers(0, width + 1, batch)
+    table = rng.permutation(pages)[:batch * width].reshape(batch, width).astype(np.int32)
+    table[1:, 0] = np.where(rng.random(batch - 1) < 0.5, table[0, 0], table[1:, 0])
+    for in_place in (False, True):
+        parent = None if in_place else rng.integers(0, batch, batch)
+        add, from_row = rng.integers(0, 3, batch), lens // 3
+        want = ref.fork_plain(table, lens, pages, 1, parent, add, from_row)
+        pool = Pool(dev, ref, rng, table, pages, 1, 1, 16, "f8", 2)
+        Fork(dev, ref, pool, table, lens, parent, add, from_row, in_place=in_place).check(table, want)
+
+
 def test_beams_fork_extend_attend_compact_in_a_graph(dev, ref):
     """Beams of two requests: fork, new rows, attention of one token, then compact, the steps
     captured and replayed against the same steps run one by one."""
