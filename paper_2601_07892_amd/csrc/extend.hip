@@ -23,7 +23,7 @@
 //
 // Measured: 32 tokens of 32 sequences, 24 + 16 heads of 128 values, fp32 4.4 us, all of it a
 // launch and its chain of reads; 8 prompts of 37 to 2048 tokens, 32 + 16 heads of 64 bf16
-// values, 60 MB 25.8 us, 2.3 TB/s.
+// values, 60 MB 21.0 us, 2.85 TB/s.
 #include "rotary.h"
 
 namespace sherry {
@@ -46,6 +46,7 @@ struct Extend {
   int64_t q_stride, k_stride, v_stride, q_out_stride;
   int tokens, heads, units;   // units: most pages that the tokens reach
   int per_q;                  // tokens of a workgroup that turns q
+  int both;                   // its lanes have both values of a pair
   FastDiv by_parts, by_qparts;  // workgroups per page, and per per_q tokens for q
 };
 
@@ -223,26 +224,75 @@ __device__ __forceinline__ void store_pages(const Extend& a, int blk) {
   if (mine == 0 && lane == 0) as_global_mut(scale)[0] = power(now);
 }
 
-// per_q tokens one after the other, 256 / LPR of their heads.
+// per_q tokens one after the other, some of their heads.  With `both`, a lane has the four
+// values d and their four partners (or, behind the rotated values, eight): x and the angles are
+// read once for the two (8 prompts of 37 to 2048 tokens, 32 heads of 64 bf16 values: 22.6 us
+// against 25.8; with the reads of four tokens together 21.0).
 template <int LPR, int TYPE, bool VEC>
 __device__ __forceinline__ void turn_q(const Extend& a, int blk) {
+  const bool both = VEC && a.both;
   const int group = a.by_qparts.div(blk), part = blk - group * a.by_qparts.d;
   const int t0 = group * a.per_q, t1 = t0 + a.per_q < a.tokens ? t0 + a.per_q : a.tokens;
-  const int r = part * (256 / LPR) + threadIdx.x / LPR, d = 4 * (threadIdx.x % LPR);
+  const int lanes = both ? LPR / 2 : LPR;
+  const int r = part * (256 / lanes) + threadIdx.x / lanes, i = threadIdx.x % lanes;
+  const int half = a.rope.cos ? a.rope.rot >> 1 : 0;
+  const bool turned = 4 * i < half;
+  const int d = !both ? 4 * i : turned ? 4 * i : 2 * half + 8 * (i - half / 4), e = turned ? d + half : d + 4;
   const bool in = r < a.heads && d < a.c.dim;
   int b = __builtin_amdgcn_readfirstlane(find_sequence(a, t0));
   b = b < 0 ? 0 : b;
   Tokens s = tokens_of(a, b);
-#pragma unroll 4
-  for (int t = t0; t < t1; ++t) {
-    while (b + 1 < a.c.batch && as_const(a.first)[b + 1] <= t) s = tokens_of(a, ++b);
-    const int row = s.len + (t - s.t0);
-    if (t < s.t0 || t - s.t0 >= s.n) continue;
-    const int page = as_const(a.c.table)[int64_t(b) * a.c.width + a.c.by_page.div(row)];
-    const int pos = a.pos ? as_const(a.pos)[t] : row;
-    if (page < 0 || page >= a.c.pages || !a.rope.has(pos) || !in) continue;
-    store4<TYPE, VEC>(a.q_out, int64_t(t) * a.q_out_stride + r * a.c.dim + d,
-                      rotated<TYPE, VEC>(a.rope, a.q, int64_t(t) * a.q_stride + r * a.c.dim, d, pos));
+  for (int t4 = t0; t4 < t1; t4 += 4) {
+    // (all reads of four tokens before the first is used; of those left out too)
+    int pos[4];
+    bool ok[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int t = t4 + j < t1 ? t4 + j : t1 - 1;
+      while (b + 1 < a.c.batch && as_const(a.first)[b + 1] <= t) s = tokens_of(a, ++b);
+      const bool here = t >= s.t0 && t - s.t0 < s.n;
+      const int row = here ? s.len + (t - s.t0) : 0;
+      const int page = as_const(a.c.table)[int64_t(b) * a.c.width + a.c.by_page.div(row)];
+      pos[j] = a.pos ? as_const(a.pos)[t] : row;
+      ok[j] = here && page >= 0 && page < a.c.pages && a.rope.has(pos[j]) && t4 + j < t1;
+      pos[j] = ok[j] ? pos[j] : 0;
+    }
+    if (!in) continue;
+    if (!both) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (ok[j])
+          store4<TYPE, VEC>(a.q_out, int64_t(t4 + j) * a.q_out_stride + r * a.c.dim + d,
+                            rotated<TYPE, VEC>(a.rope, a.q, int64_t(t4 + j) * a.q_stride + r * a.c.dim, d, pos[j]));
+      continue;
+    }
+    float4 x[4], y[4], c[4], n[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t from = int64_t(t4 + j < t1 ? t4 + j : t1 - 1) * a.q_stride + r * a.c.dim;
+      x[j] = load4<TYPE, VEC>(a.q, from + d);
+      y[j] = load4<TYPE, VEC>(a.q, from + e);
+      if (turned) {
+        c[j] = *reinterpret_cast<const SHERRY_GLOBAL float4*>(as_global(a.rope.cos) + int64_t(pos[j]) * half + d);
+        n[j] = *reinterpret_cast<const SHERRY_GLOBAL float4*>(as_global(a.rope.sin) + int64_t(pos[j]) * half + d);
+      } else {
+        c[j] = n[j] = make_float4(0, 0, 0, 0);  // (not used)
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (!ok[j]) continue;
+      const int64_t to = int64_t(t4 + j) * a.q_out_stride + r * a.c.dim;
+      float4 u = x[j], v = y[j];
+      if (turned) {
+        u = make_float4(u.x * c[j].x - v.x * n[j].x, u.y * c[j].y - v.y * n[j].y, u.z * c[j].z - v.z * n[j].z,
+                        u.w * c[j].w - v.w * n[j].w);
+        v = make_float4(v.x * c[j].x + x[j].x * n[j].x, v.y * c[j].y + x[j].y * n[j].y, v.z * c[j].z + x[j].z * n[j].z,
+                        v.w * c[j].w + x[j].w * n[j].w);
+      }
+      store4<TYPE, VEC>(a.q_out, to + d, u);
+      store4<TYPE, VEC>(a.q_out, to + e, v);
+    }
   }
 }
 
@@ -259,6 +309,7 @@ struct Grid {
   int per_q;              // tokens of a workgroup that turns q
   int64_t parts, qparts;  // workgroups per page, and per per_q tokens for q
   bool wide;              // four waves per page, head and K or V
+  bool vec, both;
   int64_t blocks(int64_t tokens) const { return units * parts + ceil_div(tokens, per_q) * qparts; }
 };
 Grid grid_of(const sherry_cache_desc& c, const sherry_extend_desc& d) {
@@ -268,16 +319,23 @@ Grid grid_of(const sherry_cache_desc& c, const sherry_extend_desc& d) {
   const int64_t units = d.tokens / c.page_size + 2 * batch;  // n tokens reach n / page_size + 2 pages at most
   g.units = static_cast<int>(units < d.tokens ? units : d.tokens);
   // new rows of a page if the sequences have equally many
-  const int64_t rows = ceil_div(d.tokens, c.batch) < c.page_size ? ceil_div(d.tokens, c.batch) : c.page_size;
+  const int64_t new_rows = ceil_div(d.tokens, c.batch) < c.page_size ? ceil_div(d.tokens, c.batch) : c.page_size;
   // (One wave / four for 8 x 1024 tokens of 8 heads, bf16, in us: 64 values with pages of 32 rows
   // 11.2 / 20.2, of 64 16.8 / 14.3; 128 values with 16 18.7 / 35.4, with 32 20.4 / 24.5, with 64
   // 35.1 / 18.8; 256 values with 16 37.9 / 42.5, with 32 40.9 / 36.7.)
-  g.wide = rows > 32 || rows * lanes > 2 * 64 * kKeep;
+  g.wide = new_rows > 32 || new_rows * lanes > 2 * 64 * kKeep;
   g.parts = g.wide ? 2 * c.kv_heads : ceil_div(2 * c.kv_heads, 4);
-  g.qparts = d.q ? ceil_div(d.heads, 256 / lanes) : 0;
+  const int64_t qrow = int64_t(d.heads) * c.head_dim, row = int64_t(c.kv_heads) * c.head_dim;
+  auto whole = [&](const void* p, int64_t stride, int64_t least) { return whole_pieces(p, stride ? stride : least, d.type); };
+  g.vec = whole(d.k, d.k_stride, row) && whole(d.v, d.v_stride, row) &&
+          (!d.q || (whole(d.q, d.q_stride, qrow) && whole(d.q_out, d.q_out_stride, qrow))) &&
+          reinterpret_cast<uintptr_t>(d.cos) % 16 == 0 && reinterpret_cast<uintptr_t>(d.sin) % 16 == 0;
+  g.both = g.vec && (!d.cos || (d.pairing == SHERRY_ROPE_HALVES && d.rot_dim % 8 == 0));
+  g.qparts = d.q ? ceil_div(d.heads, 256 / (g.both ? lanes / 2 : lanes)) : 0;
   // A workgroup finds its token's place by reads that wait for each other; past what runs at
   // once it takes several tokens, whose places follow from the first one's (8 prompts of 37 to
-  // 2048 tokens, 32 heads of 64: 26.2 us against 32.1 with one each; up to 64 each 26.1).
+  // 2048 tokens, 32 heads of 64: 26.2 us against 32.1 with one each, before what turn_q
+  // tells; up to 64 each 26.1).
   const int64_t per = d.tokens * g.qparts / kQGroups;
   g.per_q = static_cast<int>(per < 1 ? 1 : per < kMostQ ? per : kMostQ);
   return g;
@@ -314,17 +372,13 @@ int launch_extend(const sherry_cache_desc& c, const sherry_extend_desc& d, hipSt
   const Extend a{cache_of(c), d.q, d.k, d.v, d.q_out, d.first, d.length, d.pos,
                  Rotary{d.cos, d.sin, d.rope_rows, d.rot_dim, d.pairing == SHERRY_ROPE_PAIRS},
                  d.q_stride ? d.q_stride : qrow, d.k_stride ? d.k_stride : row, d.v_stride ? d.v_stride : row,
-                 d.q_out_stride ? d.q_out_stride : qrow, d.tokens, heads, g.units, g.per_q,
+                 d.q_out_stride ? d.q_out_stride : qrow, d.tokens, heads, g.units, g.per_q, g.both,
                  FastDiv::of(static_cast<uint32_t>(g.parts)),
                  FastDiv::of(static_cast<uint32_t>(g.qparts ? g.qparts : 1))};
-  auto whole = [&](const void* p, int64_t stride) { return whole_pieces(p, stride, d.type); };
-  const bool vec = whole(a.k, a.k_stride) && whole(a.v, a.v_stride) &&
-                   (!heads || (whole(a.q, a.q_stride) && whole(a.q_out, a.q_out_stride))) &&
-                   reinterpret_cast<uintptr_t>(d.cos) % 16 == 0 && reinterpret_cast<uintptr_t>(d.sin) % 16 == 0;
   switch (lanes_per_row(c.head_dim)) {
-    case 16: return launch_type<16>(a, d.type, vec, g, s);
-    case 32: return launch_type<32>(a, d.type, vec, g, s);
-    default: return launch_type<64>(a, d.type, vec, g, s);
+    case 16: return launch_type<16>(a, d.type, g.vec, g, s);
+    case 32: return launch_type<32>(a, d.type, g.vec, g, s);
+    default: return launch_type<64>(a, d.type, g.vec, g, s);
   }
 }
 
