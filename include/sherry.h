@@ -758,8 +758,8 @@ typedef struct sherry_extend_desc {
  * cos, position) is out of range, or whose page does not exist, is left out
  * entirely, tokens outside first[0] .. first[batch] - 1 too.  No page that gets rows
  * may belong to another sequence (sherry_cache_fork sees to that); lengths are the
- * caller's.  Calls of 2^32 threads and more are refused (SHERRY_E_SHAPE): about
- * 256 for every 16 heads of a token's q and for every 2 heads of a page's k and v,
+ * caller's.  Calls of 2^32 threads and more are refused (SHERRY_E_SHAPE): at most
+ * 256 for every 4 heads of a token's q and for every head of k and of v of a page,
  * tokens / page_size + 2 batch pages. */
 int sherry_cache_extend(const sherry_cache_desc* cache, const sherry_extend_desc* args,
                         void* stream);

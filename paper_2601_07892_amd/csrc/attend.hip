@@ -40,8 +40,11 @@
 // two.  Over int8 K q is three int8 digits, rounded at 2^-22 of its
 // head's power of two, and their products are summed as integers (two f16 terms
 // against K converted to f16 took 71 us instead of 64 for 64 sequences of 4000
-// rows of 64 values, 119 instead of 100 for 256, 112 instead of 110 for 128).  q is
-// scaled by that power of two over every cache.
+// rows of 64 values, 119 instead of 100 for 256, 112 instead of 110 for 128).  e4m3
+// codes become f16, exactly; their pages' powers of two are applied as int8's scales are, without
+// rounding, and q takes one f16 term of bf16 and f16 (all of their bits, but for those below
+// 2^-24 of the head's largest value), two of fp32; p takes two.  q is scaled by that power of two
+// over every cache.
 //
 // Measured (kernel trace; a streaming read of 2 GiB reaches 7.05 TB/s):
 //  * 4 sequences of 130000 rows, 32 query heads over 8 of 128 bf16 values, 2.13
@@ -54,6 +57,10 @@
 //    a workgroup's beginning and end; conversions of V, scales, masks and stored
 //    scores make more than twice the vector instructions per byte of the case before.
 //    64 sequences of 4000 rows, 0.54 GB, without them: 98 to 104 us, 5.2 to 5.5 TB/s.
+//  * the first case's sizes in e4m3, a mask, 1.07 GB: 170 to 181 us and 4.9, 5.9 to 6.3 TB/s; without
+//    a mask, 24 heads, 184 with the join (5.8 TB/s), of 64 values 99 (5.4), of 256 327 (6.5).  32
+//    sequences of 0 to 8000 rows, 24 heads over 8 of 128 values, 66 MB: 21.6 and 4.6; one of 300
+//    rows of 64 values 8.2.
 //  * one sequence of 300 rows: 7.2 to 7.7 us in one launch, all of it latency (length, table,
 //    K, V, and the waves' sums, each after the other).
 #include <type_traits>
@@ -136,7 +143,8 @@ __device__ __forceinline__ Span span_of(const Attend& a, int b) {
 //   bf16  64        1.53 / 1.00 / 1.00 / 1.03 / 1.06 / 1.09 / 1.10
 //        128        1.70 / 1.14 / 1.00 / 1.03 / 1.06 / 1.15 / 1.23
 //        256        1.76 / 1.23 / 0.95 / 0.96 / 1.03 / 1.12 / 1.20
-// and f16 within 0.02 of bf16.
+// and f16 within 0.02 of bf16.  e4m3, with 6 / 10 / 24 tiles over that with 16:
+//   64 values 1.03 / 1.01 / 1.02, 128 1.04 / 1.00 / 1.02, 256 1.08 / 1.04 / 1.00.
 constexpr int sequence_cost(int type, int dp) {
   return type == SHERRY_I8 || type == SHERRY_F8 ? 16 : dp == 256 ? 8 : 6;
 }
@@ -315,7 +323,9 @@ struct Cfg {
   static constexpr int QS = I8 ? KL : KS;      // MFMA steps of q's operands
   // Tiles in flight per wave: int8 rows are half as many bytes, and leave the
   // registers for two (64 sequences of 4000 rows 100 us against 110 with 128 values,
-  // 59 against 64 with 64, 95 against 100 with 256; with a mask 102 against 111).
+  // 59 against 64 with 64, 95 against 100 with 256; with a mask 102 against 111).  So are rows of
+  // e4m3 (4 sequences of 130000 rows 99 us against 106 with 64 values, 184 against 188 with 128,
+  // 328 against 340 with 256; shorter ones within 3%).
   static constexpr int DEEP = BYTES && !ANY ? 2 : 1;
 };
 

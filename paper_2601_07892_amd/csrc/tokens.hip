@@ -8,7 +8,10 @@
 // What bounds it: 4 head_dim operations per token, query head and row, on the matrix
 // cores; and beside them, per score, an exponential, a maximum, a sum and a rounding
 // on the vector units, which is about as much for heads of 128 values and more for
-// heads of 64.  With few tokens, the cache's bytes.
+// heads of 64; and LDS, from which every wave reads all of K and V for its 32 rows of q, at
+// 128 bytes a cycle and CU as long as the matrix cores need for them.  With few tokens, a
+// workgroup's beginning (its place, and pages, scales and rows, each read after the other) and
+// the join.
 //
 // Work mapping.  A tile is 128 rows of q: as many tokens as fit, with all the query
 // heads that share one key-value head, so that K and V are read once for them.  What a tile
@@ -35,6 +38,15 @@
 // 2^10, are one term for 16-bit outputs (error 2^-11 of each at most, where the output's own
 // rounding is 2^-8 or 2^-11), two for fp32.  Scores, maxima, sums and outputs are
 // fp32; the maximum is taken anew only when a score passes it by 2^5.
+//
+// Measured (kernel trace, then the join; an f16 product of 8192^3 reaches 1196 TFLOP/s):
+//  * a chunk of 2048 tokens on 30011 rows, 32 heads over 8 of 128 values, bf16: 1090 to 1260 us
+//    with the clock, and 19; 1.04 PFLOP at 830 to 940 TFLOP/s.  The matrix cores are busy for 40% of the
+//    cycles, vector instructions issue in most of the rest.  Two rows of q per lane, which halve LDS's
+//    part, left one wave per SIMD: 2208 us.
+//  * 6 prompts of 100 to 2500 tokens, window 1024, 24 heads over 8 of 128 values: 80 and 13; a workgroup
+//    has some two tiles of six blocks, 2.2 us for its place, 11 us a tile beside its blocks.
+//  * 16 drafts of 5 tokens on 1 to 6000 rows, 32 heads over 8 of 64 values, fp32: 23 and 7.5.
 #include <type_traits>
 
 #include "cache_internal.h"
