@@ -27,11 +27,12 @@ struct Append {
   const int32_t* seq;
   const int32_t* slot;
   const int32_t* pos;
-  Rotary rope;
+  const float* cos;
+  const float* sin;
   float* weight;
   int32_t* position;
   int64_t row_stride, q_stride, k_stride, v_stride, q_out_stride;
-  int tokens, heads, type, cache_type;
+  int tokens, heads, type, cache_type, rope_rows, rot, pairs;
   FastDiv by_parts;  // workgroups per token
 };
 
@@ -43,7 +44,7 @@ __global__ __launch_bounds__(256) void append_kernel(Append a) {
   const int d = 4 * (threadIdx.x % LPR);
   const int seq = as_const(a.seq)[t], slot = as_const(a.slot)[t], pos = as_const(a.pos)[t];
   if (seq < 0 || seq >= a.c.batch || slot < 0 || slot >= a.c.rows) return;
-  if (!a.rope.has(pos)) return;
+  if (a.cos && (pos < 0 || pos >= a.rope_rows)) return;
   const int in_table = a.c.by_page.div(slot);
   const int page = as_const(a.c.table)[int64_t(seq) * a.c.width + in_table];
   if (page < 0 || page >= a.c.pages || r >= a.heads + 2 * a.c.kv) return;
@@ -51,14 +52,14 @@ __global__ __launch_bounds__(256) void append_kernel(Append a) {
   if (r < a.heads) {
     if (in)
       store4<TYPE, VEC>(a.q_out, int64_t(t) * a.q_out_stride + r * a.c.dim + d,
-                        rotated<TYPE, VEC>(a.rope, a.q, int64_t(t) * a.q_stride + r * a.c.dim, d, pos));
+                        rotated<TYPE, VEC>(a, a.q, int64_t(t) * a.q_stride + r * a.c.dim, d, pos));
     return;
   }
   const bool is_k = r < a.heads + a.c.kv;
   const int h = r - a.heads - (is_k ? 0 : a.c.kv);
   float4 x = make_float4(0, 0, 0, 0);
   if (in)
-    x = is_k ? rotated<TYPE, VEC>(a.rope, a.k, int64_t(t) * a.k_stride + h * a.c.dim, d, pos)
+    x = is_k ? rotated<TYPE, VEC>(a, a.k, int64_t(t) * a.k_stride + h * a.c.dim, d, pos)
              : load4<TYPE, VEC>(a.v, int64_t(t) * a.v_stride + h * a.c.dim + d);
   const int off = slot - in_table * a.c.page_size;
   char* pool = is_k ? a.c.k : a.c.v;
@@ -111,11 +112,10 @@ int64_t append_threads(const sherry_cache_desc& c, const sherry_append_desc& d) 
 int launch_append(const sherry_cache_desc& c, const sherry_append_desc& d, hipStream_t s) {
   const int heads = d.q ? d.heads : 0;
   const int64_t qrow = int64_t(heads) * c.head_dim, row = int64_t(c.kv_heads) * c.head_dim;
-  const Append a{cache_of(c), d.q, d.k, d.v, d.q_out, d.seq, d.slot, d.pos,
-                 Rotary{d.cos, d.sin, d.rope_rows, d.rot_dim, d.pairing == SHERRY_ROPE_PAIRS}, d.weight,
+  const Append a{cache_of(c), d.q, d.k, d.v, d.q_out, d.seq, d.slot, d.pos, d.cos, d.sin, d.weight,
                  d.position, d.row_stride, d.q_stride ? d.q_stride : qrow, d.k_stride ? d.k_stride : row,
                  d.v_stride ? d.v_stride : row, d.q_out_stride ? d.q_out_stride : qrow, d.tokens, heads,
-                 d.type, c.type, FastDiv{1, 0, 0}};
+                 d.type, c.type, d.rope_rows, d.rot_dim, d.pairing == SHERRY_ROPE_PAIRS, FastDiv{1, 0, 0}};
   // four values at once where every row starts at a multiple of them
   auto whole = [&](const void* p, int64_t stride) { return whole_pieces(p, stride, d.type); };
   const bool vec = whole(a.k, a.k_stride) && whole(a.v, a.v_stride) &&

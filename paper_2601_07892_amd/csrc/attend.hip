@@ -407,6 +407,9 @@ struct Rows {
     }
   }
 
+  __device__ __forceinline__ int64_t scale_at(int page, int off) const {
+    return G::F8 ? a.c.one_scale_at(page, h) : a.c.scale_at(page, h) + off;
+  }
   __device__ __forceinline__ int page_of(int tile, int t) const {
     const int ph = tile * kTile + 16 * t;
     return ph < end ? as_const(a.c.table)[int64_t(b) * a.c.width + a.c.by_page.quotient(ph)] : -1;
@@ -448,7 +451,7 @@ struct Rows {
       const int pid = next_page[0], off = p - a.c.by_page.div(p) * a.c.page_size;
       ok = ok && pid >= 0 && pid < a.c.pages;
       row = ok ? a.c.at(pid, h) + int64_t(off) * a.c.dim : 0;
-      if constexpr (G::BYTES) sat = ok ? a.c.scale_at(pid, h) + (G::I8 ? off : 0) : 0;
+      if constexpr (G::BYTES) sat = ok ? scale_at(pid, off) : 0;
       valid = static_cast<uint32_t>(__ballot(ok));
     } else {
       // (scalar: the rows from begin to end, and of pages that exist)
@@ -465,7 +468,7 @@ struct Rows {
         const int off = ph - a.c.by_page.quotient(ph) * a.c.page_size;
         rows[t] = valid >> (16 * t) & 0xFFFFu ? (end - ph < 16 ? end - ph : 16) : 0;
         at[t] = a.c.at(pid, h) + int64_t(off) * a.c.dim;
-        if constexpr (G::BYTES) srow[t] = a.c.scale_at(pid, h) + (G::I8 ? off : 0);
+        if constexpr (G::BYTES) srow[t] = scale_at(pid, off);
       }
     }
   }

@@ -33,12 +33,12 @@ struct Cache {
   const int32_t* table;
   int64_t page_stride;  // elements
   int pages, kv, page_size, dim, batch, width, rows;  // rows = width * page_size
-  int scales;  // of a head in a page: page_size (SHERRY_I8) or 1 (SHERRY_F8)
   FastDiv by_page;
-  // First row of head h in page p, in scales and in elements.
+  // First row of head h in page p, in rows (SHERRY_I8's scales) and in elements; SHERRY_F8's scale.
   __device__ __forceinline__ int64_t scale_at(int page, int h) const {
-    return (int64_t(page) * kv + h) * scales;
+    return (int64_t(page) * kv + h) * page_size;
   }
+  __device__ __forceinline__ int64_t one_scale_at(int page, int h) const { return int64_t(page) * kv + h; }
   __device__ __forceinline__ int64_t at(int page, int h) const {
     return int64_t(page) * page_stride + int64_t(h) * page_size * dim;
   }
@@ -54,7 +54,6 @@ inline Cache cache_of(const sherry_cache_desc& d) {
   return Cache{static_cast<char*>(d.k), static_cast<char*>(d.v), d.k_scale, d.v_scale, d.table,
                d.page_stride ? d.page_stride : whole, d.pages, d.kv_heads, d.page_size,
                d.head_dim, d.batch, d.table_width, d.table_width * d.page_size,
-               d.type == SHERRY_F8 ? 1 : d.page_size,
                FastDiv::of(static_cast<uint32_t>(d.page_size))};
 }
 

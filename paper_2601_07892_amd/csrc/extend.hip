@@ -159,7 +159,7 @@ __device__ __forceinline__ void store_pages(const Extend& a, int blk) {
     one(x.x), one(x.y), one(x.z), one(x.w);
   };
   // (a page that holds rows already: the power that they have)
-  float* scale = (is_k ? a.c.ks : a.c.vs) + a.c.scale_at(page, h);
+  float* scale = (is_k ? a.c.ks : a.c.vs) + a.c.one_scale_at(page, h);
   const bool fresh = p0 >= t.len;
   int old = 0;
   if (!fresh) {

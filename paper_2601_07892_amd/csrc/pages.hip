@@ -489,7 +489,7 @@ Pages pages_of(const sherry_cache_desc& c, const D& d, const Layout& l) {
   a.scale_layer_bytes = d.layers > 1 ? d.scale_layer_stride * 4 : 0;
   a.page_stride_bytes = a.c.page_stride * e;
   a.page_bytes = int64_t(c.kv_heads) * c.page_size * c.head_dim * e;
-  a.scale_bytes = c.k_scale ? int64_t(c.kv_heads) * a.c.scales * 4 : 0;
+  a.scale_bytes = c.k_scale ? int64_t(c.kv_heads) * (c.type == SHERRY_F8 ? 1 : c.page_size) * 4 : 0;
   a.layers = d.layers;
   a.chunks = ceil_div(a.page_bytes, kChunk);
   return a;

@@ -40,9 +40,10 @@ struct Rotary {
   __device__ __forceinline__ bool has(int pos) const { return !cos || (pos >= 0 && pos < rows); }
 };
 
-// Values d .. d + 3 of a row at element `at`, turned.
-template <int TYPE, bool VEC>
-__device__ __forceinline__ float4 rotated(const Rotary& a, const void* p, int64_t at, int d, int pos) {
+// Values d .. d + 3 of a row at element `at`, turned (by cos, sin, rot and pairs of a Rotary or of
+// what has them too).
+template <int TYPE, bool VEC, class Angles>
+__device__ __forceinline__ float4 rotated(const Angles& a, const void* p, int64_t at, int d, int pos) {
   const float4 x = load4<TYPE, VEC>(p, at + d);
   if (!a.cos || d >= a.rot) return x;
   const int half = a.rot >> 1;

@@ -516,8 +516,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       const int page = there ? next_page : 0;
       const int off = there ? row - static_cast<int>(a.c.by_page.div(row)) * a.c.page_size : 0;
       next_at = a.c.at(page, kvh) + int64_t(off) * a.c.dim;
-      next_ks = as_global(a.c.ks)[a.c.scale_at(page, kvh)];
-      next_vs = as_global(a.c.vs)[a.c.scale_at(page, kvh)];
+      next_ks = as_global(a.c.ks)[a.c.one_scale_at(page, kvh)];
+      next_vs = as_global(a.c.vs)[a.c.one_scale_at(page, kvh)];
     };
     auto look_refs = [&](int kb) SHERRY_INLINE {
       // (largest of both at once; a row that is masked shares its factor with others of its page)
