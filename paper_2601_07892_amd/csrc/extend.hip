@@ -334,8 +334,7 @@ Grid grid_of(const sherry_cache_desc& c, const sherry_extend_desc& d) {
   g.qparts = d.q ? ceil_div(d.heads, 256 / (g.both ? lanes / 2 : lanes)) : 0;
   // A workgroup finds its token's place by reads that wait for each other; past what runs at
   // once it takes several tokens, whose places follow from the first one's (8 prompts of 37 to
-  // 2048 tokens, 32 heads of 64: 26.2 us against 32.1 with one each, before what turn_q
-  // tells; up to 64 each 26.1).
+  // 2048 tokens, 32 heads of 64: 21.0 us against 29.4 with one each).
   const int64_t per = d.tokens * g.qparts / kQGroups;
   g.per_q = static_cast<int>(per < 1 ? 1 : per < kMostQ ? per : kMostQ);
   return g;

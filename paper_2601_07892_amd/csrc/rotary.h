@@ -13,7 +13,7 @@ typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 
 // TYPE: SHERRY_F32, _F16 or _BF16 of q, k, v and q_out.  VEC: their rows and the
 // angles' start at multiples of four values (appending 2048 tokens of 32 + 16 heads of 64
-// int8 values 12 us against 18 value by value, extending by 8 prompts 26 against 43).
+// int8 values 12 us against 18 value by value, extending by 8 prompts 21 against 46).
 template <int TYPE>
 __device__ __forceinline__ float load1(const void* p, int64_t i) {
   return load_as_f32(p, i, TYPE);

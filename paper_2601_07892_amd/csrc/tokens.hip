@@ -40,13 +40,13 @@
 // fp32; the maximum is taken anew only when a score passes it by 2^5.
 //
 // Measured (kernel trace, then the join; an f16 product of 8192^3 reaches 1196 TFLOP/s):
-//  * a chunk of 2048 tokens on 30011 rows, 32 heads over 8 of 128 values, bf16: 1090 to 1260 us
-//    with the clock, and 19; 1.04 PFLOP at 830 to 940 TFLOP/s.  The matrix cores are busy for 40% of the
+//  * a chunk of 2048 tokens on 30011 rows, 32 heads over 8 of 128 values, bf16: 1100 to 1190 us
+//    with the clock, and 16; 1.04 PFLOP at 880 to 950 TFLOP/s.  The matrix cores are busy for 42% of the
 //    cycles, vector instructions issue in most of the rest.  Two rows of q per lane, which halve LDS's
 //    part, left one wave per SIMD: 2208 us.
-//  * 6 prompts of 100 to 2500 tokens, window 1024, 24 heads over 8 of 128 values: 80 and 13; a workgroup
-//    has some two tiles of six blocks, 2.2 us for its place, 11 us a tile beside its blocks.
-//  * 16 drafts of 5 tokens on 1 to 6000 rows, 32 heads over 8 of 64 values, fp32: 23 and 7.5.
+//  * 6 prompts of 100 to 2500 tokens, window 1024, 24 heads over 8 of 128 values: 76 and 10.6; a workgroup
+//    has some two tiles of six blocks, 2.2 us for its place, some 10 us a tile beside its blocks.
+//  * 16 drafts of 5 tokens on 1 to 6000 rows, 32 heads over 8 of 64 values, fp32: 23.6 and 7.6.
 #include <type_traits>
 
 #include "cache_internal.h"
@@ -218,6 +218,22 @@ __device__ __forceinline__ Place find_place(const Tokens& a, const Costs& first,
     p.t = lo;
     p.at = in - cost_of(a, p.s, lo);
     return p;
+  }
+  return Place{-1, 0, 0, 0, {0, 0, 0, 0}};
+}
+// The first tile of the next sequence from b on that has tokens (by find_place, whose scan begins
+// at the first sequence: 4096 sequences of 100 rows and a token 469 us against 219, 6 prompts 86
+// against 82, as its registers are not held then).
+__device__ __forceinline__ Place next_place(const Tokens& a, int b) {
+  const int lane = threadIdx.x & 63;
+  for (; b < a.c.batch; b += 64) {
+    const Seq s = b + lane < a.c.batch ? seq_of(a, b + lane) : Seq{0, 0, 0, 0};
+    const uint64_t some = __ballot(s.n > 0);
+    if (!some) continue;
+    const int at = __builtin_ctzll(some);
+    return Place{b + at, 0, 0, 0,
+                 Seq{__builtin_amdgcn_readlane(s.t0, at), __builtin_amdgcn_readlane(s.n, at),
+                     __builtin_amdgcn_readlane(s.len, at), __builtin_amdgcn_readlane(s.tiles, at)}};
   }
   return Place{-1, 0, 0, 0, {0, 0, 0, 0}};
 }
@@ -863,7 +879,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       ++pl.head;
       pl.t = 0;
     } else {
-      pl = find_place(a, costs, u);
+      pl = next_place(a, pl.b + 1);
       if (pl.b < 0) return;
     }
   }

@@ -415,6 +415,18 @@ def test_tokens_whose_tiles_many_workgroups_share(dev, ref, kind, heads, kv, dim
     Attend(dev, ref, c, kind, heads, length, new, window=window).check(ref)
 
 
+@pytest.mark.parametrize("kind,every", [("f32", 1), ("bf16", 3), ("f32", 130)])
+def test_tokens_of_many_sequences_most_of_them_without(dev, ref, kind, every):
+    """Workgroups that go on from sequence to sequence, over those without tokens."""
+    _case("tokens many sequences", kind, every)
+    rng = np.random.default_rng(22)
+    length = [int(n) for n in rng.integers(0, 150, 300)]
+    new = [1 + i % 4 if i % every == every // 2 else 0 for i in range(300)]
+    full = [n + m for n, m in zip(length, new)]
+    c = ref.Cache(rng, 300, -(-max(full) // 16), 1, 16, 64, full)
+    Attend(dev, ref, c, kind, 2, length, new, lead=1, tail=2).check(ref)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.2, 30.0, 1e-30])
 def test_tokens_scales_of_scores(dev, ref, scale):
     """No, negative, one-hot and vanishing scores; powers of pages far apart."""
