@@ -868,7 +868,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       const int tok0 = pl.t * a.per_tile;
       const int64_t from = u - pl.at;
       int64_t last = divide(from + cost - 1, run);
-      if (block_at(sp, last * run - from, cost) == sp.k1) --last;
+      // (runs that begin where no block is left: near the end, and, of a tile whose tokens lie past the
+      // table, behind its rows, which its cost counts all the same)
+      while (block_at(sp, last * run - from, cost) == sp.k1) --last;
       as_global_mut(a.split)[w] = Split{s.t0 + tok0, s.n - tok0 < a.per_tile ? s.n - tok0 : a.per_tile, head0, heads,
                                         static_cast<int>(last)};
     }
