@@ -867,10 +867,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
     if (tid == 0 && begins && kb0 < kb1 && !whole) {  // (another workgroup ends it)
       const int tok0 = pl.t * a.per_tile;
       const int64_t from = u - pl.at;
-      int64_t last = divide(from + cost - 1, run);
-      // (runs that begin where no block is left: near the end, and, of a tile whose tokens lie past the
-      // table, behind its rows, which its cost counts all the same)
-      while (block_at(sp, last * run - from, cost) == sp.k1) --last;
+      // the last run whose begin leaves it a block (block_at): not those near the tile's end, and, of a tile
+      // whose tokens lie past the table, not those behind its rows, which its cost counts all the same
+      const int64_t rows_end = kTileCost / 2 + int64_t(sp.k1 - sp.k0) * kRows - 1, tile_end = cost - kTileCost;
+      const int64_t last = divide(from + (rows_end < tile_end ? rows_end : tile_end), run);
       as_global_mut(a.split)[w] = Split{s.t0 + tok0, s.n - tok0 < a.per_tile ? s.n - tok0 : a.per_tile, head0, heads,
                                         static_cast<int>(last)};
     }
