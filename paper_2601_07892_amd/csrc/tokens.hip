@@ -31,8 +31,11 @@
 //    written to LDS transposed, and with its rows in the order that this asks for.
 //
 // Precision.  e4m3 codes are exact in f16, and so are their products with powers of
-// two down to 2^-15 of the largest in a tile of K, or so far of V, which take the pages'
-// scales (smaller ones are rounded at 2^-33 of that largest value).  q is scaled by the
+// two down to 2^-15, which take the pages' scales.  Where the powers of a tile lie further apart, in a
+// block or from block to block, a launch of its own (FAR) takes the rest of the workgroup's run: codes are
+// operands as they are, the scores are multiplied by the powers of K's pages, and the probabilities by those of
+// V's over the largest that the token itself has attended to (rounded at 2^-35 of that).  So rows that a token leaves
+// out change nothing for it, however large they are.  q is scaled by the
 // power of two of its row's largest value: one f16 term holds all of bf16 and f16 values (but for
 // bits below 2^-25 of that largest), two 22 bits of fp32.  Probabilities, times
 // 2^10, are one term for 16-bit outputs (error 2^-11 of each at most, where the output's own
@@ -81,6 +84,12 @@ constexpr float kUp = 10.0f;         // p is held times 2^kUp
 // Scores may pass the maximum by this (with 0, where o is rescaled at every new maximum, 6
 // prompts 94.4 us against 92.7).
 constexpr float kLazy = 5.0f;
+// A code times 2^0 .. 2^-15 is exact in f16: K's powers may differ by this in a block, V's in a block and
+// from one block's largest to another's.
+constexpr int kFarK = 15, kFarV = 8, kFarBlocks = 7;
+// K's largest biased exponent that scores may be multiplied by at once (past it the factor of rows that
+// a token leaves out could be infinite).
+constexpr int kMostK = 127 + 64;
 
 // A tile that workgroup w has the beginning of, and `last` the end: its tokens [first, first
 // + tokens) and query heads.  tokens = 0: there is none.
@@ -100,6 +109,7 @@ struct Tokens {
   float2* stat;  // [part][part_rows]: where p is 1, in units of ln 2, and the sum of p
   float* sums;   // [part][part_rows][DP]: outputs of these rows
   Split* split;  // [workgroup]
+  int64_t* rest;  // [workgroup]: the unit from which FAR takes its run, or -1
   int64_t q_stride, out_stride, mask_stride;
   int tokens, heads, group, gtiles, per_tile, hp, type, window, groups, part_rows;
   float scale;
@@ -266,6 +276,13 @@ __device__ __forceinline__ int block_at(const Span& sp, int64_t at, int64_t cost
   return k < sp.k1 ? static_cast<int>(k) : sp.k1;
 }
 
+// The kernel's arguments, to be read where this is called.
+__device__ __forceinline__ const SHERRY_CONST Tokens* late_args() {
+  uint64_t p = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return (const SHERRY_CONST Tokens*)p;
+}
+
 // ---- operands -----------------------------------------------------------------
 
 __device__ __forceinline__ v16f mfma(const u32x4& a, const u32x4& b, const v16f& c) {
@@ -339,10 +356,11 @@ struct Lds {
   // of eight blocks:
   int64_t at[8][kRows];     // where a row begins in its pool (of no page: a place that can be read)
   float kx[8][kRows], vx[8][kRows];  // what its codes are multiplied by
+  uint8_t ke[8][kRows], ve[8][kRows];  // FAR: the biased exponents of its page's scales
   // which rows there are (64 bits); kref | vref << 8 | part << 16, the biased exponents that
   // the products with kx and vx are over, and whether not every row of the tile attends to all
   u32x4 about[8];
-  int vmax[8];              // the largest biased exponent of V's scales
+  int vmax[8];              // the largest biased exponent of V's scales (0: no rows); 256 where some lie far below
   int nan[16];               // and some code of V is NaN:
   alignas(16) uint8_t odd[2][DP][16];  // of a value and four rows, a bit each
 };
@@ -434,8 +452,11 @@ __device__ __forceinline__ void take_turns() {
 
 // DP: head_dim rounded up to 64, 128 or 256; NT: terms of q and p; QUADS: page_size % 4
 // == 0, so that four rows of V together have one factor (6 prompts 92.7 us against 97.5 without,
-// the chunk 1156 against 1169).
-template <int DP, int NT, bool QUADS>
+// the chunk 1156 against 1169).  FAR: powers anywhere; takes what the launch without it has left (in one
+// launch with both, a row's own powers in every block's loop: chunk of 2048 tokens on 30011 rows 1159 us against
+// 1108, 6 prompts 89 against 80; a launch with nothing to take is 1 to 2 us).  1024 bf16 tokens on 8000 rows of 128
+// values, powers of pages anywhere in 2^-30 .. 1: 398 us, where they are near each other 191.
+template <int DP, int NT, bool QUADS, bool FAR>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_for(DP, NT)))) void tokens_kernel(
     Tokens a) {
   constexpr int KS = DP / 16;   // MFMA steps of a score
@@ -450,11 +471,19 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // consecutive runs on one XCD (workgroups go to them in turn)
   const int w = blockIdx.x % kXcds * (a.groups / kXcds) + blockIdx.x / kXcds;
+  if constexpr (FAR) {
+    if (as_const(a.rest)[w] < 0) return;
+  }
   const Costs costs = costs_of(a);
   const int64_t run = run_of(a, costs.all);
   int64_t u = int64_t(w) * run;
   const int64_t u_end = u + run < costs.all ? u + run : costs.all;
-  if (tid == 0) as_global_mut(a.split)[w] = Split{0, 0, 0, 0, 0};
+  if constexpr (FAR) {
+    u = as_const(a.rest)[w];
+  } else if (tid == 0) {
+    as_global_mut(a.split)[w] = Split{0, 0, 0, 0, 0};
+    as_global_mut(a.rest)[w] = -1;
+  }
   if (u >= u_end) return;
   Place pl = find_place(a, costs, u);
   if (pl.b < 0) return;  // (as below)
@@ -517,7 +546,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 
     // ---- what the waves find out about blocks of rows, each about every fourth block:
     // its pages, their scales, the largest of these, and what follows for its rows ----
-    int next_page = -1, next_mask = 1, seen_vref = 1, next_kref = 1;
+    int next_page = -1, next_mask = 1, seen_vref = 1, seen_vlow = 255, next_kref = 1;
+    int stop = kb1;  // the first group of blocks that FAR has to take
     int64_t next_at = 0;
     float next_ks = 0, next_vs = 0;
     bool next_ok = false;
@@ -538,27 +568,41 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       next_vs = as_global(a.c.vs)[a.c.one_scale_at(page, kvh)];
     };
     auto look_refs = [&](int kb) SHERRY_INLINE {
-      // (largest of both at once; a row that is masked shares its factor with others of its page)
-      const uint32_t both = next_ok ? exponent(next_ks) | exponent(next_vs) << 16 : 0x10001u;
-      const uint32_t top = wave_max_pairs(both);
-      next_kref = top & 0xFFFF;
-      if (lane == 0) lds.vmax[(kb - kb0 + wave) & 7] = top >> 16;
+      if constexpr (!FAR) {
+        // (largest of both at once; a row that is masked shares its factor with others of its page)
+        const int ke = exponent(next_ks), ve = exponent(next_vs);
+        const uint32_t top = wave_max_pairs(next_ok ? static_cast<uint32_t>(ke | ve << 16) : 0u);
+        const int vref = top >> 16;
+        next_kref = top & 0xFFFF;
+        const bool far = __any(next_ok && (ke + kFarK < next_kref || ve + kFarV < vref)) || next_kref > kMostK;
+        if (lane == 0) lds.vmax[(kb - kb0 + wave) & 7] = far ? vref | 256 : vref;
+      }
     };
     auto publish = [&](int kb) SHERRY_INLINE {
       const int slot = (kb - kb0 + wave) & 7;
+      if constexpr (!FAR) {
+        bool far = false;
 #pragma unroll
-      for (int i = 0; i < kWaves; ++i) {
-        const int v = __builtin_amdgcn_readfirstlane(lds.vmax[(kb - kb0 + i) & 7]);
-        seen_vref = v > seen_vref ? v : seen_vref;
+        for (int i = 0; i < kWaves; ++i) {
+          const int v = __builtin_amdgcn_readfirstlane(lds.vmax[(kb - kb0 + i) & 7]), top = v & 0xFF;
+          seen_vref = top > seen_vref ? top : seen_vref;
+          seen_vlow = top > 0 && top < seen_vlow ? top : seen_vlow;
+          far = far || v > 255;
+        }
+        if (far || seen_vref > seen_vlow + kFarBlocks) stop = stop < kb ? stop : kb;
       }
       auto over = [](int ref, int e) { return power(ref - e < 0 ? 127 : ref - e < 126 ? 127 - (ref - e) : 1); };
       lds.at[slot][lane] = next_at;
-      lds.kx[slot][lane] = over(next_kref, exponent(next_ks));
-      lds.vx[slot][lane] = over(seen_vref, exponent(next_vs));
+      lds.kx[slot][lane] = FAR ? 1.0f : over(next_kref, exponent(next_ks));
+      lds.vx[slot][lane] = FAR ? 1.0f : over(seen_vref, exponent(next_vs));
+      if constexpr (FAR) {
+        lds.ke[slot][lane] = static_cast<uint8_t>(exponent(next_ks));
+        lds.ve[slot][lane] = static_cast<uint8_t>(exponent(next_vs));
+      }
       const uint64_t valid = __ballot(next_ok);
       const int row0 = (kb + wave) * kRows;
       if (lane == 0) {
-        const bool part = ~valid != 0 || row0 + kRows > all_lim || row0 < all_low;
+        const bool part = FAR || ~valid != 0 || row0 + kRows > all_lim || row0 < all_low;
         lds.about[slot] = u32x4{static_cast<uint32_t>(valid), static_cast<uint32_t>(valid >> 32),
                                 static_cast<uint32_t>(next_kref | seen_vref << 8 | int(part) << 16), 0};
         lds.nan[(kb - kb0 + wave) & 15] = 0;
@@ -684,9 +728,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       }
       const uint32_t refs = __builtin_amdgcn_readfirstlane(about[2]);
       const bool part = refs >> 16;
-      const int vref = refs >> 8 & 0xFF;
+      int vref = refs >> 8 & 0xFF;
       // (above 0, so that -infinity stays what it is)
-      const float f = fmaxf(factor * power(refs & 0xFF), 0x1p-126f);
+      float f = fmaxf(FAR ? factor : factor * power(refs & 0xFF), 0x1p-126f);
       // the rows that this row of q attends to
       auto attended = [&](int h) {
         const int most = lim - row0 - 32 * h, least = low - row0 - 32 * h;
@@ -701,11 +745,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
           for (int i = 0; i < 16; ++i) sc[h][i] = (ok >> (8 * (i / 4) + i % 4)) & 1 ? sc[h][i] : kMinusInf;
         }
       }
+      auto exponent_of = [&](const uint8_t (&x)[8][kRows], int h, int i) SHERRY_INLINE {  // of a score's row
+        const uint8_t* four = &x[(kb - kb0) & 7][32 * h + 8 * (i / 4) + 4 * g];
+        return *reinterpret_cast<const uint32_t*>(four) >> (8 * (i % 4)) & 0xFF;
+      };
+      if constexpr (FAR) {
+        uint32_t most = 1;  // of V's exponents in attended rows
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t v = exponent_of(lds.ve, h, i);
+            most = v > most && sc[h][i] != kMinusInf ? v : most;
+            sc[h][i] = sc[h][i] * f * power(exponent_of(lds.ke, h, i));
+          }
+        f = 1.0f;
+        vref = static_cast<int>(max_of_halves(most));
+        vref = vref > vrun ? vref : vrun;
+      }
       float top = sc[0][0];
 #pragma unroll
       for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i >> 4][i & 15]);
       top = max_of_halves(top) * f;
-      if (__any(top > m + kLazy) || vref > vrun) {
+      if (FAR ? __any(top > m + kLazy || vref > vrun) : __any(top > m + kLazy) || vref > vrun) {
         const bool up = top > m;
         const float to = up ? top - kUp : base;
         float down = m == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(base - to);
@@ -714,12 +776,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
           m = top;
         }
         l *= down;
-        down *= power(vref - vrun < 126 ? 127 - (vref - vrun) : 1);
+        if constexpr (FAR) down = __builtin_amdgcn_ldexpf(down, vrun - vref);
+        else down *= power(vref - vrun < 126 ? 127 - (vref - vrun) : 1);  // (so far only where o is 0)
         vrun = vref;
 #pragma unroll
         for (int i = 0; i < DB; ++i)
 #pragma unroll
           for (int j = 0; j < 16; ++j) o[i][j] *= down;
+      }
+      if constexpr (FAR) {  // p's sum, and the scores whose p is times V's powers
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            l += __builtin_amdgcn_exp2f(sc[h][i] - base);
+            sc[h][i] += static_cast<float>(static_cast<int>(exponent_of(lds.ve, h, i)) - vrun);
+          }
       }
       float sum[2] = {0.0f, 0.0f};
       u32x4 pf[2][NT];
@@ -756,7 +828,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         fence();
       }
       __builtin_amdgcn_s_setprio(0);
-      l += sum[0] + sum[1];
+      if constexpr (!FAR) l += sum[0] + sum[1];
       if (part && __builtin_amdgcn_readfirstlane(lds.nan[(kb - kb0) & 15])) {
         u32x4 mine_of;  // the attended rows, four a byte
 #pragma unroll
@@ -823,7 +895,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       load((rel + 2) & 7);
       __syncthreads();
     };
-    for (int kb = kb0; kb < kb1; kb += 4) {
+    for (int kb = kb0; kb < stop; kb += 4) {
       turn(std::integral_constant<int, 0>{}, kb);
       if (kb + 1 >= kb1) break;
       turn(std::integral_constant<int, 1>{}, kb + 1);
@@ -833,18 +905,27 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       turn(std::integral_constant<int, 3>{}, kb + 3);
     }
 
+    if constexpr (!FAR) {
+      if (__builtin_expect(stop < kb1, 0)) {
+        if (tid == 0) as_global_mut(late_args()->rest)[w] = u;
+        return;
+      }
+    }
+
     // ---- the way out: o over p's sum ----
     l += __shfl_xor(l, 32, 64);
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    // (arguments that only this part needs, read here: kept, they would take registers all the way)
+    const SHERRY_CONST Tokens& late = *late_args();
     int again = n;  // (found anew: it would take registers all the way)
     asm volatile("" : "+v"(again));
     const Row out = row_of(again);
     if (out.mine && (kb0 < kb1 || whole)) {
       const float times = power(vrun);
-      const int64_t part = int64_t(2 * w + begins) * a.part_rows + out.r;
-      const int64_t at = whole ? int64_t(out.token) * a.out_stride + int64_t(out.head) * a.c.dim : part * DP;
-      if (!whole && g == 0) as_global_mut(a.stat)[part] = make_float2(base, l);
-      SHERRY_GLOBAL char* to = as_global_mut(static_cast<char*>(whole ? a.out : a.sums)) +
+      const int64_t part = int64_t(2 * w + begins) * late.part_rows + out.r;
+      const int64_t at = whole ? int64_t(out.token) * late.out_stride + int64_t(out.head) * a.c.dim : part * DP;
+      if (!whole && g == 0) as_global_mut(late.stat)[part] = make_float2(base, l);
+      SHERRY_GLOBAL char* to = as_global_mut(static_cast<char*>(whole ? late.out : late.sums)) +
                                (at + 4 * g) * (whole && NT == 1 ? 2 : 4);
 #pragma unroll
       for (int db = 0; db < DB; ++db)
@@ -859,7 +940,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
             *reinterpret_cast<SHERRY_GLOBAL v4f*>(to + 4 * d) = x;
           else
             *reinterpret_cast<SHERRY_GLOBAL u32x2*>(to + 2 * d) =
-                a.type == SHERRY_BF16 ? u32x2{pair_bf16(x[0], x[1]), pair_bf16(x[2], x[3])}
+                late.type == SHERRY_BF16 ? u32x2{pair_bf16(x[0], x[1]), pair_bf16(x[2], x[3])}
                                       : u32x2{pair_f16(x[0], x[1]), pair_f16(x[2], x[3])};
         }
     }
@@ -871,7 +952,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
       // whose tokens lie past the table, not those behind its rows, which its cost counts all the same
       const int64_t rows_end = kTileCost / 2 + int64_t(sp.k1 - sp.k0) * kRows - 1, tile_end = cost - kTileCost;
       const int64_t last = divide(from + (rows_end < tile_end ? rows_end : tile_end), run);
-      as_global_mut(a.split)[w] = Split{s.t0 + tok0, s.n - tok0 < a.per_tile ? s.n - tok0 : a.per_tile, head0, heads,
+      as_global_mut(late.split)[w] = Split{s.t0 + tok0, s.n - tok0 < a.per_tile ? s.n - tok0 : a.per_tile, head0, heads,
                                         static_cast<int>(last)};
     }
     u += upto - pl.at;
@@ -942,7 +1023,7 @@ int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 struct Shape {
   int group, gtiles, hp, per_tile, groups, part_rows;
-  size_t split_bytes, stat_bytes, sum_bytes;
+  size_t split_bytes, rest_bytes, stat_bytes, sum_bytes;
 };
 Shape shape_of(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d) {
   Shape s{};
@@ -962,15 +1043,20 @@ Shape shape_of(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d) {
   const int64_t part = int64_t(d.tokens) * s.hp;
   s.part_rows = static_cast<int>(part < kQRows ? part : kQRows);
   s.split_bytes = (s.groups * sizeof(Split) + 255) / 256 * 256;
+  s.rest_bytes = (s.groups * sizeof(int64_t) + 255) / 256 * 256;
   s.stat_bytes = (size_t(2) * s.groups * s.part_rows * 8 + 255) / 256 * 256;
   s.sum_bytes = size_t(2) * s.groups * s.part_rows * dp * 4;
   return s;
 }
+template <int DP, int NT, bool QUADS>
+int launch_both(const Tokens& a, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(a.groups));
+  const int rc = launch(tokens_kernel<DP, NT, QUADS, false>, grid, dim3(kThreads), 0, s, a);
+  return rc != SHERRY_OK ? rc : launch(tokens_kernel<DP, NT, QUADS, true>, grid, dim3(kThreads), 0, s, a);
+}
 template <int DP, bool QUADS>
 int launch_terms(const Tokens& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(a.groups));
-  return a.type == SHERRY_F32 ? launch(tokens_kernel<DP, 2, QUADS>, grid, dim3(kThreads), 0, s, a)
-                              : launch(tokens_kernel<DP, 1, QUADS>, grid, dim3(kThreads), 0, s, a);
+  return a.type == SHERRY_F32 ? launch_both<DP, 2, QUADS>(a, s) : launch_both<DP, 1, QUADS>(a, s);
 }
 template <int DP>
 int launch_dim(const Tokens& a, hipStream_t s) {
@@ -984,18 +1070,21 @@ int launch_dim(const Tokens& a, hipStream_t s) {
 
 size_t attend_tokens_workspace(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d) {
   const Shape s = shape_of(c, d);
-  return s.split_bytes + s.stat_bytes + s.sum_bytes;
+  return s.split_bytes + s.rest_bytes + s.stat_bytes + s.sum_bytes;
 }
 
 int launch_attend_tokens(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d, hipStream_t s) {
   const Shape sh = shape_of(c, d);
   char* ws = static_cast<char*>(d.workspace);
   const int64_t row = int64_t(d.heads) * c.head_dim;
-  const Tokens a{cache_of(c), d.q, d.out, d.first, d.length, d.mask, reinterpret_cast<float2*>(ws + sh.split_bytes),
-                 reinterpret_cast<float*>(ws + sh.split_bytes + sh.stat_bytes), reinterpret_cast<Split*>(ws), d.q_stride ? d.q_stride : row,
-                 d.out_stride ? d.out_stride : row, d.mask_stride, d.tokens, d.heads, sh.group, sh.gtiles,
-                 sh.per_tile, sh.hp, d.type, d.window, sh.groups, sh.part_rows, d.scale,
-                 FastDiv::of(static_cast<uint32_t>(sh.hp)), FastDiv::of(static_cast<uint32_t>(sh.per_tile))};
+  char* rest = ws + sh.split_bytes;
+  char* stat = rest + sh.rest_bytes;
+  const Tokens a{cache_of(c), d.q, d.out, d.first, d.length, d.mask, reinterpret_cast<float2*>(stat),
+                 reinterpret_cast<float*>(stat + sh.stat_bytes), reinterpret_cast<Split*>(ws),
+                 reinterpret_cast<int64_t*>(rest), d.q_stride ? d.q_stride : row, d.out_stride ? d.out_stride : row,
+                 d.mask_stride, d.tokens, d.heads, sh.group, sh.gtiles, sh.per_tile, sh.hp, d.type, d.window, sh.groups,
+                 sh.part_rows, d.scale, FastDiv::of(static_cast<uint32_t>(sh.hp)),
+                 FastDiv::of(static_cast<uint32_t>(sh.per_tile))};
   switch (padded_dim(c.head_dim)) {
     case 64: return launch_dim<64>(a, s);
     case 128: return launch_dim<128>(a, s);

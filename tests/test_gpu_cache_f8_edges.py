@@ -5,7 +5,13 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_cache_f8 import Attend, _case, dev, ref  # noqa: E402, F401
+from test_gpu_cache_f8 import TOL, Attend, _case, _rel, dev, ref  # noqa: E402, F401
+
+
+def _check_each(a, got, want, tokens, tol):
+    for t in tokens:
+        assert np.all(np.isfinite(got[t])), t
+        assert _rel(got[t], want[t]) <= tol, (t, _rel(got[t], want[t]))
 
 
 # ---- tokens past the table ---------------------------------------------------------
@@ -19,3 +25,96 @@ def test_tokens_far_past_a_long_table(dev, ref, kind, heads, kv, dim, length, ne
     _case("tokens far past", kind, heads, kv, dim, length, new, window)
     c = ref.Cache(np.random.default_rng(30), len(length), 128, kv, 32, dim, [4096] * len(length))
     Attend(dev, ref, c, kind, heads, length, new, window=window).check(ref)
+
+
+# ---- powers far apart --------------------------------------------------------------
+
+def _powers(c, b, name, exponent):
+    """Sets the exponents of sequence b's pages, one a page of its table."""
+    for j, e in enumerate(exponent):
+        c.scale[name][c.table[b, j]] = np.float32(2.0 ** int(e))
+
+
+@pytest.mark.parametrize("kind,base,up", [("f32", -14, 20), ("bf16", -14, 20), ("f16", -14, 20), ("f32", -30, 45), ("bf16", -90, 150)])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 7), (256, 32)])
+@pytest.mark.parametrize("window", [0, 40])
+def test_tokens_v_of_rows_that_a_token_leaves_out(dev, ref, kind, base, up, dim, page, window):
+    """V far larger in rows behind a token, or before its window, than in the rows that it attends to."""
+    _case("tokens v powers", kind, base, up, dim, page, window)
+    n, new = 230, 170
+    c = ref.Cache(np.random.default_rng(31), 1, -(-n // page), 2, page, dim, [n])
+    at = np.arange(c.width) * page
+    _powers(c, 0, "v", base + up * ((at < 100) if window else (at >= 130)))
+    a = Attend(dev, ref, c, kind, 6, [n - new], [new], window=window)
+    got, want = a.run(), ref.attend64(c, a.q, a.first, a.length, a.scale, window)
+    _check_each(a, got, want, range(new), 4 * TOL[kind])
+
+
+@pytest.mark.parametrize("kind,up", [("f32", 18), ("bf16", 30), ("f32", 120), ("f16", 50)])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 10), (256, 32)])
+@pytest.mark.parametrize("window", [0, 40])
+def test_tokens_k_of_rows_that_a_token_leaves_out(dev, ref, kind, up, dim, page, window):
+    """K far larger in rows that some tokens leave out: what these get (the others' scores pass what
+    fp32 tells apart)."""
+    _case("tokens k powers", kind, up, dim, page, window)
+    n, new = 230, 170
+    c = ref.Cache(np.random.default_rng(32), 1, -(-n // page), 2, page, dim, [n])
+    at = np.arange(c.width) * page
+    big = (at < 100) if window else (at >= 130)
+    _powers(c, 0, "k", -6 + up * big)
+    a = Attend(dev, ref, c, kind, 6, [n - new], [new], window=window)
+    got = a.run()
+    with np.errstate(over="ignore", invalid="ignore"):
+        want = ref.attend64(c, a.q, a.first, a.length, a.scale, window)
+    rows = np.flatnonzero(np.repeat(big, page)[:n])
+    own = n - new + np.arange(new)
+    free = [t for t in range(new) if not np.any((rows <= own[t]) & ((rows > own[t] - window) | (window == 0)))]
+    assert len(free) > 20
+    _check_each(a, got, want, free, 4 * TOL[kind])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,page,window", [(64, 16, 0), (64, 5, 90), (128, 20, 0), (128, 64, 300), (256, 16, 70)])
+def test_tokens_over_pages_of_any_powers(dev, ref, kind, dim, page, window):
+    """Powers from page to page anywhere, masks, absent pages, NaN in rows that are left out, pages
+    of zeros (whose power is the smallest that extend gives), runs that end inside tiles."""
+    _case("tokens any powers", kind, dim, page, window)
+    rng = np.random.default_rng(33)
+    length, new = [0, 500, 3, 1100], [150, 40, 1, 5]
+    full = [n + m for n, m in zip(length, new)]
+    c = ref.Cache(rng, 4, -(-max(full) // page), 2, page, dim, full)
+    for b in range(4):
+        _powers(c, b, "v", rng.integers(-60, 20, c.width))
+        _powers(c, b, "k", rng.integers(-45, -5, c.width))
+    for b, j in ((0, 2), (1, 0), (3, 7)):
+        for name in "kv":
+            c.code[name][c.table[b, j]] &= 0x80
+            c.scale[name][c.table[b, j]] = 2.0 ** -100
+    mask = (rng.random((4, c.rows)) < 0.9).astype(np.uint8)
+    for b in range(4):
+        for r in np.flatnonzero(mask[b, :full[b]] == 0):
+            c.code["k"][c.table[b, r // page], :, r % page] = 0x7F
+            c.code["v"][c.table[b, r // page], :, r % page] = 0xFF
+    c.table[1, 3] = -1
+    Attend(dev, ref, c, kind, 6, length, new, window=window, mask=mask).check(ref)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_tokens_nan_on_pages_of_powers_far_apart(dev, ref, kind):
+    """As where the powers are near: NaN in V reaches its value of the tokens that attend to the row,
+    and no others."""
+    for window in (0, 20):
+        _case("tokens nan, powers", kind, window)
+        c = ref.Cache(np.random.default_rng(34), 1, 9, 1, 16, 64, [140])
+        _powers(c, 0, "v", [-5, 30, -40, 7, -5, -6, 20, 0, 1])
+        row = 100
+        c.code["v"][c.table[0, row // 16], 0, row % 16, 5] = 0x7F
+        a = Attend(dev, ref, c, kind, 4, [60], [80], window=window)
+        got = a.run()
+        tokens = np.arange(60, 140)
+        hit = (tokens >= row) & ((tokens < row + window) if window else True)
+        bad = np.isnan(got)
+        assert bad[hit][..., 5].all() and bad.sum() == hit.sum() * 4
+        with np.errstate(invalid="ignore"):
+            want = ref.attend64(c, a.q, a.first, a.length, a.scale, window)
+        _check_each(a, got, want, np.flatnonzero(~hit), 4 * TOL[kind])
