@@ -801,9 +801,9 @@ size_t sherry_cache_attend_tokens_workspace(const sherry_cache_desc* cache,
  * Rows and pages that are left out, outputs of nothing, NaN and infinities are as
  * in sherry_cache_attend; tokens of no sequence are not written.  Scores,
  * statistics and sums are in fp32; q is kept to 22 bits of its head's largest
- * value.  The probabilities are rounded to 22 bits for fp32 outputs; for bf16 and
- * f16 outputs to the 11 of f16, which moves an output by at most 2^-11 sum_r p_r
- * |v_r| before its own rounding; and, times the powers of V's pages, at 2^-35 of the
+ * value.  The probabilities are rounded to 22 bits for fp32 and f16 outputs; for bf16
+ * outputs to 11, which moves an output by at most 2^-11 sum_r p_r |v_r| before its own
+ * rounding; and, times the powers of V's pages, at 2^-35 of the
  * largest power that the token attends to.  Pages may have any powers beside each
  * other; where they lie far apart (V's 2^8, K's 2^16 and more) the call takes up to
  * about twice as long.  tokens * heads < 2^31 (SHERRY_E_SHAPE). */

@@ -38,8 +38,9 @@
 // out change nothing for it, however large they are.  q is scaled by the
 // power of two of its row's largest value: one f16 term holds all of bf16 and f16 values (but for
 // bits below 2^-25 of that largest), two 22 bits of fp32.  Probabilities, times
-// 2^10, are one term for 16-bit outputs (error 2^-11 of each at most, where the output's own
-// rounding is 2^-8 or 2^-11), two for fp32.  Scores, maxima, sums and outputs are
+// 2^10, are one term for bf16 outputs (error 2^-11 of each at most, where the output's own rounding is
+// 2^-8: 1% more error than the rounding alone), two for f16 and fp32 (with one, f16 outputs had 1.1 to 1.5 times the
+// error of their rounding; chunk of 2048 tokens on 30011 rows 1390 us with two against 1095, 6 prompts 91 against 80).  Scores, maxima, sums and outputs are
 // fp32; the maximum is taken anew only when a score passes it by 2^5.
 //
 // Measured (kernel trace, then the join; an f16 product of 8192^3 reaches 1196 TFLOP/s):
@@ -450,13 +451,13 @@ __device__ __forceinline__ void take_turns() {
   }
 }
 
-// DP: head_dim rounded up to 64, 128 or 256; NT: terms of q and p; QUADS: page_size % 4
+// DP: head_dim rounded up to 64, 128 or 256; NT, NP: terms of q and p; QUADS: page_size % 4
 // == 0, so that four rows of V together have one factor (6 prompts 92.7 us against 97.5 without,
 // the chunk 1156 against 1169).  FAR: powers anywhere; takes what the launch without it has left (in one
 // launch with both, a row's own powers in every block's loop: chunk of 2048 tokens on 30011 rows 1159 us against
 // 1108, 6 prompts 89 against 80; a launch with nothing to take is 1 to 2 us).  1024 bf16 tokens on 8000 rows of 128
 // values, powers of pages anywhere in 2^-30 .. 1: 398 us, where they are near each other 191.
-template <int DP, int NT, bool QUADS, bool FAR>
+template <int DP, int NT, int NP, bool QUADS, bool FAR>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_for(DP, NT)))) void tokens_kernel(
     Tokens a) {
   constexpr int KS = DP / 16;   // MFMA steps of a score
@@ -794,7 +795,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
           }
       }
       float sum[2] = {0.0f, 0.0f};
-      u32x4 pf[2][NT];
+      u32x4 pf[2][NP];
       auto probabilities = [&](int st) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -804,10 +805,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
             p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[st >> 1][8 * (st & 1) + 2 * i + j], f, -base));
             sum[j] += p[j];
           }
-          uint32_t t[NT];
-          split<NT>(p[0], p[1], t);
+          uint32_t t[NP];
+          split<NP>(p[0], p[1], t);
 #pragma unroll
-          for (int j = 0; j < NT; ++j) pf[st & 1][j][i] = t[j];
+          for (int j = 0; j < NP; ++j) pf[st & 1][j][i] = t[j];
         }
       };
       // (Of two workgroups on a CU the older one was served first, 2.1 us a block against 3.2, and
@@ -823,8 +824,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
-          for (int j = NT - 1; j >= 0; --j) o[db] = mfma(vf[st & 1][db], pf[st & 1][j], o[db]);
-        if (st < 3) take_turns<DB * NT, (28 + 24 * (NT - 1)) / (DB * NT)>();
+          for (int j = NP - 1; j >= 0; --j) o[db] = mfma(vf[st & 1][db], pf[st & 1][j], o[db]);
+        if (st < 3) take_turns<DB * NP, (28 + 24 * (NP - 1)) / (DB * NP)>();
         fence();
       }
       __builtin_amdgcn_s_setprio(0);
@@ -1048,15 +1049,19 @@ Shape shape_of(const sherry_cache_desc& c, const sherry_attend_tokens_desc& d) {
   s.sum_bytes = size_t(2) * s.groups * s.part_rows * dp * 4;
   return s;
 }
-template <int DP, int NT, bool QUADS>
+template <int DP, int NT, int NP, bool QUADS>
 int launch_both(const Tokens& a, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(a.groups));
-  const int rc = launch(tokens_kernel<DP, NT, QUADS, false>, grid, dim3(kThreads), 0, s, a);
-  return rc != SHERRY_OK ? rc : launch(tokens_kernel<DP, NT, QUADS, true>, grid, dim3(kThreads), 0, s, a);
+  const int rc = launch(tokens_kernel<DP, NT, NP, QUADS, false>, grid, dim3(kThreads), 0, s, a);
+  return rc != SHERRY_OK ? rc : launch(tokens_kernel<DP, NT, NP, QUADS, true>, grid, dim3(kThreads), 0, s, a);
 }
 template <int DP, bool QUADS>
 int launch_terms(const Tokens& a, hipStream_t s) {
-  return a.type == SHERRY_F32 ? launch_both<DP, 2, QUADS>(a, s) : launch_both<DP, 1, QUADS>(a, s);
+  switch (a.type) {
+    case SHERRY_F32: return launch_both<DP, 2, 2, QUADS>(a, s);
+    case SHERRY_F16: return launch_both<DP, 1, 2, QUADS>(a, s);
+    default: return launch_both<DP, 1, 1, QUADS>(a, s);
+  }
 }
 template <int DP>
 int launch_dim(const Tokens& a, hipStream_t s) {

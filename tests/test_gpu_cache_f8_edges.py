@@ -118,3 +118,21 @@ def test_tokens_nan_on_pages_of_powers_far_apart(dev, ref, kind):
         with np.errstate(invalid="ignore"):
             want = ref.attend64(c, a.q, a.first, a.length, a.scale, window)
         _check_each(a, got, want, np.flatnonzero(~hit), 4 * TOL[kind])
+
+
+# ---- f16 outputs -------------------------------------------------------------------
+
+@pytest.mark.parametrize("heads,kv,dim,length,new,window", [
+    (4, 1, 64, [0], [200], 0), (6, 2, 128, [30, 700], [130, 40], 0), (2, 1, 256, [300], [60], 0), (4, 2, 64, [2500, 40], [5, 90], 64)], ids=str)
+def test_tokens_f16_outputs_are_rounded_once(dev, ref, heads, kv, dim, length, new, window):
+    """The output's own rounding is all that an f16 output loses beside what an fp32 output does.
+    With y the unrounded output, |y - want| <= 2e-6 |want| (as fp32 outputs are held to), and the distance
+    to the nearest f16 value changes by no more than its argument:
+    |f16(y) - want| <= |f16(y) - y| + |y - want| <= |f16(want) - want| + 2 |y - want|."""
+    _case("tokens f16", heads, kv, dim, length, new, window)
+    full = [n + m for n, m in zip(length, new)]
+    c = ref.Cache(np.random.default_rng(35), len(full), -(-max(full) // 16), kv, 16, dim, full)
+    a = Attend(dev, ref, c, "f16", heads, length, new, window=window)
+    got, want = a.run(), ref.attend64(c, a.q, a.first, a.length, a.scale, window)
+    least = np.linalg.norm(want.astype(np.float16).astype(np.float64) - want)
+    assert np.linalg.norm(got - want) <= least + 4e-6 * np.linalg.norm(want)
