@@ -168,6 +168,7 @@ __device__ __forceinline__ void store_pages(const Extend& a, int blk) {
   }
   float4 kept[kKeep];
   uint32_t there = 0;
+  bool some = false;  // rows past the kept ones are stored
   const int from = r0 + mine * RPW + lane / LPR;
 #pragma unroll
   for (int i = 0; i < kKeep; ++i) {
@@ -178,12 +179,15 @@ __device__ __forceinline__ void store_pages(const Extend& a, int blk) {
   for (int i = 0; i < kKeep; ++i) see(kept[i]);
   for (int row = from + kKeep * STEP; row < r1; row += STEP) {
     float4 x = make_float4(0, 0, 0, 0);
-    value(row, x);
+    if (value(row, x)) some = true;
     see(x);
   }
   top = wave_max_f32(top);
-  int now = power_of(top);
-  now = now > old ? now : old;
+  int now = 0;  // (none of these rows is stored)
+  if (__any(there != 0 || some)) {
+    now = power_of(top);
+    now = now > old ? now : old;
+  }
   if constexpr (WPP > 1) {
     if (lane == 0) most[wave] = now;
     __syncthreads();
@@ -191,6 +195,7 @@ __device__ __forceinline__ void store_pages(const Extend& a, int blk) {
     for (int i = 0; i < 4; ++i) now = now > most[i] ? now : most[i];
   }
   now = __builtin_amdgcn_readfirstlane(now);
+  if (now == 0) return;  // (every token of the page is left out, and so is the page)
 
   char* rows = (is_k ? a.c.k : a.c.v) + a.c.at(page, h);
   auto store = [&](int row, const float4& x) {

@@ -5,7 +5,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_cache_f8 import TOL, Attend, _case, _rel, dev, ref  # noqa: E402, F401
+from test_gpu_cache_f8 import TOL, Attend, Extend, _case, _rel, dev, ref  # noqa: E402, F401
 
 
 def _check_each(a, got, want, tokens, tol):
@@ -136,3 +136,30 @@ def test_tokens_f16_outputs_are_rounded_once(dev, ref, heads, kv, dim, length, n
     got, want = a.run(), ref.attend64(c, a.q, a.first, a.length, a.scale, window)
     least = np.linalg.norm(want.astype(np.float16).astype(np.float64) - want)
     assert np.linalg.norm(got - want) <= least + 4e-6 * np.linalg.norm(want)
+
+
+# ---- extend: tokens left out, the largest power ---------------------------------------
+
+def _bytes(c):
+    return {n: (c.d[n].cpu().numpy().copy(), c.ds[n].cpu().numpy().view(np.uint32).copy()) for n in "kv"}
+
+
+@pytest.mark.parametrize("page,new,kv", [(16, 3, 2), (16, 40, 5), (128, 200, 1)])
+def test_extend_leaves_pages_alone_that_get_no_rows(dev, ref, page, new, kv):
+    """Every token's position is out of range: no code and no power changes, of a page that holds
+    rows (with a power below the least that extend gives) and of one that holds none."""
+    for n in (5, 0):
+        _case("extend nothing stored", page, new, kv, n)
+        c = ref.Cache(np.random.default_rng(36), 1, 4, kv, page, 64, [n])
+        for name in "kv":
+            if n:
+                c.scale[name][c.table[0, 0]] = 2.0 ** -110
+            c.scale[name][c.table[0, 1:]] = 0.375
+        e = Extend(dev, ref, c, "f32", 4, [n], [new], 64, pos=[-1 - i for i in range(new)])
+        before, q = _bytes(c), e.out.clone()
+        e.sh.sherry_cache_extend(e.cd, e.d)
+        torch.cuda.synchronize()
+        after = _bytes(c)
+        for name in "kv":
+            assert np.array_equal(before[name][0], after[name][0]) and np.array_equal(before[name][1], after[name][1])
+        assert torch.equal(q, e.out)
