@@ -145,9 +145,9 @@ __device__ __forceinline__ void store_pages(const Extend& a, int blk) {
   const int d = 4 * (lane % LPR);
   const bool in = d < a.c.dim;
 
+  auto position = [&](int row) { return a.pos ? as_global(a.pos)[t.t0 + row - t.len] : row; };
   auto value = [&](int row, float4& x) {
-    const int tok = t.t0 + row - t.len;
-    const int pos = a.pos ? as_global(a.pos)[tok] : row;
+    const int tok = t.t0 + row - t.len, pos = position(row);
     if (!in || !a.rope.has(pos)) return false;
     x = is_k ? rotated<TYPE, VEC>(a.rope, a.k, int64_t(tok) * a.k_stride + h * a.c.dim, d, pos)
              : load4<TYPE, VEC>(a.v, int64_t(tok) * a.v_stride + h * a.c.dim + d);
@@ -224,6 +224,11 @@ __device__ __forceinline__ void store_pages(const Extend& a, int blk) {
 #pragma unroll
       for (int w = 0; w < 4; ++w) x[w] = requantized(x[w], ratio);
       *at = x;
+    }
+    for (int row = from; row < r1; row += STEP) {  // rows of tokens that are left out
+      if (!in || a.rope.has(position(row))) continue;
+      SHERRY_GLOBAL uint32_t* at = reinterpret_cast<SHERRY_GLOBAL uint32_t*>(as_global_mut(rows) + int64_t(row - p0) * a.c.dim + d);
+      *at = requantized(*at, ratio);
     }
   }
   if (mine == 0 && lane == 0) as_global_mut(scale)[0] = power(now);

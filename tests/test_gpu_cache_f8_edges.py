@@ -163,3 +163,32 @@ def test_extend_leaves_pages_alone_that_get_no_rows(dev, ref, page, new, kv):
         for name in "kv":
             assert np.array_equal(before[name][0], after[name][0]) and np.array_equal(before[name][1], after[name][1])
         assert torch.equal(q, e.out)
+
+
+@pytest.mark.parametrize("page,new", [(16, 6), (64, 50), (128, 100)])
+def test_extend_rounds_rows_of_tokens_left_out_as_the_page_s_others(dev, ref, page, new):
+    """The power of a page that holds rows rises: every row that gets no new codes follows it, the
+    rows of tokens that are left out too."""
+    _case("extend left out", page, new)
+    rng = np.random.default_rng(37)
+    c = ref.Cache(rng, 1, 2, 2, page, 64, [page])
+    for name in "kv":
+        c.scale[name][c.table[0, 0]] = 2.0 ** -6
+    n = 7
+    pos = np.arange(n, n + new)
+    out = np.arange(new) % 3 == 1
+    pos[out] = -1
+    e = Extend(dev, ref, c, "f32", 2, [n], [new], 64, pos=pos, cos=True,
+               values=lambda name, x: np.multiply(x, np.float32(64), out=x))
+    e.sh.sherry_cache_extend(e.cd, e.d)
+    torch.cuda.synchronize()
+    stored = np.zeros(page, bool)
+    stored[[n + i for i in range(new) if not out[i] and n + i < page]] = True
+    p = c.table[0, 0]
+    for name in "kv":
+        code, scale = c.read(name)
+        for h in range(2):
+            ratio = 2.0 ** -6 / float(scale[p, h])
+            assert ratio < 1
+            want = ref.encode(ref.VALUES[c.code[name][p, h]] * ratio)
+            assert np.array_equal(code[p, h][~stored], want[~stored])
