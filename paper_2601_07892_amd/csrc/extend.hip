@@ -110,6 +110,10 @@ __device__ __forceinline__ int power_of(float top) {
   return e > 127 + kLeast ? e : 127 + kLeast;
 }
 __device__ __forceinline__ float power(int biased) { return __uint_as_float(uint32_t(biased) << 23); }
+// Its reciprocal (2^-127, of the largest, is a subnormal number).
+__device__ __forceinline__ float over_power(int biased) {
+  return __uint_as_float(biased < 254 ? uint32_t(254 - biased) << 23 : 0x00400000u);
+}
 
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
   const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
@@ -200,7 +204,7 @@ __device__ __forceinline__ void store_pages(const Extend& a, int blk) {
   char* rows = (is_k ? a.c.k : a.c.v) + a.c.at(page, h);
   auto store = [&](int row, const float4& x) {
     auto one = [&](float v) {
-      return fabsf(v) < __builtin_huge_valf() ? v * power(254 - now) : __uint_as_float(0x7FC00000u);
+      return fabsf(v) < __builtin_huge_valf() ? v * over_power(now) : __uint_as_float(0x7FC00000u);
     };
     *reinterpret_cast<SHERRY_GLOBAL uint32_t*>(as_global_mut(rows) + int64_t(row - p0) * a.c.dim + d) =
         codes4(one(x.x), one(x.y), one(x.z), one(x.w));

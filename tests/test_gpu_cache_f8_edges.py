@@ -192,3 +192,22 @@ def test_extend_rounds_rows_of_tokens_left_out_as_the_page_s_others(dev, ref, pa
             assert ratio < 1
             want = ref.encode(ref.VALUES[c.code[name][p, h]] * ratio)
             assert np.array_equal(code[p, h][~stored], want[~stored])
+
+
+@pytest.mark.parametrize("old", [2.0 ** 127, 2.0 ** 126, float("inf")])
+@pytest.mark.parametrize("page", [16, 128])
+def test_extend_into_pages_of_the_largest_power(dev, ref, old, page):
+    """A page's power of 2^127 (an infinity counts as that) stays, and values near fp32's largest are
+    codes about 1 of it."""
+    _case("extend largest power", old, page)
+
+    def values(name, x):
+        x[:] = np.float32(3e38) * np.random.default_rng(38).uniform(-1, 1, x.shape).astype(np.float32)
+
+    c = ref.Cache(np.random.default_rng(39), 1, 1, 2, page, 64, [3])
+    for name in "kv":
+        c.scale[name][c.table[0, 0]] = old
+    with np.errstate(all="ignore"):
+        Extend(dev, ref, c, "f32", 2, [3], [9], 64, values=values, cos=False).check(ref)
+    code, scale = c.read("v")
+    assert np.all(scale[c.table[0, 0]] == min(old, 2.0 ** 127)) and np.any(ref.VALUES[code[c.table[0, 0], :, 3:12]] != 0)
