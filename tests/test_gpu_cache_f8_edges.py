@@ -5,7 +5,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_cache_f8 import TOL, Attend, Extend, _case, _rel, dev, ref  # noqa: E402, F401
+from test_gpu_cache_f8 import TOL, Attend, Extend, _case, _i32, _rel, dev, ref  # noqa: E402, F401
 
 
 def _check_each(a, got, want, tokens, tol):
@@ -211,3 +211,117 @@ def test_extend_into_pages_of_the_largest_power(dev, ref, old, page):
         Extend(dev, ref, c, "f32", 2, [3], [9], 64, values=values, cos=False).check(ref)
     code, scale = c.read("v")
     assert np.all(scale[c.table[0, 0]] == min(old, 2.0 ** 127)) and np.any(ref.VALUES[code[c.table[0, 0], :, 3:12]] != 0)
+
+
+# ---- replays with new lengths, against the plain references -----------------------------
+
+def test_replays_with_new_lengths_give_what_the_references_do(dev, ref):
+    """extend and attention of its tokens in one graph, under fixed descriptors and workspace:
+    every replay's codes, powers and outputs against the references, with eager work between."""
+    rng = np.random.default_rng(40)
+    c = ref.Cache(rng, 2, 40, 2, 16, 64, [640, 640])
+    e = Extend(dev, ref, c, "f32", 4, [0, 0], [9, 9], 64)
+    a = Attend(dev, ref, c, "f32", 4, [0, 0], [9, 9])
+    e.cd, a.d.length, a.d.first, a.d.q = a.cd, e.d.length, e.d.first, e.d.q_out
+    a.d.q_stride = a.d.out_stride = 0
+    code, scale = {n: c.d[n].clone() for n in "kv"}, {n: c.ds[n].clone() for n in "kv"}
+    start = {n: (c.code[n].copy(), c.scale[n].copy()) for n in "kv"}
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        e.sh.sherry_cache_extend(e.cd, e.d)
+        a.sh.sherry_cache_attend_tokens(a.cd, a.d)
+    for length in ([0, 0], [600, 3], [20, 631], [1, 0], [600, 3]):
+        _case("replay", length)
+        for n in "kv":
+            c.code[n], c.scale[n] = start[n][0].copy(), start[n][1].copy()
+            c.d[n].copy_(code[n])
+            c.ds[n].copy_(scale[n])
+        e.length = np.array(length)
+        e.dl.copy_(_i32(length, dev))
+        e.out.fill_(9.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want, powers, there, _ = ref.extend_plain(c, e.host, e.first, e.length, e.cos, e.sin, 64, False)
+        assert there.all()
+        for n in "kv":
+            got, got_scale = c.read(n)
+            assert np.array_equal(got, want[n]) and np.array_equal(got_scale, powers[n], equal_nan=True)
+            c.code[n], c.scale[n] = got, got_scale
+        q = e.out.float().cpu().numpy().reshape(18, 4, 64)
+        out = a.out.double().cpu().numpy().reshape(18, 4, 64)
+        _check_each(a, out, ref.attend64(c, q, e.first, e.length, a.scale), range(18), 4 * TOL["f32"])
+
+
+# ---- strides and pools beyond 2^31 bytes ------------------------------------------------
+
+def _far_apart(c, dev):
+    """c.to(dev) with its pages so far from each other that the pools pass 2^31 bytes."""
+    import paper_2601_07892_amd as sh
+    whole = c.kv * c.page * c.dim
+    small = c.stride
+    c.stride = whole
+    cd = c.to(dev)
+    c.stride = ((2 ** 31 // (c.pages - 1)) // 16 + 1) * 16
+    for n in "kv":
+        far = torch.zeros(c.pages * c.stride, dtype=torch.uint8, device=dev)
+        far.view(c.pages, c.stride)[:, :whole] = c.d[n]
+        c.d[n] = far
+    cd.k, cd.v, cd.page_stride = c.d["k"].data_ptr(), c.d["v"].data_ptr(), c.stride
+    assert cd.type == sh.SHERRY_F8 and (c.pages - 1) * c.stride >= 2 ** 31 and small == whole
+    return cd
+
+
+def test_pools_beyond_31_bits(dev, ref):
+    """extend, attention of many tokens and of one, over pages up to 2^31 bytes and more from the pool's start."""
+    import paper_2601_07892_amd as sh
+    _case("far pages")
+    c = ref.Cache(np.random.default_rng(41), 2, 4, 2, 16, 64, [30, 9])
+    c.table[0, 0], c.table[1, 0] = c.pages - 1, c.pages - 2  # (taken from no other place)
+    spare = [p for p in range(c.pages - 2) if p not in set(c.table.ravel())]
+    seen = set()
+    for i in np.ndindex(*c.table.shape):  # every page once
+        if int(c.table[i]) in seen:
+            c.table[i] = spare.pop()
+        seen.add(int(c.table[i]))
+    for name in "kv":
+        c.code[name] = ref.encode(np.random.default_rng(42).standard_normal(c.code[name].shape) * 40)
+        c.scale[name][:] = 2.0 ** -6
+    e = Extend(dev, ref, c, "f32", 4, [30, 9], [20, 12], 64)
+    e.cd = _far_apart(c, dev)
+    want, powers, _, _ = ref.extend_plain(c, e.host, e.first, e.length, e.cos, e.sin, 64, False)
+    sh.sherry_cache_extend(e.cd, e.d)
+    torch.cuda.synchronize()
+    whole = c.kv * c.page * c.dim
+    for n in "kv":
+        got = c.d[n].view(c.pages, c.stride)[:, :whole].cpu().numpy().reshape(c.code[n].shape)
+        assert np.array_equal(got, want[n]) and np.array_equal(c.ds[n].cpu().numpy(), powers[n])
+        c.code[n], c.scale[n] = got, powers[n]
+    pools, scales, table = dict(c.d), dict(c.ds), c.dt  # (the harness below makes others)
+    c.stride = whole
+    a = Attend(dev, ref, c, "f32", 4, [30, 9], [20, 12])
+    a.cd = e.cd
+    c.d, c.ds = pools, scales
+    a.check(ref)
+    assert table.data_ptr() == e.cd.table
+    d, out = sh.sherry_attend_desc(), torch.empty((2, 256), device=dev)
+    q = torch.from_numpy(np.random.default_rng(43).standard_normal((2, 4, 64)).astype(np.float32))
+    qd, dl = q.to(dev), _i32([50, 21], dev)
+    d.q, d.out, d.length, d.heads, d.type, d.scale = qd.data_ptr(), out.data_ptr(), dl.data_ptr(), 4, sh.SHERRY_F32, 0.125
+    n = sh.sherry_cache_attend_workspace(e.cd, d)
+    ws = torch.empty(n, dtype=torch.uint8, device=dev)
+    d.workspace, d.workspace_bytes = ws.data_ptr(), n
+    sh.sherry_cache_attend(e.cd, d)
+    torch.cuda.synchronize()
+    first = np.array([0, 1, 2])
+    want = ref.attend64(c, q.numpy(), first, np.array([49, 20]), 0.125)
+    _check_each(a, out.double().cpu().numpy().reshape(2, 4, 64), want, range(2), 4 * TOL["f32"])
+
+
+@pytest.mark.parametrize("kind,dim,page,extra", [("f32", 64, 16, 16), ("bf16", 128, 20, 48), ("f16", 256, 7, 4096)])
+def test_pages_further_apart_than_they_are_long(dev, ref, kind, dim, page, extra):
+    _case("page stride", kind, dim, page, extra)
+    full = [150, 33, 0]
+    c = ref.Cache(np.random.default_rng(44), 3, 1 + 150 // page, 2, page, dim, full, extra=extra)
+    Attend(dev, ref, c, kind, 6, [100, 0, 0], [50, 33, 0]).check(ref)
