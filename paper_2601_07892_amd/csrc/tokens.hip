@@ -85,6 +85,10 @@ constexpr float kUp = 10.0f;         // p is held times 2^kUp
 // Scores may pass the maximum by this (with 0, where o is rescaled at every new maximum, 6
 // prompts 94.4 us against 92.7).
 constexpr float kLazy = 5.0f;
+// From here on a score's own rounding is in the way: an exponent taken from the unrounded product is
+// off from the maximum by a part of the rounding, without bound, and kUp would be rounded too.
+constexpr float kLarge = 0x1p22f;
+constexpr float kNowhere = -__FLT_MAX__;  // base where nothing is attended to yet
 // A code times 2^0 .. 2^-15 is exact in f16: K's powers may differ by this in a block, V's in a block and
 // from one block's largest to another's.
 constexpr int kFarK = 15, kFarV = 8, kFarBlocks = 7;
@@ -542,7 +546,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
     float factor = 0.0f;
 
     v16f o[DB];
-    float m = kMinusInf, base = 0.0f, l = 0.0f;
+    float base = kNowhere, limit = kMinusInf, l = 0.0f;  // limit: scores past it move base
     int vrun = 1;  // o is over this power of two
 
     // ---- what the waves find out about blocks of rows, each about every fourth block:
@@ -768,14 +772,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 #pragma unroll
       for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i >> 4][i & 15]);
       top = max_of_halves(top) * f;
-      if (FAR ? __any(top > m + kLazy || vref > vrun) : __any(top > m + kLazy) || vref > vrun) {
-        const bool up = top > m;
-        const float to = up ? top - kUp : base;
-        float down = m == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(base - to);
-        if (up) {
-          base = to;
-          m = top;
-        }
+      if (FAR ? __any(top > limit || vref > vrun) : __any(top > limit) || vref > vrun) {
+        const float over = fabsf(top) < kLarge ? top - kUp : top, to = over > base ? over : base;
+        float down = __builtin_amdgcn_exp2f(base - to);
+        base = to;
+        limit = fabsf(to) < kLarge ? to + (kUp + kLazy) : kMinusInf;
         l *= down;
         if constexpr (FAR) down = __builtin_amdgcn_ldexpf(down, vrun - vref);
         else down *= power(vref - vrun < 126 ? 127 - (vref - vrun) : 1);  // (so far only where o is 0)
@@ -784,6 +785,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         for (int i = 0; i < DB; ++i)
 #pragma unroll
           for (int j = 0; j < 16; ++j) o[i][j] *= down;
+      }
+      // (all scores rounded once, as top is.  A branch of its own: inside the one before, 1024 fp32 tokens on 8000
+      // rows of 128 values took 338 us against 317)
+      if (!FAR && __builtin_expect(__any(limit == kMinusInf && base > kNowhere), 0)) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sc[i >> 4][i & 15] *= f;
+        f = 1.0f;
       }
       if constexpr (FAR) {  // p's sum, and the scores whose p is times V's powers
 #pragma unroll

@@ -325,3 +325,27 @@ def test_pages_further_apart_than_they_are_long(dev, ref, kind, dim, page, extra
     full = [150, 33, 0]
     c = ref.Cache(np.random.default_rng(44), 3, 1 + 150 // page, 2, page, dim, full, extra=extra)
     Attend(dev, ref, c, kind, 6, [100, 0, 0], [50, 33, 0]).check(ref)
+
+
+# ---- scores of any size ------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("dim,page,far", [(64, 16, False), (128, 10, False), (256, 32, False), (64, 32, True), (128, 16, True)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_tokens_scores_far_beyond_24_bits(dev, ref, kind, dim, page, far, sign):
+    """Scores of 2^12 to 2^60, exact in fp32 (one value of q counts, a power of two): the rows of the
+    largest score share a token's output, the others are too far below it."""
+    _case("tokens scores", kind, dim, page, far, sign)
+    rng = np.random.default_rng(45)
+    n, new = 310, 49
+    c = ref.Cache(rng, 1, -(-n // page), 2, page, dim, [n])
+    c.code["k"][..., 0] = rng.integers(0x30, 0x7F, c.code["k"].shape[:3])  # 0.5 to 448
+    for j in range(c.width):
+        c.scale["k"][c.table[0, j]] = 2.0 ** (20 - (int(rng.integers(0, 30)) if far else j % 2))
+    q = np.zeros((new, 4, dim))
+    q[:, :, 0] = sign * 2.0 ** (np.arange(new)[:, None] - 16)
+    if kind == "f16":
+        q = np.clip(q, -2.0 ** 15, 2.0 ** 15)
+    a = Attend(dev, ref, c, kind, 4, [n - new], [new], scale=1.0, q=q)
+    got, want = a.run(), ref.attend64(c, a.q, a.first, a.length, a.scale)
+    _check_each(a, got, want, range(new), 4 * TOL[kind])
