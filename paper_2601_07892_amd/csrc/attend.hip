@@ -789,7 +789,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(G::
             for (int i = G::QT - 1; i >= 0; --i) s[t] = mfma<G::F16>(kf, qf[i][st], s[t]);
           }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3] * (G::F8 ? factor * ksc[i] : factor);
+        for (int i = 0; i < 8; ++i) {
+          x[i] = s[i >> 2][i & 3] * factor;
+          if constexpr (G::F8) x[i] *= ksc[i];  // (last: the product of the factors may pass fp32 where the score is 0)
+        }
       }
       if (more) fetch_k(slot, next);
       uint32_t mine = 0xFF;  // bit i: row of x[i] is attended to

@@ -349,3 +349,89 @@ def test_tokens_scores_far_beyond_24_bits(dev, ref, kind, dim, page, far, sign):
     a = Attend(dev, ref, c, kind, 4, [n - new], [new], scale=1.0, q=q)
     got, want = a.run(), ref.attend64(c, a.q, a.first, a.length, a.scale)
     _check_each(a, got, want, range(new), 4 * TOL[kind])
+
+
+# ---- one token ------------------------------------------------------------------------------
+
+def _one(dev, ref, c, kind, heads, lens, window=0, mask=None, scale=None, q=None):
+    """out [batch][heads][dim] of the one-token form, q as it took it, and its scale."""
+    import paper_2601_07892_amd as sh
+    cd, scale = c.to(dev), float(np.float32(c.dim ** -0.5 if scale is None else scale))
+    if q is None:
+        q = np.random.default_rng(46).standard_normal((c.batch, heads, c.dim)) * 2
+    q = torch.from_numpy(q.astype(np.float32)).to(ref.TYPES[kind])
+    qd, out, dl = q.to(dev), torch.empty_like(q, device=dev), _i32(lens, dev)
+    dm = None if mask is None else torch.from_numpy(mask).to(dev)
+    d = sh.sherry_attend_desc()
+    d.q, d.out, d.length, d.mask, d.mask_stride = qd.data_ptr(), out.data_ptr(), dl.data_ptr(), ref.at(dm), c.rows
+    d.heads, d.type, d.window, d.scale = heads, ref.CODES[kind], window, scale
+    n = sh.sherry_cache_attend_workspace(cd, d)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device=dev)
+    d.workspace, d.workspace_bytes = ws.data_ptr(), n
+    sh.sherry_cache_attend(cd, d)
+    torch.cuda.synchronize()
+    return out.double().cpu().numpy(), q.float().numpy(), scale
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("dim,page,window", [(64, 16, 0), (128, 10, 300), (256, 32, 70), (64, 1, 0)])
+def test_one_token_over_pages_of_any_powers(dev, ref, kind, dim, page, window):
+    _case("one token, any powers", kind, dim, page, window)
+    rng = np.random.default_rng(47)
+    lens = [700, 33, 1, 90]
+    c = ref.Cache(rng, 4, -(-700 // page), 2, page, dim, lens)
+    for b in range(4):
+        _powers(c, b, "v", rng.integers(-60 if kind != "f16" else -15, 20 if kind != "f16" else 3, c.width))
+        _powers(c, b, "k", rng.integers(-45, -5, c.width))
+    mask = (rng.random((4, c.rows)) < 0.8).astype(np.uint8)
+    mask[2, 0] = 1
+    for m in (None, mask):
+        got, q, scale = _one(dev, ref, c, kind, 6, lens, window, m)
+        want = ref.attend64(c, q, np.arange(5), np.array(lens) - 1, scale, window, m)
+        _check_each(None, got, want, range(4), 4 * TOL[kind])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 10)])
+@pytest.mark.parametrize("many", [False, True])
+def test_zeros_on_pages_of_large_powers(dev, ref, kind, dim, page, many):
+    """A row that is masked has given its page a power that times q's passes fp32; the others are
+    zeros of that page, and their scores 0.  One new token, and many."""
+    _case("zeros", kind, dim, page, many)
+    n = 5 * page + 1
+    c = ref.Cache(np.random.default_rng(48), 1, 6, 2, page, dim, [n])
+    p = c.table[0, 2]
+    c.code["k"][p] &= 0x80
+    c.code["k"][p, :, 3] = 0x7E
+    c.scale["k"][p] = 2.0 ** 119
+    mask = np.ones((1, c.rows), np.uint8)
+    mask[0, 2 * page + 3] = 0
+    q = np.random.default_rng(49).standard_normal((1, 4, dim)) * 2.0 ** 12
+    if many:
+        a = Attend(dev, ref, c, kind, 4, [n - 1], [1], mask=mask, scale=2.0 ** -3, q=q)
+        got, q, scale = a.run(), a.q, a.scale
+    else:
+        got, q, scale = _one(dev, ref, c, kind, 4, [n], mask=mask, scale=2.0 ** -3, q=q)
+    want = ref.attend64(c, q, np.arange(2), np.array([n - 1]), scale, mask=mask)
+    assert np.all(np.isfinite(got))
+    # (scores of some 2^14 times 2^-22 of the largest terms, 2^-6 in the exponents)
+    assert _rel(got[0], want[0]) <= 2.0 ** -4
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 10), (256, 32)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_one_token_scores_far_beyond_24_bits(dev, ref, kind, dim, page, sign):
+    """As with many tokens."""
+    _case("one token, scores", kind, dim, page, sign)
+    rng = np.random.default_rng(50)
+    lens = [310 - i for i in range(40)]
+    c = ref.Cache(rng, 40, -(-310 // page), 2, page, dim, lens)
+    c.code["k"][..., 0] = rng.integers(0x30, 0x7F, c.code["k"].shape[:3])
+    for b in range(40):
+        _powers(c, b, "k", [20 - j % 2 for j in range(c.width)])
+    q = np.zeros((40, 4, dim))
+    q[:, :, 0] = sign * 2.0 ** (np.arange(40)[:, None] - 16)
+    got, q, scale = _one(dev, ref, c, kind, 4, lens, scale=1.0, q=q)
+    want = ref.attend64(c, q, np.arange(41), np.array(lens) - 1, scale)
+    _check_each(None, got, want, range(40), 4 * TOL[kind])
