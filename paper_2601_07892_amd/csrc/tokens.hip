@@ -39,7 +39,7 @@
 // power of two of its row's largest value: one f16 term holds all of bf16 and f16 values (but for
 // bits below 2^-25 of that largest), two 22 bits of fp32.  Probabilities, times
 // 2^10, are one term for bf16 outputs (error 2^-11 of each at most, where the output's own rounding is
-// 2^-8: 1% more error than the rounding alone), two for f16 and fp32 (with one, f16 outputs had 1.1 to 1.5 times the
+// 2^-8: 0.1 to 0.6% more error than the rounding alone), two for f16 and fp32 (with one, f16 outputs had 1.1 to 1.5 times the
 // error of their rounding; chunk of 2048 tokens on 30011 rows 1390 us with two against 1095, 6 prompts 91 against 80).  Scores, maxima, sums and outputs are
 // fp32; the maximum is taken anew only when a score passes it by 2^5.
 //
@@ -460,7 +460,8 @@ __device__ __forceinline__ void take_turns() {
 // the chunk 1156 against 1169).  FAR: powers anywhere; takes what the launch without it has left (in one
 // launch with both, a row's own powers in every block's loop: chunk of 2048 tokens on 30011 rows 1159 us against
 // 1108, 6 prompts 89 against 80; a launch with nothing to take is 1 to 2 us).  1024 bf16 tokens on 8000 rows of 128
-// values, powers of pages anywhere in 2^-30 .. 1: 398 us, where they are near each other 191.
+// values, powers of pages anywhere in 2^-30 .. 1: 362 us, where they are near each other 192 (64 values 274 and 125, 256 950
+// and 480, fp32 of 128 650 and 317).
 template <int DP, int NT, int NP, bool QUADS, bool FAR>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_for(DP, NT)))) void tokens_kernel(
     Tokens a) {
@@ -793,14 +794,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         for (int i = 0; i < 32; ++i) sc[i >> 4][i & 15] *= f;
         f = 1.0f;
       }
-      if constexpr (FAR) {  // p's sum, and the scores whose p is times V's powers
+      float from = base;
+      if constexpr (FAR) {  // p's sum, and the exponents of p times V's powers
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            l += __builtin_amdgcn_exp2f(sc[h][i] - base);
-            sc[h][i] += static_cast<float>(static_cast<int>(exponent_of(lds.ve, h, i)) - vrun);
+            // (over base first: a large score's rounding is more than V's exponent)
+            const float x = sc[h][i] - base;
+            l += __builtin_amdgcn_exp2f(x);
+            sc[h][i] = x + static_cast<float>(static_cast<int>(exponent_of(lds.ve, h, i)) - vrun);
           }
+        from = 0.0f;
       }
       float sum[2] = {0.0f, 0.0f};
       u32x4 pf[2][NP];
@@ -810,7 +815,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
           float p[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[st >> 1][8 * (st & 1) + 2 * i + j], f, -base));
+            p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[st >> 1][8 * (st & 1) + 2 * i + j], f, -from));
             sum[j] += p[j];
           }
           uint32_t t[NP];

@@ -351,6 +351,26 @@ def test_tokens_scores_far_beyond_24_bits(dev, ref, kind, dim, page, far, sign):
     _check_each(a, got, want, range(new), 4 * TOL[kind])
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 10), (256, 1)])
+def test_tokens_large_scores_on_pages_of_powers_far_apart(dev, ref, kind, dim, page):
+    """V's powers count whatever the scores' size is (they are a part of the exponent in which the
+    scores are)."""
+    _case("tokens scores, powers", kind, dim, page)
+    rng = np.random.default_rng(51)
+    n, new = 150, 60
+    c = ref.Cache(rng, 1, -(-n // page), 2, page, dim, [n])
+    c.code["k"][..., 0] = rng.integers(0x30, 0x7F, c.code["k"].shape[:3])
+    _powers(c, 0, "k", [20] * c.width)
+    _powers(c, 0, "v", [(-20, 3, -9, -1)[j % 4] for j in range(c.width)])
+    q = np.zeros((new, 4, dim))
+    # (every token another order of the rows: its own window)
+    q[:, :, 0] = 2.0 ** (np.arange(new)[:, None] % 30 - 12)
+    a = Attend(dev, ref, c, kind, 4, [n - new], [new], scale=1.0, q=q, window=13)
+    got, want = a.run(), ref.attend64(c, a.q, a.first, a.length, a.scale, 13)
+    _check_each(a, got, want, range(new), 4 * TOL[kind])
+
+
 # ---- one token ------------------------------------------------------------------------------
 
 def _one(dev, ref, c, kind, heads, lens, window=0, mask=None, scale=None, q=None):
