@@ -625,9 +625,9 @@ typedef struct sherry_append_desc {
  * sequences share, the same row of a page.  Input rows are
  * aligned to their element.  cache->table and the rows that exist are not
  * changed; lengths are the caller's.  SHERRY_F8 caches, where a row's power of two
- * is its page's, are sherry_cache_extend's (SHERRY_E_INVALID here).  Calls of 2^32 threads and more are refused
- * (SHERRY_E_SHAPE): a token takes 256 for every 16 rows of q, k and v of up to 64
- * values, 8 of up to 128, 4 of more. */
+ * is its page's, are sherry_cache_extend's (SHERRY_E_INVALID here).  Calls of 2^32
+ * threads and more are refused (SHERRY_E_SHAPE): a token takes 256 for every 16 rows
+ * of q, k and v of up to 64 values, 8 of up to 128, 4 of more. */
 int sherry_cache_append(const sherry_cache_desc* cache, const sherry_append_desc* args,
                         void* stream);
 
@@ -756,11 +756,12 @@ typedef struct sherry_extend_desc {
  * halve from one to the next).  A new code is the e4m3 value nearest to value /
  * power, ties to even; infinities and NaN become NaN.  A token whose row (or, with
  * cos, position) is out of range, or whose page does not exist, is left out
- * entirely, tokens outside first[0] .. first[batch] - 1 too.  No page that gets rows
- * may belong to another sequence (sherry_cache_fork sees to that); lengths are the
- * caller's.  Calls of 2^32 threads and more are refused (SHERRY_E_SHAPE): at most
- * 256 for every 4 heads of a token's q and for every head of k and of v of a page,
- * tokens / page_size + 2 batch pages. */
+ * entirely (its row, if it has one, is one of its page's others), tokens outside
+ * first[0] .. first[batch] - 1 too.  No page that gets rows may stand anywhere else
+ * in the table (sherry_cache_fork sees to that); lengths are the caller's.  Calls of
+ * 2^32 threads and more are refused (SHERRY_E_SHAPE): at most 256 for every 4 heads of
+ * a token's q and for every head of k and of v of a page, tokens / page_size + 2 batch
+ * pages. */
 int sherry_cache_extend(const sherry_cache_desc* cache, const sherry_extend_desc* args,
                         void* stream);
 
@@ -859,9 +860,11 @@ size_t sherry_cache_fork_workspace(const sherry_cache_desc* cache, const sherry_
  * unless all the places where it stands are written: then the last of them (the
  * highest b, then the highest place) keeps it.  Free pages are those that no new
  * sequence reaches; they are given out from the lowest, to the places in order.
- * Entries of table_out behind a sequence's last page, and of pages outside [0,
- * pages), are -1.  Any sequence may be the parent of any number of others.
- * batch * table_width < 2^31 (SHERRY_E_SHAPE). */
+ * They are not cleared: rows before from_row that did not exist, on a page that now
+ * does, hold anything (and of SHERRY_F8 the page's power is any).  Entries of table_out
+ * behind a sequence's last page, and of pages outside [0, pages), are -1.  Any sequence
+ * may be the parent of any number of others.  batch * table_width < 2^31
+ * (SHERRY_E_SHAPE). */
 int sherry_cache_fork(const sherry_cache_desc* cache, const sherry_fork_desc* args, void* stream);
 
 typedef struct sherry_compact_desc {

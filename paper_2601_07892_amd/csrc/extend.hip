@@ -23,7 +23,7 @@
 //
 // Measured: 32 tokens of 32 sequences, 24 + 16 heads of 128 values, fp32 4.4 us, all of it a
 // launch and its chain of reads; 8 prompts of 37 to 2048 tokens, 32 + 16 heads of 64 bf16
-// values, 60 MB 21.0 us, 2.85 TB/s.
+// values, 60 MB 20.5 us, 2.9 TB/s.
 #include "rotary.h"
 
 namespace sherry {

@@ -31,28 +31,29 @@
 //    written to LDS transposed, and with its rows in the order that this asks for.
 //
 // Precision.  e4m3 codes are exact in f16, and so are their products with powers of
-// two down to 2^-15, which take the pages' scales.  Where the powers of a tile lie further apart, in a
-// block or from block to block, a launch of its own (FAR) takes the rest of the workgroup's run: codes are
-// operands as they are, the scores are multiplied by the powers of K's pages, and the probabilities by those of
-// V's over the largest that the token itself has attended to (rounded at 2^-35 of that).  So rows that a token leaves
-// out change nothing for it, however large they are.  q is scaled by the
-// power of two of its row's largest value: one f16 term holds all of bf16 and f16 values (but for
-// bits below 2^-25 of that largest), two 22 bits of fp32.  Probabilities, times
-// 2^10, are one term for bf16 outputs (error 2^-11 of each at most, where the output's own rounding is
-// 2^-8: 0.1 to 0.6% more error than the rounding alone), two for f16 and fp32 (with one, f16 outputs had 1.1 to 1.5 times the
-// error of their rounding; chunk of 2048 tokens on 30011 rows 1390 us with two against 1095, 6 prompts 91 against 80).  Scores, maxima, sums and outputs are
-// fp32; the maximum is taken anew only when a score passes it by 2^5.
+// two down to 2^-15, which take the pages' scales.  Where the powers of a tile lie further apart,
+// in a block or from block to block, a launch of its own (FAR) takes the rest of the workgroup's
+// run: codes are operands as they are, the scores are multiplied by the powers of K's pages, and the
+// probabilities by those of V's over the largest that the token itself has attended to (rounded at
+// 2^-35 of that).  So rows that a token leaves out change nothing for it, however large they are.
+// q is scaled by the power of two of its row's largest value: one f16 term holds all of bf16 and f16
+// values (but for bits below 2^-25 of that largest), two 22 bits of fp32.  Probabilities, times 2^10,
+// are one term for bf16 outputs (error 2^-11 of each at most, where the output's own rounding is 2^-8:
+// 0.1 to 0.6% more error than that rounding alone), two for f16 and fp32 (with one, f16 outputs had 1.1
+// to 1.5 times the error of their rounding; chunk of 2048 tokens on 30011 rows 1390 us with two against
+// 1095, 6 prompts 91 against 80).  Scores, maxima, sums and outputs are fp32; the maximum is taken anew
+// only when a score passes it by 2^5.
 //
 // Measured (kernel trace, then the join; an f16 product of 8192^3 reaches 1196 TFLOP/s):
-//  * a chunk of 2048 tokens on 30011 rows, 32 heads over 8 of 128 values, bf16: 1100 to 1190 us
-//    with the clock, and 16; 1.04 PFLOP at 880 to 950 TFLOP/s.  The matrix cores are busy for 42% of the
+//  * a chunk of 2048 tokens on 30011 rows, 32 heads over 8 of 128 values, bf16: 1110 to 1250 us
+//    with the clock, and 16; 1.04 PFLOP at 830 to 940 TFLOP/s.  The matrix cores are busy for 41% of the
 //    cycles, vector instructions issue in most of the rest.  Two rows of q per lane, which halve LDS's
 //    part, left one wave per SIMD: 2208 us.
-//  * 6 prompts of 100 to 2500 tokens, window 1024, 24 heads over 8 of 128 values: 76 and 10.6; a workgroup
+//  * 6 prompts of 100 to 2500 tokens, window 1024, 24 heads over 8 of 128 values: 78 and 10.6; a workgroup
 //    has some two tiles of six blocks, 2.2 us for its place, some 10 us a tile beside its blocks.
-//  * 16 drafts of 5 tokens on 1 to 6000 rows, 32 heads over 8 of 64 values, fp32: 23.6 and 7.6.
-//  * 1024 tokens on 8000 rows, 32 heads over 8 (with the join): bf16 133, 190 and 466 us with 64, 128 and
-//    256 values, fp32, twice the products, 171, 383 and 827.
+//  * 16 drafts of 5 tokens on 1 to 6000 rows, 32 heads over 8 of 64 values, fp32: 22.4 and 7.6.
+//  * 1024 tokens on 8000 rows, 32 heads over 8 (whole calls), 64, 128 and 256 values: bf16 125, 192 and 481 us, f16
+//    153, 235 and 558, fp32, twice the products, 167, 325 and 845.
 #include <type_traits>
 
 #include "cache_internal.h"
